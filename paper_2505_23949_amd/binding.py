@@ -22,6 +22,7 @@ TSENOR_ERR_PARAM = -5
 TSENOR_ERR_WORKSPACE = -6
 TSENOR_ERR_HIP = -7
 TSENOR_ERR_TOO_LARGE = -8
+TSENOR_ERR_ALIGN = -9
 
 TSENOR_F32 = 0
 TSENOR_BF16 = 1
@@ -43,6 +44,9 @@ EXPORTS = (
     "tsenor_workspace_bytes", "tsenor_mask_ex", "tsenor_mask_batched", "tsenor_mask", "tsenor_mask_ex_static",
     "tsenor_mask_ex_profile", "tsenor_last_hip_error",
     "tsenor_status_string", "tsenor_version",
+    # layer.py
+    "tsenor_quantize", "tsenor_norm", "tsenor_norm_backward_workspace_bytes", "tsenor_norm_backward",
+    "tsenor_product_workspace_bytes", "tsenor_product", "tsenor_clip_workspace_bytes", "tsenor_clip",
 )
 
 
@@ -117,6 +121,9 @@ def load() -> ctypes.CDLL:
         lib.tsenor_status_string.restype = ctypes.c_char_p
         lib.tsenor_version.restype = ctypes.c_int
         lib.tsenor_last_hip_error.restype = ctypes.c_int
+        from . import layer  # (which imports from here: not at the top)
+
+        layer.declare(lib)
         _lib = lib
     return _lib
 

@@ -1,6 +1,6 @@
 """Build step of the HIP library for gfx950, output in-tree next to the binding.
 
-The host code and the kernels of every block size are translation units of their own, compiled side by side
+The host code, the kernels of every block size and each layer operator are translation units of their own, compiled side by side
 (one hipcc process each) and linked into libtsenor.so.
 """
 from __future__ import annotations
@@ -13,7 +13,8 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 CSRC = PKG / "csrc"
-SOURCES = [CSRC / "tsenor.hip"] + [CSRC / f"launch_m{m}.hip" for m in (64, 32, 16, 8, 4)]
+SOURCES = ([CSRC / "tsenor.hip"] + [CSRC / f"launch_m{m}.hip" for m in (64, 32, 16, 8, 4)]
+           + [CSRC / f"layer_{name}.hip" for name in ("quantize", "norm", "product", "clip")])
 OUTPUT = PKG / "libtsenor.so"
 OBJ_DIR = PKG / "_build"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

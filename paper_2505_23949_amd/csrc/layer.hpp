@@ -1,0 +1,148 @@
+// What the layer operators (tsenor_layer.h) share: loads and stores of rows, the 8-bit format with its scales, checks.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lanes.hpp"
+#include "tsenor.h"
+#include "tsenor_layer.h"
+
+namespace tsenor_dev {
+
+// TSENOR_OK or TSENOR_ERR_HIP for the launches since the last call (tsenor.hip)
+int status_of_launches();
+
+constexpr int kBlock = TSENOR_SCALE_BLOCK;
+constexpr uint32_t kInfinityBits = 0x7F800000u;
+
+// ---- host: checks ----------------------------------------------------------------------------------------------------
+inline bool aligned_to(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+inline size_t size_of(int dtype) { return dtype == TSENOR_BF16 ? 2 : 4; }
+inline bool known(int dtype) { return dtype == TSENOR_F32 || dtype == TSENOR_BF16; }
+inline int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
+// (tiles: a grid of one workgroup of 256 threads each counts fewer than 2^32 threads)
+inline bool shape_ok(int64_t rows, int64_t cols) {
+  return rows >= 0 && rows <= INT32_MAX && cols >= 0 && cols <= (int64_t)1 << 24 && blocks_of(rows) * blocks_of(cols) < (int64_t)1 << 24;
+}
+constexpr int64_t kMaxLd = (int64_t)1 << 40;  // (products with a row number stay far below 2^63 + bytes per element)
+inline bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld <= kMaxLd; }
+// rows of 16-byte vectors: the base and every row begin at a multiple of 16 bytes
+inline bool rows_of_vectors(const void* p, int64_t ld, size_t element) { return aligned_to(p, 16) && (size_t)ld * element % 16 == 0; }
+inline int check_scaled(const tsenor_scaled& s) {
+  if (s.rows != 0 && s.cols != 0 && (!s.values || !s.scales)) return TSENOR_ERR_NULL;
+  if (!shape_ok(s.rows, s.cols) || !ld_ok(s.ld, s.cols) || !ld_ok(s.scale_ld, s.rows)) return TSENOR_ERR_SHAPE;
+  if (s.ld < blocks_of(s.cols) * kBlock) return TSENOR_ERR_SHAPE;
+  if (!aligned_to(s.values, 16) || !aligned_to(s.scales, 16) || s.ld % kBlock || s.scale_ld % 16) return TSENOR_ERR_ALIGN;
+  return TSENOR_OK;
+}
+
+// ---- device: rows ----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float widen(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+// two values rounded to bf16 (nearest, ties to even), the first in the low half
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, b}, bf16x2));
+}
+
+// 8 elements of a row from column `c` on, as floats: with 16-byte loads where `vec` says that the row allows it and all of them
+// lie inside, else one by one; 0 past the last column
+template <bool BF16>
+__device__ __forceinline__ void load_row8(const void* row, int c, int cols, bool vec, float (&x)[8]) {
+  if (vec && c + 8 <= cols) {
+    if constexpr (BF16) {
+      const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + c);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[2 * k] = __uint_as_float(w[k] << 16), x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+    } else {
+      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + c);
+      const float4 a = p[0], b = p[1];
+      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = 0.0f;
+      if (c + k < cols) {
+        if constexpr (BF16)
+          x[k] = widen(static_cast<const uint16_t*>(row)[c + k]);
+        else
+          x[k] = static_cast<const float*>(row)[c + k];
+      }
+    }
+  }
+}
+
+// the same way back, rounded once; returns in `x` what was stored
+template <bool BF16>
+__device__ __forceinline__ void store_row8(void* row, int c, int cols, bool vec, const float (&x)[8]) {
+  if constexpr (BF16) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = pack_bf16(x[2 * k], x[2 * k + 1]);
+    if (vec && c + 8 <= cols) {
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < cols) static_cast<uint16_t*>(row)[c + k] = (uint16_t)(w[k / 2] >> (k % 2 * 16));
+    }
+  } else {
+    if (vec && c + 8 <= cols) {
+      float4* p = reinterpret_cast<float4*>(static_cast<float*>(row) + c);
+      p[0] = make_float4(x[0], x[1], x[2], x[3]), p[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < cols) static_cast<float*>(row)[c + k] = x[k];
+    }
+  }
+}
+
+// ---- device: the 8-bit format ------------------------------------------------------------------------------------------
+// |x| as bits that compare like it; 0 for infinities and NaN, which no scale is made for
+__device__ __forceinline__ uint32_t finite_size(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+  return u < kInfinityBits ? u : 0u;
+}
+// Byte of the smallest power of two s with largest <= 448 s: 448 = 1.75 * 2^8, so the exponent of `largest` goes down by 8, and up
+// by one where its fraction is above 1.75, which a carry does.  At least 2^-126: its reciprocal is finite, and so is that of
+// the largest one, 2^120.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t largest) {
+  const int e = (int)((largest + 0x1FFFFFu) >> 23) - 8;
+  return largest == 0u ? 127u : (uint32_t)max(e, 1);
+}
+__device__ __forceinline__ float inverse_of_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// 8 values times a power of two (exact but for results below 2^-126, which are 0 in 8 bits) to the nearest 8-bit ones, ties to even
+__device__ __forceinline__ uint2 to_8bit(const float (&x)[8], float inverse) {
+  uint2 q;
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inverse, x[1] * inverse, 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inverse, x[3] * inverse, lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * inverse, x[5] * inverse, 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * inverse, x[7] * inverse, hi, true);
+  q.x = (uint32_t)lo, q.y = (uint32_t)hi;
+  return q;
+}
+
+// largest over the 16 lanes of a DPP row, in all of them
+__device__ __forceinline__ uint32_t row16_max(uint32_t v) {
+  v = max(v, (uint32_t)lane_xor_i32<1>((int)v));
+  v = max(v, (uint32_t)lane_xor_i32<2>((int)v));
+  v = max(v, (uint32_t)lane_xor_i32<7>((int)v));
+  return max(v, (uint32_t)lane_xor_i32<15>((int)v));
+}
+
+// sum over the wave, in all lanes, the same bits in each
+__device__ __forceinline__ float wave_sum(float v) {
+  v += lane_xor<1>(v);
+  v += lane_xor<2>(v);
+  v += lane_xor<7>(v);
+  v += lane_xor<15>(v);
+  v += lane_xor<16>(v);
+  return v + lane_xor<32>(v);
+}
+
+}  // namespace tsenor_dev

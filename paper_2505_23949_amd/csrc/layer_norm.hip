@@ -1,0 +1,403 @@
+// tsenor_norm: residual addition, root-mean-square norm, 8-bit output with scales; tsenor_norm_backward: its gradients.
+//
+// Both need a sum over the row before the first result, and both keep the row in registers meanwhile, so that it is read once:
+// THREADS threads to a row, VECTORS vectors of 8 to a thread, 128 columns on 16 neighbouring lanes, whose maximum is the scale's.
+// Rows too long for that are read twice.  Bound by memory; a single row by the launch.
+#include <algorithm>
+#include <cmath>
+
+#include "layer.hpp"
+
+namespace {
+
+using namespace tsenor_dev;
+
+struct NormArgs {
+  const void *x, *residual, *gain;
+  void *sum_out, *y_out;
+  int64_t ld, residual_ld;
+  int rows, cols;
+  float eps;
+  tsenor_scaled out;
+  bool gain_bf16;
+  bool x_vec, residual_vec, sum_vec, y_vec, gain_vec;  // rows begin at multiples of 16 bytes
+};
+
+__device__ __forceinline__ const void* at_row(const void* p, int64_t row, int64_t ld, bool bf16) {
+  return static_cast<const char*>(p) + row * ld * (bf16 ? 2 : 4);
+}
+__device__ __forceinline__ void* at_row(void* p, int64_t row, int64_t ld, bool bf16) {
+  return static_cast<char*>(p) + row * ld * (bf16 ? 2 : 4);
+}
+__device__ __forceinline__ void load_gain8(const void* gain, bool bf16, int c, int cols, bool vec, float (&g)[8]) {
+  if (bf16)
+    load_row8<true>(gain, c, cols, vec, g);
+  else
+    load_row8<false>(gain, c, cols, vec, g);
+}
+
+// h of 8 columns of a row: x, or its sum with the residual as it is stored
+template <bool BF16>
+__device__ __forceinline__ void load_sum8(const NormArgs& a, int64_t row, int c, float (&h)[8]) {
+  load_row8<BF16>(at_row(a.x, row, a.ld, BF16), c, a.cols, a.x_vec, h);
+  if (!a.residual) return;
+  float r[8];
+  load_row8<BF16>(at_row(a.residual, row, a.residual_ld, BF16), c, a.cols, a.residual_vec, r);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) h[k] = h[k] + r[k];
+  if constexpr (BF16) {
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+      const uint32_t w = pack_bf16(h[k], h[k + 1]);
+      h[k] = __uint_as_float(w << 16), h[k + 1] = __uint_as_float(w & 0xFFFF0000u);
+    }
+  }
+}
+
+// y of 8 columns from h, written as asked for
+template <bool BF16>
+__device__ __forceinline__ void write_norm8(const NormArgs& a, int64_t row, int c, float inverse, float (&h)[8]) {
+  float g[8];
+  load_gain8(a.gain, a.gain_bf16, c, a.cols, a.gain_vec, g);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) h[k] = c + k < a.cols ? h[k] * inverse * g[k] : 0.0f;
+  if (a.y_out) store_row8<BF16>(at_row(a.y_out, row, a.cols, BF16), c, a.cols, a.y_vec, h);
+  if (a.out.values) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = max(m, finite_size(h[k]));
+    const uint32_t byte = scale_byte(row16_max(m));
+    if (c / kBlock * kBlock < a.cols) {
+      *reinterpret_cast<uint2*>(a.out.values + row * a.out.ld + c) = to_8bit(h, inverse_of_scale(byte));
+      if (c % kBlock == 0) a.out.scales[(int64_t)(c / kBlock) * a.out.scale_ld + row] = (uint8_t)byte;
+    }
+  }
+}
+
+// sum over the THREADS threads of a row; `part` holds one float per wave, and may be used again after the next barrier
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float v, float* part) {
+  v = wave_sum(v);
+  if constexpr (THREADS > kWave) {
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < THREADS / kWave; ++k) v += part[k];
+  }
+  return v;
+}
+
+constexpr int group_of(int threads) { return threads < 256 ? 256 : threads; }
+
+template <bool BF16, int THREADS, int VECTORS>
+__global__ __launch_bounds__(group_of(THREADS)) void norm_kernel(NormArgs a) {
+  __shared__ float part[16];
+  const int t = (int)threadIdx.x % THREADS;
+  const int64_t row = (int64_t)blockIdx.x * (group_of(THREADS) / THREADS) + threadIdx.x / THREADS;
+  if (THREADS == kWave && row >= a.rows) return;  // (whole waves, and no barrier follows)
+  float h[VECTORS][8];
+#pragma unroll
+  for (int v = 0; v < VECTORS; ++v) load_sum8<BF16>(a, row, (v * THREADS + t) * 8, h[v]);
+  float sum = 0.0f;
+#pragma unroll
+  for (int v = 0; v < VECTORS; ++v) {
+    if (a.sum_out) store_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), (v * THREADS + t) * 8, a.cols, a.sum_vec, h[v]);
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s = fmaf(h[v][k], h[v][k], s);
+    sum += s;
+  }
+  const float inverse = 1.0f / sqrtf(row_sum<THREADS>(sum, part) / (float)a.cols + a.eps);
+#pragma unroll
+  for (int v = 0; v < VECTORS; ++v) write_norm8<BF16>(a, row, (v * THREADS + t) * 8, inverse, h[v]);
+}
+
+// rows of any length, read twice: h comes back from sum_out where that is written (it may be x or the residual)
+constexpr int kLongThreads = 1024;
+template <bool BF16>
+__global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormArgs a) {
+  __shared__ float part[16];
+  const int64_t row = blockIdx.x;
+  const int step = kLongThreads * 8, end = (a.cols + kBlock - 1) / kBlock * kBlock;
+  float sum = 0.0f;
+  for (int c = (int)threadIdx.x * 8; c < a.cols; c += step) {
+    float h[8], s = 0.0f;
+    load_sum8<BF16>(a, row, c, h);
+    if (a.sum_out) store_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), c, a.cols, a.sum_vec, h);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s = fmaf(h[k], h[k], s);
+    sum += s;
+  }
+  const float inverse = 1.0f / sqrtf(row_sum<kLongThreads>(sum, part) / (float)a.cols + a.eps);
+  // (whole groups of 16 lanes stay together: a step of 8192 columns is a multiple of 128, and so is `end`)
+  for (int c = (int)threadIdx.x * 8; c < end; c += step) {
+    float h[8];
+    if (a.sum_out)
+      load_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), c, a.cols, a.sum_vec, h);
+    else
+      load_sum8<BF16>(a, row, c, h);
+    write_norm8<BF16>(a, row, c, inverse, h);
+  }
+}
+
+// ---- backward ----------------------------------------------------------------------------------------------------------
+struct BackwardArgs {
+  const void *h, *gain, *dy, *dsum;
+  void* dh;
+  float* dgain;  // of each workgroup, `cols` apart; the result itself where there is one workgroup
+  int64_t ld, dy_ld, dsum_ld;
+  int rows, cols;
+  float eps;
+  bool gain_bf16;
+  bool h_vec, dy_vec, dsum_vec, dh_vec, dgain_vec, gain_vec;
+};
+
+// sums of two values over the THREADS threads of a row, in all of them
+template <int THREADS>
+__device__ __forceinline__ void row_sum2(float& u, float& v, float (*part)[2]) {
+  u = wave_sum(u), v = wave_sum(v);
+  if constexpr (THREADS > kWave) {
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave][0] = u, part[threadIdx.x / kWave][1] = v;
+    __syncthreads();
+    u = 0.0f, v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < THREADS / kWave; ++k) u += part[k][0], v += part[k][1];
+  }
+}
+
+// dh of 8 columns, and their part of dgain added to `dg`
+template <bool BF16>
+__device__ __forceinline__ void write_backward8(const BackwardArgs& a, int64_t row, int c, float inverse, float toward, const float (&h)[8],
+                                                const float (&dy)[8], const float (&g)[8], float (&dg)[8]) {
+  float d[8] = {};
+  if (a.dsum) load_row8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols, a.dsum_vec, d);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    d[k] += fmaf(inverse, g[k] * dy[k], -(h[k] * toward));  // (d last: it may cancel what the norm gives)
+    dg[k] = fmaf(dy[k], h[k] * inverse, dg[k]);
+  }
+  store_row8<BF16>(at_row(a.dh, row, a.cols, BF16), c, a.cols, a.dh_vec, d);
+}
+
+// A workgroup takes every gridDim.x-th row and keeps its sum of dgain in registers.
+template <bool BF16, int THREADS, int VECTORS>
+__global__ __launch_bounds__(THREADS) void norm_backward_kernel(BackwardArgs a) {
+  __shared__ float part[2][16][2];
+  const int t = (int)threadIdx.x;
+  float g[VECTORS][8], dg[VECTORS][8] = {};
+#pragma unroll
+  for (int v = 0; v < VECTORS; ++v) load_gain8(a.gain, a.gain_bf16, (v * THREADS + t) * 8, a.cols, a.gain_vec, g[v]);
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {  // (two places for the sums: one barrier a row)
+    float h[VECTORS][8], dy[VECTORS][8];
+    float squares = 0.0f, along = 0.0f;
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v) {
+      const int c = (v * THREADS + t) * 8;
+      load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, a.h_vec, h[v]);
+      load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, a.dy_vec, dy[v]);
+    }
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) squares = fmaf(h[v][k], h[v][k], squares), along = fmaf(g[v][k] * dy[v][k], h[v][k], along);
+    row_sum2<THREADS>(squares, along, part[turn]);
+    const float inverse = 1.0f / sqrtf(squares / (float)a.cols + a.eps);
+    const float toward = inverse * inverse * inverse * (along / (float)a.cols);
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v) write_backward8<BF16>(a, row, (v * THREADS + t) * 8, inverse, toward, h[v], dy[v], g[v], dg[v]);
+  }
+  float* sums = a.dgain + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+  for (int v = 0; v < VECTORS; ++v) store_row8<false>(sums, (v * THREADS + t) * 8, a.cols, a.dgain_vec, dg[v]);
+}
+
+// Rows too long for registers: their two numbers first,
+template <bool BF16>
+__global__ __launch_bounds__(kLongThreads) void backward_stats_kernel(BackwardArgs a, float2* stats) {
+  __shared__ float part[16][2];
+  const int64_t row = blockIdx.x;
+  float squares = 0.0f, along = 0.0f;
+  for (int c = (int)threadIdx.x * 8; c < a.cols; c += kLongThreads * 8) {
+    float h[8], dy[8], g[8], s = 0.0f, l = 0.0f;
+    load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, a.h_vec, h);
+    load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, a.dy_vec, dy);
+    load_gain8(a.gain, a.gain_bf16, c, a.cols, a.gain_vec, g);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s = fmaf(h[k], h[k], s), l = fmaf(g[k] * dy[k], h[k], l);
+    squares += s, along += l;
+  }
+  row_sum2<kLongThreads>(squares, along, part);
+  const float inverse = 1.0f / sqrtf(squares / (float)a.cols + a.eps);
+  if (threadIdx.x == 0) stats[row] = make_float2(inverse, inverse * inverse * inverse * (along / (float)a.cols));
+}
+// then the gradients, 2048 columns and every gridDim.y-th row to a workgroup.
+constexpr int kSlab = 2048;
+template <bool BF16>
+__global__ __launch_bounds__(256) void backward_apply_kernel(BackwardArgs a, const float2* stats) {
+  const int c = (int)blockIdx.x * kSlab + (int)threadIdx.x * 8;
+  float g[8], dg[8] = {};
+  load_gain8(a.gain, a.gain_bf16, c, a.cols, a.gain_vec, g);
+  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    float h[8], dy[8];
+    load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, a.h_vec, h);
+    load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, a.dy_vec, dy);
+    const float2 s = stats[row];
+    write_backward8<BF16>(a, row, c, s.x, s.y, h, dy, g, dg);
+  }
+  store_row8<false>(a.dgain + (int64_t)blockIdx.y * a.cols, c, a.cols, a.dgain_vec, dg);
+}
+
+// dgain from what the `groups` workgroups left, added in their order: 16 runs of them for 64 columns, then the runs
+__global__ __launch_bounds__(1024) void gather_dgain_kernel(const float* sums, int groups, int cols, float* dgain) {
+  __shared__ float run[16][kWave];
+  const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+  const int64_t c = (int64_t)blockIdx.x * kWave + lane;
+  const int per = (groups + 15) / 16, end = min(groups, (wave + 1) * per);
+  float s = 0.0f;
+  if (c < cols)
+#pragma unroll 8
+    for (int k = wave * per; k < end; ++k) s += sums[(int64_t)k * cols + c];
+  run[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < cols) {
+#pragma unroll
+    for (int k = 1; k < 16; ++k) s += run[k][lane];
+    dgain[c] = s;
+  }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------
+int check(const tsenor_norm_problem* p) {
+  if (!p) return TSENOR_ERR_NULL;
+  if (p->rows != 0 && p->cols != 0 && (!p->x || !p->gain || (!p->sum_out && !p->y_out && !p->out.values))) return TSENOR_ERR_NULL;
+  if (!known(p->dtype) || !known(p->gain_dtype)) return TSENOR_ERR_UNSUPPORTED;
+  if (!shape_ok(p->rows, p->cols) || !ld_ok(p->ld, p->cols) || (p->residual && !ld_ok(p->residual_ld, p->cols))) return TSENOR_ERR_SHAPE;
+  if (!(p->eps >= 0.0) || !std::isfinite((float)p->eps)) return TSENOR_ERR_PARAM;
+  const size_t e = size_of(p->dtype);
+  if (!aligned_to(p->x, e) || !aligned_to(p->residual, e) || !aligned_to(p->sum_out, e) || !aligned_to(p->y_out, e) ||
+      !aligned_to(p->gain, size_of(p->gain_dtype)))
+    return TSENOR_ERR_ALIGN;
+  if (!p->out.values) return TSENOR_OK;
+  if (p->out.rows != p->rows || p->out.cols != p->cols) return TSENOR_ERR_SHAPE;
+  return check_scaled(p->out);
+}
+
+int check(const tsenor_norm_backward_problem* p) {
+  if (!p) return TSENOR_ERR_NULL;
+  if (p->cols != 0 && (!p->gain || !p->dgain_out || (p->rows != 0 && (!p->h || !p->dy || !p->dh_out)))) return TSENOR_ERR_NULL;
+  if (!known(p->dtype) || !known(p->gain_dtype)) return TSENOR_ERR_UNSUPPORTED;
+  if (!shape_ok(p->rows, p->cols) || !ld_ok(p->ld, p->cols) || !ld_ok(p->dy_ld, p->cols) || (p->dsum && !ld_ok(p->dsum_ld, p->cols)))
+    return TSENOR_ERR_SHAPE;
+  if (!(p->eps >= 0.0) || !std::isfinite((float)p->eps)) return TSENOR_ERR_PARAM;
+  const size_t e = size_of(p->dtype);
+  if (!aligned_to(p->h, e) || !aligned_to(p->dy, e) || !aligned_to(p->dsum, e) || !aligned_to(p->dh_out, e) ||
+      !aligned_to(p->gain, size_of(p->gain_dtype)) || !aligned_to(p->dgain_out, 4))
+    return TSENOR_ERR_ALIGN;
+  return TSENOR_OK;
+}
+
+constexpr int kLongRow = 16384;  // columns that the registers of 1024 threads hold, 16 to a thread
+inline size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// workgroups that share the rows of a backward pass: each leaves a sum of dgain
+inline int64_t backward_groups(const tsenor_norm_backward_problem& p) {
+  const int64_t most = p.cols <= kLongRow ? 512 : std::max<int64_t>(1, 1024 / ((p.cols + kSlab - 1) / kSlab));
+  return std::max<int64_t>(1, std::min(p.rows, most));
+}
+struct BackwardLayout {
+  size_t stats, sums, total;
+};
+inline BackwardLayout layout_of(const tsenor_norm_backward_problem& p) {
+  BackwardLayout l = {0, 0, 0};
+  const int64_t groups = backward_groups(p);
+  l.sums = p.cols > kLongRow ? padded((size_t)p.rows * sizeof(float2)) : 0;
+  l.total = l.sums + (groups > 1 ? padded((size_t)(groups * p.cols) * sizeof(float)) : 0);
+  return l;
+}
+
+template <bool BF16>
+void launch_norm(const NormArgs& a, hipStream_t s) {
+  const unsigned rows = (unsigned)a.rows;
+  if (a.cols <= 512)
+    norm_kernel<BF16, 64, 1><<<(rows + 3) / 4, 256, 0, s>>>(a);
+  else if (a.cols <= 1024)
+    norm_kernel<BF16, 64, 2><<<(rows + 3) / 4, 256, 0, s>>>(a);
+  else if (a.cols <= 2048)
+    norm_kernel<BF16, 256, 1><<<rows, 256, 0, s>>>(a);
+  else if (a.cols <= 4096)
+    norm_kernel<BF16, 256, 2><<<rows, 256, 0, s>>>(a);
+  else if (a.cols <= 8192)
+    norm_kernel<BF16, 256, 4><<<rows, 256, 0, s>>>(a);
+  else if (a.cols <= kLongRow)
+    norm_kernel<BF16, 1024, 2><<<rows, 1024, 0, s>>>(a);
+  else
+    norm_long_kernel<BF16><<<rows, kLongThreads, 0, s>>>(a);
+}
+
+template <bool BF16>
+void launch_backward(const BackwardArgs& a, unsigned groups, float2* stats, hipStream_t s) {
+  if (a.cols <= 512) {
+    norm_backward_kernel<BF16, 64, 1><<<groups, 64, 0, s>>>(a);
+  } else if (a.cols <= 2048) {
+    norm_backward_kernel<BF16, 256, 1><<<groups, 256, 0, s>>>(a);
+  } else if (a.cols <= 4096) {
+    norm_backward_kernel<BF16, 256, 2><<<groups, 256, 0, s>>>(a);
+  } else if (a.cols <= 8192) {
+    norm_backward_kernel<BF16, 512, 2><<<groups, 512, 0, s>>>(a);
+  } else if (a.cols <= kLongRow) {
+    norm_backward_kernel<BF16, 1024, 2><<<groups, 1024, 0, s>>>(a);
+  } else {
+    if (a.rows > 0) backward_stats_kernel<BF16><<<(unsigned)a.rows, kLongThreads, 0, s>>>(a, stats);
+    backward_apply_kernel<BF16><<<dim3((unsigned)((a.cols + kSlab - 1) / kSlab), groups), 256, 0, s>>>(a, stats);
+  }
+}
+
+}  // namespace
+
+extern "C" int tsenor_norm(const tsenor_norm_problem* p, tsenor_stream_t stream) {
+  const int rc = check(p);
+  if (rc != TSENOR_OK) return rc;
+  if (p->rows == 0 || p->cols == 0) return TSENOR_OK;
+  NormArgs a = {};
+  a.x = p->x, a.residual = p->residual, a.gain = p->gain, a.sum_out = p->sum_out, a.y_out = p->y_out;
+  a.ld = p->ld, a.residual_ld = p->residual_ld, a.rows = (int)p->rows, a.cols = (int)p->cols, a.eps = (float)p->eps;
+  a.out = p->out;
+  a.gain_bf16 = p->gain_dtype == TSENOR_BF16;
+  const size_t e = size_of(p->dtype);
+  a.x_vec = rows_of_vectors(p->x, p->ld, e), a.residual_vec = rows_of_vectors(p->residual, p->residual_ld, e);
+  a.sum_vec = rows_of_vectors(p->sum_out, p->cols, e), a.y_vec = rows_of_vectors(p->y_out, p->cols, e);
+  a.gain_vec = aligned_to(p->gain, 16);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  p->dtype == TSENOR_BF16 ? launch_norm<true>(a, s) : launch_norm<false>(a, s);
+  return status_of_launches();
+}
+
+extern "C" size_t tsenor_norm_backward_workspace_bytes(const tsenor_norm_backward_problem* p) {
+  return check(p) == TSENOR_OK ? layout_of(*p).total : 0;
+}
+
+extern "C" int tsenor_norm_backward(const tsenor_norm_backward_problem* p, void* workspace, size_t workspace_bytes, tsenor_stream_t stream) {
+  const int rc = check(p);
+  if (rc != TSENOR_OK) return rc;
+  const BackwardLayout l = layout_of(*p);
+  if (l.total && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < l.total)) return TSENOR_ERR_WORKSPACE;
+  if (p->cols == 0) return TSENOR_OK;
+  const int groups = (int)backward_groups(*p);
+  char* ws = static_cast<char*>(workspace);
+  BackwardArgs a = {};
+  a.h = p->h, a.gain = p->gain, a.dy = p->dy, a.dsum = p->dsum, a.dh = p->dh_out;
+  a.dgain = groups > 1 ? reinterpret_cast<float*>(ws + l.sums) : p->dgain_out;
+  a.ld = p->ld, a.dy_ld = p->dy_ld, a.dsum_ld = p->dsum_ld, a.rows = (int)p->rows, a.cols = (int)p->cols, a.eps = (float)p->eps;
+  a.gain_bf16 = p->gain_dtype == TSENOR_BF16;
+  const size_t e = size_of(p->dtype);
+  a.h_vec = rows_of_vectors(p->h, p->ld, e), a.dy_vec = rows_of_vectors(p->dy, p->dy_ld, e);
+  a.dsum_vec = rows_of_vectors(p->dsum, p->dsum_ld, e), a.dh_vec = rows_of_vectors(p->dh_out, p->cols, e);
+  a.dgain_vec = rows_of_vectors(a.dgain, p->cols, 4), a.gain_vec = aligned_to(p->gain, 16);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  float2* stats = reinterpret_cast<float2*>(ws);
+  p->dtype == TSENOR_BF16 ? launch_backward<true>(a, (unsigned)groups, stats, s) : launch_backward<false>(a, (unsigned)groups, stats, s);
+  if (groups > 1) gather_dgain_kernel<<<(unsigned)((p->cols + kWave - 1) / kWave), 1024, 0, s>>>(a.dgain, groups, (int)p->cols, p->dgain_out);
+  return status_of_launches();
+}

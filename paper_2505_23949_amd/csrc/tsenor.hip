@@ -23,6 +23,7 @@
 
 #include "lanes.hpp"
 #include "launch.hpp"
+#include "layer.hpp"
 #include "outputs.hpp"
 #include "problem.hpp"
 #include "tsenor.h"
@@ -201,7 +202,11 @@ inline int hip_status_of_launches() {
   g_last_hip_error = (int)e;
   return TSENOR_ERR_HIP;
 }
+}  // namespace
 
+int tsenor_dev::status_of_launches() { return hip_status_of_launches(); }
+
+namespace {
 struct WsLayout {
   size_t header, partials, potentials, accept, objective, total;
 };
@@ -615,12 +620,13 @@ const char* tsenor_status_string(int status) {
   switch (status) {
     case TSENOR_OK: return "ok";
     case TSENOR_ERR_NULL: return "a required pointer is NULL";
-    case TSENOR_ERR_SHAPE: return "rows/cols must be positive multiples of M, ld >= cols, at most 2^40 weights and fewer than 2^31 blocks of one size per call";
+    case TSENOR_ERR_SHAPE: return "rows/cols must be positive multiples of M, ld >= cols, at most 2^40 weights and fewer than 2^31 blocks of one size per call (layer operators: shapes that agree, counts >= 0, at most 2^31 - 1 rows and 2^24 columns)";
     case TSENOR_ERR_NM: return "N must satisfy 0 <= N <= M";
     case TSENOR_ERR_UNSUPPORTED: return "unsupported M (4, 8, 16, 32, 64), dtype, tau_mode or flag";
-    case TSENOR_ERR_PARAM: return "tau must be finite and > 0 (>= 1/690 in REL_MATRIX_MAX mode), iters and local_search_steps >= 0, at most one TSENOR_FLAG_GREEDY_* and one TSENOR_FLAG_TILES_* flag";
-    case TSENOR_ERR_WORKSPACE: return "workspace is NULL, not 256-byte aligned or smaller than tsenor_workspace_bytes";
+    case TSENOR_ERR_PARAM: return "tau must be finite and > 0 (>= 1/690 in REL_MATRIX_MAX mode), iters and local_search_steps >= 0, at most one TSENOR_FLAG_GREEDY_* and one TSENOR_FLAG_TILES_* flag (layer operators: eps finite and >= 0, max_norm >= 0)";
+    case TSENOR_ERR_WORKSPACE: return "workspace is NULL, not 256-byte aligned or smaller than the call's *_workspace_bytes";
     case TSENOR_ERR_HIP: return "a HIP call failed";
+    case TSENOR_ERR_ALIGN: return "a pointer or leading dimension is not aligned as tsenor_layer.h states";
     case TSENOR_ERR_TOO_LARGE: return "tsenor_mask_ex_static: the problem needs more scratch than TSENOR_STATIC_SCRATCH_BYTES; use tsenor_mask_ex with a workspace";
   }
   return "unknown status";
