@@ -16,7 +16,7 @@
  * workspace, and every call can be captured in a HIP graph.  Besides:
  *   - rows, columns and counts may be zero (no tokens this time): outputs that have elements are still written, and pointers to
  *     matrices without elements may be NULL.
- *   - Matrices have at most 2^31 - 1 rows, 2^24 columns and 2^24 - 1 tiles of 128 x 128, else TSENOR_ERR_SHAPE.  Rows need not be aligned (matrices whose
+ *   - Matrices have at most 2^31 - 256 rows, 2^24 columns and 2^24 - 1 tiles of 128 x 128, else TSENOR_ERR_SHAPE.  Rows need not be aligned (matrices whose
  *     rows all begin at multiples of 16 bytes are read and written faster); scaled matrices have to be, see below.
  *   - A misaligned pointer or leading dimension is TSENOR_ERR_ALIGN (pointers: to their elements, workspaces to 256 bytes).
  *   - Results do not depend on what else runs, nor on earlier calls: sums have a fixed order, and there are no atomics.
@@ -105,7 +105,7 @@ int tsenor_norm_backward(const tsenor_norm_backward_problem* p, void* workspace,
  * bits below it, so a result of normal operands is 1.6e-5 off before its rounding to bf16 (2e-3), and operands
  * in 8 bits are 3e-2 off each. */
 typedef struct tsenor_product_problem {
-  tsenor_scaled a, b;     /* a.cols == b.cols */
+  tsenor_scaled a, b;     /* a.cols == b.cols; ld at most 2^22, ceil(cols / 128) * scale_ld below 2^31, b.rows at most 2^24 */
   void* out;              /* a.rows x b.rows bf16, leading dimension out_ld */
   int64_t out_ld;
   const uint8_t* mask;    /* optional, a.rows x b.rows bytes, leading dimension b.rows: 0 drops the result */

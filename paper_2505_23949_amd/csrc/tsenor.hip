@@ -620,7 +620,7 @@ const char* tsenor_status_string(int status) {
   switch (status) {
     case TSENOR_OK: return "ok";
     case TSENOR_ERR_NULL: return "a required pointer is NULL";
-    case TSENOR_ERR_SHAPE: return "rows/cols must be positive multiples of M, ld >= cols, at most 2^40 weights and fewer than 2^31 blocks of one size per call (layer operators: shapes that agree, counts >= 0, at most 2^31 - 1 rows and 2^24 columns)";
+    case TSENOR_ERR_SHAPE: return "rows/cols must be positive multiples of M, ld >= cols, at most 2^40 weights and fewer than 2^31 blocks of one size per call (layer operators: shapes that agree, counts >= 0, at most 2^31 - 256 rows and 2^24 columns)";
     case TSENOR_ERR_NM: return "N must satisfy 0 <= N <= M";
     case TSENOR_ERR_UNSUPPORTED: return "unsupported M (4, 8, 16, 32, 64), dtype, tau_mode or flag";
     case TSENOR_ERR_PARAM: return "tau must be finite and > 0 (>= 1/690 in REL_MATRIX_MAX mode), iters and local_search_steps >= 0, at most one TSENOR_FLAG_GREEDY_* and one TSENOR_FLAG_TILES_* flag (layer operators: eps finite and >= 0, max_norm >= 0)";

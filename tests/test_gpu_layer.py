@@ -270,7 +270,7 @@ def product(layer, a, b, out, mask=None):
 
 PRODUCTS = [(1, 1, 1), (1, 130, 128), (2, 16, 129), (16, 100, 256), (17, 513, 384), (1, 4096, 512), (33, 260, 1000), (48, 300, 2200), (64, 64, 64),
             (65, 70, 140), (100, 129, 640), (127, 255, 1024), (129, 128, 100), (200, 520, 3500), (256, 256, 256), (257, 300, 500), (300, 1000, 130),
-            (520, 260, 2049), (1000, 770, 384)]
+            (520, 260, 2049), (1000, 770, 384), (128, 200, 9000), (12, 5000, 260), (2000, 4001, 300), (4000, 4010, 260)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
@@ -308,6 +308,13 @@ def test_product(layer, m, n, k, square):
 def test_product_without_columns_is_zero(layer):
     a, b = layer.empty_scaled(5, 0, "cuda"), layer.empty_scaled(9, 0, "cuda")
     assert not product(layer, a, b, torch.full((5, 9), 3.0, dtype=torch.bfloat16, device="cuda")).any()
+
+
+def test_large_product_without_columns_is_zero(layer):
+    a, b = layer.empty_scaled(300, 0, "cuda"), layer.empty_scaled(500, 0, "cuda")
+    wide = torch.full((300, 503), 3.0, dtype=torch.bfloat16, device="cuda")
+    product(layer, a, b, wide[:, 2:502])
+    assert not wide[:, 2:502].any() and (wide[:, :2] == 3).all() and (wide[:, 502:] == 3).all()
 
 
 def test_product_keeps_infinite_and_undefined_rows_apart(layer):
