@@ -25,7 +25,7 @@ struct ClipTensor {
 struct ClipTable {
   int count;
   uint32_t first[kMaxTensors + 1];  // chunk that each tensor begins with
-  uint8_t bf16[kMaxTensors], vec[kMaxTensors];  // type; whether it can be moved in vectors of 16 bytes
+  uint8_t bf16[kMaxTensors];
   ClipTensor t[kMaxTensors];
 };
 static_assert(sizeof(ClipTable) <= 4000, "the table travels as a kernel argument");
@@ -46,13 +46,13 @@ __device__ __forceinline__ int tensor_of(const ClipTable& table, uint32_t chunk)
 __device__ __forceinline__ double square_of(float v) { return (double)v * (double)v; }
 
 template <bool BF16>
-__device__ __forceinline__ double squares_of_chunk(const void* in, int64_t begin, int64_t end, bool vec) {
+__device__ __forceinline__ double squares_of_chunk(const void* in, int64_t begin, int64_t end) {
   double s = 0.0;
-  if (vec && end - begin == kChunk) {
+  if (end - begin == kChunk) {
 #pragma unroll
     for (int k = 0; k < kChunk / (kThreads * 8); ++k) {
       float x[8];
-      load_row8<BF16>(static_cast<const char*>(in) + begin * (BF16 ? 2 : 4), (k * kThreads + (int)threadIdx.x) * 8, kChunk, true, x);
+      load_row8<BF16>(static_cast<const char*>(in) + begin * (BF16 ? 2 : 4), (k * kThreads + (int)threadIdx.x) * 8, kChunk, x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s = fma((double)x[j], (double)x[j], s);
     }
@@ -78,23 +78,23 @@ __global__ __launch_bounds__(kThreads) void squares_kernel(ClipTable table, doub
     const int k = tensor_of(table, chunk);
     const ClipTensor t = table.t[k];
     const int64_t begin = (int64_t)(chunk - table.first[k]) * kChunk, end = min(t.count, begin + kChunk);
-    s += table.bf16[k] ? squares_of_chunk<true>(t.in, begin, end, table.vec[k]) : squares_of_chunk<false>(t.in, begin, end, table.vec[k]);
+    s += table.bf16[k] ? squares_of_chunk<true>(t.in, begin, end) : squares_of_chunk<false>(t.in, begin, end);
   }
   s = group_sum(s);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
 template <bool BF16>
-__device__ __forceinline__ void scale_chunk(const ClipTensor& t, int64_t begin, int64_t end, bool vec, float factor) {
-  if (vec && end - begin == kChunk) {
+__device__ __forceinline__ void scale_chunk(const ClipTensor& t, int64_t begin, int64_t end, float factor) {
+  if (end - begin == kChunk) {
 #pragma unroll
     for (int k = 0; k < kChunk / (kThreads * 8); ++k) {
       const int c = (k * kThreads + (int)threadIdx.x) * 8;
       float x[8];
-      load_row8<BF16>(static_cast<const char*>(t.in) + begin * (BF16 ? 2 : 4), c, kChunk, true, x);
+      load_row8<BF16>(static_cast<const char*>(t.in) + begin * (BF16 ? 2 : 4), c, kChunk, x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] *= factor;
-      store_row8<BF16>(static_cast<char*>(t.out) + begin * (BF16 ? 2 : 4), c, kChunk, true, x);
+      store_row8<BF16>(static_cast<char*>(t.out) + begin * (BF16 ? 2 : 4), c, kChunk, x);
     }
   } else {
     for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(ClipTable table, const 
     const ClipTensor t = table.t[k];
     if (factor == 1.0f && t.in == t.out) continue;
     const int64_t begin = (int64_t)(chunk - table.first[k]) * kChunk, end = min(t.count, begin + kChunk);
-    table.bf16[k] ? scale_chunk<true>(t, begin, end, table.vec[k], factor) : scale_chunk<false>(t, begin, end, table.vec[k], factor);
+    table.bf16[k] ? scale_chunk<true>(t, begin, end, factor) : scale_chunk<false>(t, begin, end, factor);
   }
 }
 
@@ -156,7 +156,6 @@ int fill_table(const tsenor_clip_problem& p, int k, ClipTable& table) {
     const int i = table.count++;
     table.first[i] = (uint32_t)chunks;
     table.bf16[i] = g.dtype == TSENOR_BF16;
-    table.vec[i] = aligned_to(g.in, 16) && aligned_to(g.out, 16);
     table.t[i] = {g.in, g.out, g.count};
     chunks += chunks_of(g.count);
   }

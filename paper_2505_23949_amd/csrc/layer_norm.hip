@@ -20,7 +20,6 @@ struct NormArgs {
   float eps;
   tsenor_scaled out;
   bool gain_bf16;
-  bool x_vec, residual_vec, sum_vec, y_vec, gain_vec;  // rows begin at multiples of 16 bytes
 };
 
 __device__ __forceinline__ const void* at_row(const void* p, int64_t row, int64_t ld, bool bf16) {
@@ -29,20 +28,28 @@ __device__ __forceinline__ const void* at_row(const void* p, int64_t row, int64_
 __device__ __forceinline__ void* at_row(void* p, int64_t row, int64_t ld, bool bf16) {
   return static_cast<char*>(p) + row * ld * (bf16 ? 2 : 4);
 }
-__device__ __forceinline__ void load_gain8(const void* gain, bool bf16, int c, int cols, bool vec, float (&g)[8]) {
+__device__ __forceinline__ void load_gain8(const void* gain, bool bf16, int c, int cols, float (&g)[8]) {
   if (bf16)
-    load_row8<true>(gain, c, cols, vec, g);
+    load_row8<true>(gain, c, cols, g);
   else
-    load_row8<false>(gain, c, cols, vec, g);
+    load_row8<false>(gain, c, cols, g);
+}
+
+// x^-1/2 to within 0.51 units: the quotient's own error, and that of the root, taken off once more.  (A value whose error moves it over
+// the middle between two 8-bit ones is 2^-4 off there, so each half unit less halves how many are.)
+__device__ __forceinline__ float inverse_root(float x) {
+  const float r = 1.0f / sqrtf(x);
+  const float t = x * r, low = fmaf(x, r, -t), d = fmaf(-t, r, 1.0f) - low * r;
+  return x > 0.0f && x < __builtin_inff() ? fmaf(0.5f * r, d, r) : r;
 }
 
 // h of 8 columns of a row: x, or its sum with the residual as it is stored
 template <bool BF16>
 __device__ __forceinline__ void load_sum8(const NormArgs& a, int64_t row, int c, float (&h)[8]) {
-  load_row8<BF16>(at_row(a.x, row, a.ld, BF16), c, a.cols, a.x_vec, h);
+  load_row8<BF16>(at_row(a.x, row, a.ld, BF16), c, a.cols, h);
   if (!a.residual) return;
   float r[8];
-  load_row8<BF16>(at_row(a.residual, row, a.residual_ld, BF16), c, a.cols, a.residual_vec, r);
+  load_row8<BF16>(at_row(a.residual, row, a.residual_ld, BF16), c, a.cols, r);
 #pragma unroll
   for (int k = 0; k < 8; ++k) h[k] = h[k] + r[k];
   if constexpr (BF16) {
@@ -58,10 +65,10 @@ __device__ __forceinline__ void load_sum8(const NormArgs& a, int64_t row, int c,
 template <bool BF16>
 __device__ __forceinline__ void write_norm8(const NormArgs& a, int64_t row, int c, float inverse, float (&h)[8]) {
   float g[8];
-  load_gain8(a.gain, a.gain_bf16, c, a.cols, a.gain_vec, g);
+  load_gain8(a.gain, a.gain_bf16, c, a.cols, g);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) h[k] = c + k < a.cols ? h[k] * inverse * g[k] : 0.0f;
-  if (a.y_out) store_row8<BF16>(at_row(a.y_out, row, a.cols, BF16), c, a.cols, a.y_vec, h);
+  for (int k = 0; k < 8; ++k) h[k] = c + k < a.cols ? h[k] * g[k] * inverse : 0.0f;  // (h g is exact in bf16)
+  if (a.y_out) store_row8<BF16>(at_row(a.y_out, row, a.cols, BF16), c, a.cols, h);
   if (a.out.values) {
     uint32_t m = 0;
 #pragma unroll
@@ -102,13 +109,13 @@ __global__ __launch_bounds__(group_of(THREADS)) void norm_kernel(NormArgs a) {
   float sum = 0.0f;
 #pragma unroll
   for (int v = 0; v < VECTORS; ++v) {
-    if (a.sum_out) store_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), (v * THREADS + t) * 8, a.cols, a.sum_vec, h[v]);
+    if (a.sum_out) store_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), (v * THREADS + t) * 8, a.cols, h[v]);
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) s = fmaf(h[v][k], h[v][k], s);
     sum += s;
   }
-  const float inverse = 1.0f / sqrtf(row_sum<THREADS>(sum, part) / (float)a.cols + a.eps);
+  const float inverse = inverse_root(row_sum<THREADS>(sum, part) / (float)a.cols + a.eps);
 #pragma unroll
   for (int v = 0; v < VECTORS; ++v) write_norm8<BF16>(a, row, (v * THREADS + t) * 8, inverse, h[v]);
 }
@@ -124,17 +131,17 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormArgs a) {
   for (int c = (int)threadIdx.x * 8; c < a.cols; c += step) {
     float h[8], s = 0.0f;
     load_sum8<BF16>(a, row, c, h);
-    if (a.sum_out) store_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), c, a.cols, a.sum_vec, h);
+    if (a.sum_out) store_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), c, a.cols, h);
 #pragma unroll
     for (int k = 0; k < 8; ++k) s = fmaf(h[k], h[k], s);
     sum += s;
   }
-  const float inverse = 1.0f / sqrtf(row_sum<kLongThreads>(sum, part) / (float)a.cols + a.eps);
+  const float inverse = inverse_root(row_sum<kLongThreads>(sum, part) / (float)a.cols + a.eps);
   // (whole groups of 16 lanes stay together: a step of 8192 columns is a multiple of 128, and so is `end`)
   for (int c = (int)threadIdx.x * 8; c < end; c += step) {
     float h[8];
     if (a.sum_out)
-      load_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), c, a.cols, a.sum_vec, h);
+      load_row8<BF16>(at_row(a.sum_out, row, a.cols, BF16), c, a.cols, h);
     else
       load_sum8<BF16>(a, row, c, h);
     write_norm8<BF16>(a, row, c, inverse, h);
@@ -150,7 +157,6 @@ struct BackwardArgs {
   int rows, cols;
   float eps;
   bool gain_bf16;
-  bool h_vec, dy_vec, dsum_vec, dh_vec, dgain_vec, gain_vec;
 };
 
 // sums of two values over the THREADS threads of a row, in all of them
@@ -171,13 +177,13 @@ template <bool BF16>
 __device__ __forceinline__ void write_backward8(const BackwardArgs& a, int64_t row, int c, float inverse, float toward, const float (&h)[8],
                                                 const float (&dy)[8], const float (&g)[8], float (&dg)[8]) {
   float d[8] = {};
-  if (a.dsum) load_row8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols, a.dsum_vec, d);
+  if (a.dsum) load_row8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols, d);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     d[k] += fmaf(inverse, g[k] * dy[k], -(h[k] * toward));  // (d last: it may cancel what the norm gives)
     dg[k] = fmaf(dy[k], h[k] * inverse, dg[k]);
   }
-  store_row8<BF16>(at_row(a.dh, row, a.cols, BF16), c, a.cols, a.dh_vec, d);
+  store_row8<BF16>(at_row(a.dh, row, a.cols, BF16), c, a.cols, d);
 }
 
 // A workgroup takes every gridDim.x-th row and keeps its sum of dgain in registers.
@@ -187,7 +193,7 @@ __global__ __launch_bounds__(THREADS) void norm_backward_kernel(BackwardArgs a) 
   const int t = (int)threadIdx.x;
   float g[VECTORS][8], dg[VECTORS][8] = {};
 #pragma unroll
-  for (int v = 0; v < VECTORS; ++v) load_gain8(a.gain, a.gain_bf16, (v * THREADS + t) * 8, a.cols, a.gain_vec, g[v]);
+  for (int v = 0; v < VECTORS; ++v) load_gain8(a.gain, a.gain_bf16, (v * THREADS + t) * 8, a.cols, g[v]);
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {  // (two places for the sums: one barrier a row)
     float h[VECTORS][8], dy[VECTORS][8];
@@ -195,22 +201,22 @@ __global__ __launch_bounds__(THREADS) void norm_backward_kernel(BackwardArgs a) 
 #pragma unroll
     for (int v = 0; v < VECTORS; ++v) {
       const int c = (v * THREADS + t) * 8;
-      load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, a.h_vec, h[v]);
-      load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, a.dy_vec, dy[v]);
+      load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, h[v]);
+      load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, dy[v]);
     }
 #pragma unroll
     for (int v = 0; v < VECTORS; ++v)
 #pragma unroll
       for (int k = 0; k < 8; ++k) squares = fmaf(h[v][k], h[v][k], squares), along = fmaf(g[v][k] * dy[v][k], h[v][k], along);
     row_sum2<THREADS>(squares, along, part[turn]);
-    const float inverse = 1.0f / sqrtf(squares / (float)a.cols + a.eps);
+    const float inverse = inverse_root(squares / (float)a.cols + a.eps);
     const float toward = inverse * inverse * inverse * (along / (float)a.cols);
 #pragma unroll
     for (int v = 0; v < VECTORS; ++v) write_backward8<BF16>(a, row, (v * THREADS + t) * 8, inverse, toward, h[v], dy[v], g[v], dg[v]);
   }
   float* sums = a.dgain + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
-  for (int v = 0; v < VECTORS; ++v) store_row8<false>(sums, (v * THREADS + t) * 8, a.cols, a.dgain_vec, dg[v]);
+  for (int v = 0; v < VECTORS; ++v) store_row8<false>(sums, (v * THREADS + t) * 8, a.cols, dg[v]);
 }
 
 // Rows too long for registers: their two numbers first,
@@ -221,15 +227,15 @@ __global__ __launch_bounds__(kLongThreads) void backward_stats_kernel(BackwardAr
   float squares = 0.0f, along = 0.0f;
   for (int c = (int)threadIdx.x * 8; c < a.cols; c += kLongThreads * 8) {
     float h[8], dy[8], g[8], s = 0.0f, l = 0.0f;
-    load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, a.h_vec, h);
-    load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, a.dy_vec, dy);
-    load_gain8(a.gain, a.gain_bf16, c, a.cols, a.gain_vec, g);
+    load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, h);
+    load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, dy);
+    load_gain8(a.gain, a.gain_bf16, c, a.cols, g);
 #pragma unroll
     for (int k = 0; k < 8; ++k) s = fmaf(h[k], h[k], s), l = fmaf(g[k] * dy[k], h[k], l);
     squares += s, along += l;
   }
   row_sum2<kLongThreads>(squares, along, part);
-  const float inverse = 1.0f / sqrtf(squares / (float)a.cols + a.eps);
+  const float inverse = inverse_root(squares / (float)a.cols + a.eps);
   if (threadIdx.x == 0) stats[row] = make_float2(inverse, inverse * inverse * inverse * (along / (float)a.cols));
 }
 // then the gradients, 2048 columns and every gridDim.y-th row to a workgroup.
@@ -238,15 +244,15 @@ template <bool BF16>
 __global__ __launch_bounds__(256) void backward_apply_kernel(BackwardArgs a, const float2* stats) {
   const int c = (int)blockIdx.x * kSlab + (int)threadIdx.x * 8;
   float g[8], dg[8] = {};
-  load_gain8(a.gain, a.gain_bf16, c, a.cols, a.gain_vec, g);
+  load_gain8(a.gain, a.gain_bf16, c, a.cols, g);
   for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
     float h[8], dy[8];
-    load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, a.h_vec, h);
-    load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, a.dy_vec, dy);
+    load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, h);
+    load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, dy);
     const float2 s = stats[row];
     write_backward8<BF16>(a, row, c, s.x, s.y, h, dy, g, dg);
   }
-  store_row8<false>(a.dgain + (int64_t)blockIdx.y * a.cols, c, a.cols, a.dgain_vec, dg);
+  store_row8<false>(a.dgain + (int64_t)blockIdx.y * a.cols, c, a.cols, dg);
 }
 
 // dgain from what the `groups` workgroups left, added in their order: 16 runs of them for 64 columns, then the runs
@@ -365,10 +371,6 @@ extern "C" int tsenor_norm(const tsenor_norm_problem* p, tsenor_stream_t stream)
   a.ld = p->ld, a.residual_ld = p->residual_ld, a.rows = (int)p->rows, a.cols = (int)p->cols, a.eps = (float)p->eps;
   a.out = p->out;
   a.gain_bf16 = p->gain_dtype == TSENOR_BF16;
-  const size_t e = size_of(p->dtype);
-  a.x_vec = rows_of_vectors(p->x, p->ld, e), a.residual_vec = rows_of_vectors(p->residual, p->residual_ld, e);
-  a.sum_vec = rows_of_vectors(p->sum_out, p->cols, e), a.y_vec = rows_of_vectors(p->y_out, p->cols, e);
-  a.gain_vec = aligned_to(p->gain, 16);
   hipStream_t s = static_cast<hipStream_t>(stream);
   p->dtype == TSENOR_BF16 ? launch_norm<true>(a, s) : launch_norm<false>(a, s);
   return status_of_launches();
@@ -391,10 +393,6 @@ extern "C" int tsenor_norm_backward(const tsenor_norm_backward_problem* p, void*
   a.dgain = groups > 1 ? reinterpret_cast<float*>(ws + l.sums) : p->dgain_out;
   a.ld = p->ld, a.dy_ld = p->dy_ld, a.dsum_ld = p->dsum_ld, a.rows = (int)p->rows, a.cols = (int)p->cols, a.eps = (float)p->eps;
   a.gain_bf16 = p->gain_dtype == TSENOR_BF16;
-  const size_t e = size_of(p->dtype);
-  a.h_vec = rows_of_vectors(p->h, p->ld, e), a.dy_vec = rows_of_vectors(p->dy, p->dy_ld, e);
-  a.dsum_vec = rows_of_vectors(p->dsum, p->dsum_ld, e), a.dh_vec = rows_of_vectors(p->dh_out, p->cols, e);
-  a.dgain_vec = rows_of_vectors(a.dgain, p->cols, 4), a.gain_vec = aligned_to(p->gain, 16);
   hipStream_t s = static_cast<hipStream_t>(stream);
   float2* stats = reinterpret_cast<float2*>(ws);
   p->dtype == TSENOR_BF16 ? launch_backward<true>(a, (unsigned)groups, stats, s) : launch_backward<false>(a, (unsigned)groups, stats, s);
