@@ -1,9 +1,13 @@
 // tsenor_clip: the norm of all gradients of a model, and the gradients scaled down to a largest norm.
 //
-// A tensor is cut into chunks; the chunks of up to kMaxTensors tensors share a launch, whose table is a kernel argument.  Each
-// workgroup of the first pass leaves one sum of squares in double, and each of the second adds all of those in the same order
-// before it scales: no atomics, nothing to clear, and no launch between the two.  Bound by memory.  The second pass goes
-// through the chunks from the last to the first: what the first one read last is still in the cache of the memory side.
+// A tensor is cut into chunks of 4096 elements; the chunks of up to kMaxTensors tensors share a launch, whose table is a kernel
+// argument, and workgroups take every gridDim.x-th of them, so that what is read at a time lies together.  In the first pass each
+// leaves one sum of squares in double, and each of the second adds all of those in the same order before it scales: no
+// atomics, nothing to clear, and no launch between the two.  Bound by memory.  The second pass goes through the chunks from the
+// last to the first, what the first one read last being still in the cache of the memory side (2 % for a layer of 436 MB), and
+// its accesses are marked as the last ones to what they touch, so that results do not drive out what is still to be read: the
+// gradients of a layer of 4096 (218 M in bf16) 215 us, 243 without the mark.  (8 or 4 vectors in flight and half as many
+// workgroups: 241, 227.)
 #include <algorithm>
 
 #include "layer.hpp"
@@ -13,9 +17,10 @@ namespace {
 using namespace tsenor_dev;
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 8192;       // elements
-constexpr int kMaxTensors = 100;   // of a launch
-constexpr int kMaxGroups = 1024;   // workgroups of a launch, sums that it leaves
+constexpr int kVectors = 2;                      // of 8 elements, that a thread has in flight
+constexpr int kChunk = kThreads * 8 * kVectors;  // elements
+constexpr int kMaxTensors = 100;                 // of a launch
+constexpr int kMaxGroups = 2048;                 // workgroups of a launch, sums that it leaves
 
 struct ClipTensor {
   const void* in;
@@ -43,27 +48,63 @@ __device__ __forceinline__ int tensor_of(const ClipTable& table, uint32_t chunk)
   return lo;
 }
 
-__device__ __forceinline__ double square_of(float v) { return (double)v * (double)v; }
+// element of a chunk that the thread's vector v begins with
+__device__ __forceinline__ int element_of(int v) { return (v * kThreads + (int)threadIdx.x) * 8; }
 
+// squares of `size` elements
 template <bool BF16>
-__device__ __forceinline__ double squares_of_chunk(const void* in, int64_t begin, int64_t end) {
-  double s = 0.0;
-  if (end - begin == kChunk) {
+__device__ __forceinline__ double add_squares(const char* in, int size, double s) {
+  float x[kVectors][8];
 #pragma unroll
-    for (int k = 0; k < kChunk / (kThreads * 8); ++k) {
-      float x[8];
-      load_row8<BF16>(static_cast<const char*>(in) + begin * (BF16 ? 2 : 4), (k * kThreads + (int)threadIdx.x) * 8, kChunk, x);
+  for (int v = 0; v < kVectors; ++v) load_row8<BF16>(in, element_of(v), size, x[v]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s = fma((double)x[j], (double)x[j], s);
-    }
-  } else {
-    for (int64_t i = begin + threadIdx.x; i < end; i += kThreads)
-      s += square_of(BF16 ? widen(static_cast<const uint16_t*>(in)[i]) : static_cast<const float*>(in)[i]);
-  }
+  for (int v = 0; v < kVectors; ++v)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fma((double)x[v][j], (double)x[v][j], s);
   return s;
 }
 
-// sum over the workgroup, in thread 0
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4), aligned(2)));
+template <bool BF16>
+__device__ __forceinline__ void scale(const char* in, char* out, int size, float factor) {
+  float x[kVectors][8];
+#pragma unroll
+  for (int v = 0; v < kVectors; ++v) {
+    const int at = element_of(v);
+    if (size != kChunk) {
+      load_row8<BF16>(in, at, size, x[v]);
+    } else if constexpr (BF16) {
+      const uintx4 w = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(in + at * 2));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[v][2 * k] = __uint_as_float(w[k] << 16), x[v][2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+    } else {
+      const uintx4 a = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(in + at * 4));
+      const uintx4 b = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(in + at * 4 + 16));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[v][k] = __uint_as_float(a[k]), x[v][4 + k] = __uint_as_float(b[k]);
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < kVectors; ++v) {
+    const int at = element_of(v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[v][j] *= factor;
+    if (size != kChunk) {
+      store_row8<BF16>(out, at, size, x[v]);
+    } else if constexpr (BF16) {
+      const uintx4 w = {pack_bf16(x[v][0], x[v][1]), pack_bf16(x[v][2], x[v][3]), pack_bf16(x[v][4], x[v][5]), pack_bf16(x[v][6], x[v][7])};
+      __builtin_nontemporal_store(w, reinterpret_cast<uintx4*>(out + at * 2));
+    } else {
+      uintx4 a, b;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] = __float_as_uint(x[v][k]), b[k] = __float_as_uint(x[v][4 + k]);
+      __builtin_nontemporal_store(a, reinterpret_cast<uintx4*>(out + at * 4));
+      __builtin_nontemporal_store(b, reinterpret_cast<uintx4*>(out + at * 4 + 16));
+    }
+  }
+}
+
+// sum over the workgroup, in all threads
 __device__ __forceinline__ double group_sum(double s) {
   __shared__ double part[kThreads / kWave];
   s += lane_xor<1>(s), s += lane_xor<2>(s), s += lane_xor<7>(s), s += lane_xor<15>(s), s += lane_xor<16>(s), s += lane_xor<32>(s);
@@ -74,36 +115,21 @@ __device__ __forceinline__ double group_sum(double s) {
 
 __global__ __launch_bounds__(kThreads) void squares_kernel(ClipTable table, double* sums) {
   double s = 0.0;
-  for (uint32_t chunk = blockIdx.x; chunk < table.first[table.count]; chunk += gridDim.x) {
-    const int k = tensor_of(table, chunk);
-    const ClipTensor t = table.t[k];
-    const int64_t begin = (int64_t)(chunk - table.first[k]) * kChunk, end = min(t.count, begin + kChunk);
-    s += table.bf16[k] ? squares_of_chunk<true>(t.in, begin, end) : squares_of_chunk<false>(t.in, begin, end);
+  const uint32_t chunks = table.first[table.count];
+  int k = tensor_of(table, blockIdx.x);
+  for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+    while (table.first[k + 1] <= chunk) ++k;
+    const int64_t at = (int64_t)(chunk - table.first[k]) * kChunk;
+    const int size = (int)min(table.t[k].count - at, (int64_t)kChunk);
+    const char* in = static_cast<const char*>(table.t[k].in);
+    // (a whole chunk's size is a constant: its loads have no conditions between them)
+    if (size == kChunk)
+      s = table.bf16[k] ? add_squares<true>(in + at * 2, kChunk, s) : add_squares<false>(in + at * 4, kChunk, s);
+    else
+      s = table.bf16[k] ? add_squares<true>(in + at * 2, size, s) : add_squares<false>(in + at * 4, size, s);
   }
   s = group_sum(s);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
-}
-
-template <bool BF16>
-__device__ __forceinline__ void scale_chunk(const ClipTensor& t, int64_t begin, int64_t end, float factor) {
-  if (end - begin == kChunk) {
-#pragma unroll
-    for (int k = 0; k < kChunk / (kThreads * 8); ++k) {
-      const int c = (k * kThreads + (int)threadIdx.x) * 8;
-      float x[8];
-      load_row8<BF16>(static_cast<const char*>(t.in) + begin * (BF16 ? 2 : 4), c, kChunk, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= factor;
-      store_row8<BF16>(static_cast<char*>(t.out) + begin * (BF16 ? 2 : 4), c, kChunk, x);
-    }
-  } else {
-    for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
-      if constexpr (BF16)
-        static_cast<uint16_t*>(t.out)[i] = (uint16_t)pack_bf16(widen(static_cast<const uint16_t*>(t.in)[i]) * factor, 0.0f);
-      else
-        static_cast<float*>(t.out)[i] = static_cast<const float*>(t.in)[i] * factor;
-    }
-  }
 }
 
 __global__ __launch_bounds__(kThreads) void scale_kernel(ClipTable table, const double* sums, int count, double max_norm, float* norm_out) {
@@ -113,13 +139,21 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(ClipTable table, const 
   const float factor = norm > max_norm && norm <= 1.7976931348623157e308 ? (float)(max_norm / norm) : 1.0f;
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) norm_out[0] = (float)norm, norm_out[1] = factor;
   const uint32_t chunks = table.first[table.count];
+  if (blockIdx.x >= chunks) return;
+  int k = tensor_of(table, chunks - 1 - blockIdx.x);
   for (uint32_t back = blockIdx.x; back < chunks; back += gridDim.x) {
     const uint32_t chunk = chunks - 1 - back;
-    const int k = tensor_of(table, chunk);
+    while (table.first[k] > chunk) --k;
     const ClipTensor t = table.t[k];
     if (factor == 1.0f && t.in == t.out) continue;
-    const int64_t begin = (int64_t)(chunk - table.first[k]) * kChunk, end = min(t.count, begin + kChunk);
-    table.bf16[k] ? scale_chunk<true>(t, begin, end, factor) : scale_chunk<false>(t, begin, end, factor);
+    const int64_t at = (int64_t)(chunk - table.first[k]) * kChunk;
+    const int size = (int)min(t.count - at, (int64_t)kChunk);
+    const char* in = static_cast<const char*>(t.in);
+    char* out = static_cast<char*>(t.out);
+    if (size == kChunk)
+      table.bf16[k] ? scale<true>(in + at * 2, out + at * 2, kChunk, factor) : scale<false>(in + at * 4, out + at * 4, kChunk, factor);
+    else
+      table.bf16[k] ? scale<true>(in + at * 2, out + at * 2, size, factor) : scale<false>(in + at * 4, out + at * 4, size, factor);
   }
 }
 
