@@ -37,8 +37,6 @@ inline int check_scaled(const tsenor_scaled& s) {
 }
 
 // ---- device: rows ----------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float widen(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
-
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 // two values rounded to bf16 (nearest, ties to even), the first in the low half
@@ -49,28 +47,40 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // 8 elements of a row from column `c` on, as floats; 0 past the last column.  Rows may begin anywhere: a load of 16 bytes needs no
 // alignment here, and an 8192 x 8192 bf16 matrix with rows of 8195 elements is quantised in 67 us, with loads of 2 bytes in 125.
 template <bool BF16>
-__device__ __forceinline__ void load_row8(const void* row, int c, int cols, float (&x)[8]) {
+struct Raw8 {
+  uint32_t w[BF16 ? 4 : 8];
+};
+// as it stands in memory, so that nothing waits for it yet
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> load_raw8(const void* row, int c, int cols) {
+  Raw8<BF16> raw = {};
   if (c + 8 <= cols) {
-    if constexpr (BF16) {
-      uint32_t w[4];
-      __builtin_memcpy(w, static_cast<const uint16_t*>(row) + c, 16);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[2 * k] = __uint_as_float(w[k] << 16), x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-    } else {
-      __builtin_memcpy(x, static_cast<const float*>(row) + c, 32);
-    }
+    __builtin_memcpy(raw.w, static_cast<const char*>(row) + c * (BF16 ? 2 : 4), sizeof(raw.w));
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      x[k] = 0.0f;
+    for (int k = 0; k < 8; ++k)
       if (c + k < cols) {
         if constexpr (BF16)
-          x[k] = widen(static_cast<const uint16_t*>(row)[c + k]);
+          raw.w[k / 2] |= (uint32_t)static_cast<const uint16_t*>(row)[c + k] << (k % 2 * 16);
         else
-          x[k] = static_cast<const float*>(row)[c + k];
+          raw.w[k] = static_cast<const uint32_t*>(row)[c + k];
       }
-    }
   }
+  return raw;
+}
+template <bool BF16>
+__device__ __forceinline__ void widen8(const Raw8<BF16>& raw, float (&x)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if constexpr (BF16)
+      x[k] = __uint_as_float(k % 2 ? raw.w[k / 2] & 0xFFFF0000u : raw.w[k / 2] << 16);
+    else
+      x[k] = __uint_as_float(raw.w[k]);
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ void load_row8(const void* row, int c, int cols, float (&x)[8]) {
+  widen8<BF16>(load_raw8<BF16>(row, c, cols), x);
 }
 
 // the same way back, rounded once

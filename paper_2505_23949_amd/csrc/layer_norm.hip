@@ -2,7 +2,8 @@
 //
 // Both need a sum over the row before the first result, and both keep the row in registers meanwhile, so that it is read once:
 // THREADS threads to a row, VECTORS vectors of 8 to a thread, 128 columns on 16 neighbouring lanes, whose maximum is the scale's.
-// Rows too long for that are read twice.  Bound by memory; a single row by the launch.
+// Rows too long for that are read twice.  Bound by memory: bf16 4096 x 8192 with residual, sum, norm and its 8-bit form 66 us
+// (4.6 TB/s), single precision 4096 x 4096 45 us (4.9); a single row by the launch (2.7 us).
 #include <algorithm>
 #include <cmath>
 
@@ -95,7 +96,7 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
-constexpr int group_of(int threads) { return threads < 256 ? 256 : threads; }
+constexpr int group_of(int threads) { return threads == kWave ? 256 : threads; }  // (four rows of a wave each)
 
 template <bool BF16, int THREADS, int VECTORS>
 __global__ __launch_bounds__(group_of(THREADS)) void norm_kernel(NormArgs a) {
@@ -172,12 +173,10 @@ __device__ __forceinline__ void row_sum2(float& u, float& v, float (*part)[2]) {
   }
 }
 
-// dh of 8 columns, and their part of dgain added to `dg`
+// dh of 8 columns, and their part of dgain added to `dg`; d: the gradient that reaches h past the norm
 template <bool BF16>
 __device__ __forceinline__ void write_backward8(const BackwardArgs& a, int64_t row, int c, float inverse, float toward, const float (&h)[8],
-                                                const float (&dy)[8], const float (&g)[8], float (&dg)[8]) {
-  float d[8] = {};
-  if (a.dsum) load_row8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols, d);
+                                                const float (&dy)[8], const float (&g)[8], float (&d)[8], float (&dg)[8]) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     d[k] += fmaf(inverse, g[k] * dy[k], -(h[k] * toward));  // (d last: it may cancel what the norm gives)
@@ -186,33 +185,71 @@ __device__ __forceinline__ void write_backward8(const BackwardArgs& a, int64_t r
   store_row8<BF16>(at_row(a.dh, row, a.cols, BF16), c, a.cols, d);
 }
 
-// A workgroup takes every gridDim.x-th row and keeps its sum of dgain in registers.
-template <bool BF16, int THREADS, int VECTORS>
+// what a thread reads of a row
+template <bool BF16, int VECTORS>
+struct BackwardRow {
+  Raw8<BF16> h[VECTORS], dy[VECTORS], dsum[VECTORS];
+};
+template <bool BF16, int THREADS, bool AHEAD, int VECTORS>
+__device__ __forceinline__ void load_backward(const BackwardArgs& a, int64_t row, BackwardRow<BF16, VECTORS>& x) {
+  if (row >= a.rows) return;
+#pragma unroll
+  for (int v = 0; v < VECTORS; ++v) {
+    const int c = (v * THREADS + (int)threadIdx.x) * 8;
+    x.h[v] = load_raw8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols);
+    x.dy[v] = load_raw8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols);
+    if (AHEAD && a.dsum) x.dsum[v] = load_raw8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols);
+  }
+}
+
+// A workgroup takes every gridDim.x-th row, asks for the next before it works on one (AHEAD: where the registers hold both), and keeps
+// its sum of dgain in registers.  Bound by memory: 2047 x 4096 in single precision 31 us (4.35 TB/s), bf16 4096 x 4096 with dsum 33
+// (45 where each row was asked for when its turn came).
+template <bool BF16, int THREADS, int VECTORS, bool AHEAD>
 __global__ __launch_bounds__(THREADS) void norm_backward_kernel(BackwardArgs a) {
   __shared__ float part[2][16][2];
   const int t = (int)threadIdx.x;
   float g[VECTORS][8], dg[VECTORS][8] = {};
 #pragma unroll
   for (int v = 0; v < VECTORS; ++v) load_gain8(a.gain, a.gain_bf16, (v * THREADS + t) * 8, a.cols, g[v]);
-  int turn = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {  // (two places for the sums: one barrier a row)
+  const auto work = [&](int64_t row, const BackwardRow<BF16, VECTORS>& x, float (&sums)[16][2]) {
     float h[VECTORS][8], dy[VECTORS][8];
     float squares = 0.0f, along = 0.0f;
 #pragma unroll
     for (int v = 0; v < VECTORS; ++v) {
-      const int c = (v * THREADS + t) * 8;
-      load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, h[v]);
-      load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, dy[v]);
-    }
-#pragma unroll
-    for (int v = 0; v < VECTORS; ++v)
+      widen8<BF16>(x.h[v], h[v]), widen8<BF16>(x.dy[v], dy[v]);
 #pragma unroll
       for (int k = 0; k < 8; ++k) squares = fmaf(h[v][k], h[v][k], squares), along = fmaf(g[v][k] * dy[v][k], h[v][k], along);
-    row_sum2<THREADS>(squares, along, part[turn]);
+    }
+    row_sum2<THREADS>(squares, along, sums);
     const float inverse = inverse_root(squares / (float)a.cols + a.eps);
     const float toward = inverse * inverse * inverse * (along / (float)a.cols);
 #pragma unroll
-    for (int v = 0; v < VECTORS; ++v) write_backward8<BF16>(a, row, (v * THREADS + t) * 8, inverse, toward, h[v], dy[v], g[v], dg[v]);
+    for (int v = 0; v < VECTORS; ++v) {
+      const int c = (v * THREADS + t) * 8;
+      float d[8] = {};
+      if (a.dsum) widen8<BF16>(AHEAD ? x.dsum[v] : load_raw8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols), d);
+      write_backward8<BF16>(a, row, c, inverse, toward, h[v], dy[v], g[v], d, dg[v]);
+    }
+  };
+  // (two places for the sums: one barrier a row)
+  if constexpr (AHEAD) {
+    BackwardRow<BF16, VECTORS> even = {}, odd = {};
+    load_backward<BF16, THREADS, true>(a, blockIdx.x, even);
+    for (int64_t row = blockIdx.x; row < a.rows; row += 2 * (int64_t)gridDim.x) {
+      load_backward<BF16, THREADS, true>(a, row + gridDim.x, odd);
+      work(row, even, part[0]);
+      if (row + gridDim.x >= a.rows) break;
+      load_backward<BF16, THREADS, true>(a, row + 2 * (int64_t)gridDim.x, even);
+      work(row + gridDim.x, odd, part[1]);
+    }
+  } else {
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+      BackwardRow<BF16, VECTORS> x;
+      load_backward<BF16, THREADS, false>(a, row, x);
+      work(row, x, part[turn]);
+    }
   }
   float* sums = a.dgain + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
@@ -250,26 +287,30 @@ __global__ __launch_bounds__(256) void backward_apply_kernel(BackwardArgs a, con
     load_row8<BF16>(at_row(a.h, row, a.ld, BF16), c, a.cols, h);
     load_row8<BF16>(at_row(a.dy, row, a.dy_ld, BF16), c, a.cols, dy);
     const float2 s = stats[row];
-    write_backward8<BF16>(a, row, c, s.x, s.y, h, dy, g, dg);
+    float d[8] = {};
+    if (a.dsum) load_row8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols, d);
+    write_backward8<BF16>(a, row, c, s.x, s.y, h, dy, g, d, dg);
   }
   store_row8<false>(a.dgain + (int64_t)blockIdx.y * a.cols, c, a.cols, dg);
 }
 
-// dgain from what the `groups` workgroups left, added in their order: 16 runs of them for 64 columns, then the runs
+// dgain from what the `groups` workgroups left, in a fixed order: for 16 columns, 64 runs of workgroups, then the runs
 __global__ __launch_bounds__(1024) void gather_dgain_kernel(const float* sums, int groups, int cols, float* dgain) {
-  __shared__ float run[16][kWave];
-  const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
-  const int64_t c = (int64_t)blockIdx.x * kWave + lane;
-  const int per = (groups + 15) / 16, end = min(groups, (wave + 1) * per);
+  __shared__ float part[16][16];
+  const int lane = (int)threadIdx.x % 16, run = (int)threadIdx.x / 16, wave = (int)threadIdx.x / kWave;
+  const int64_t c = (int64_t)blockIdx.x * 16 + lane;
+  const int per = (groups + 63) / 64, end = min(groups, (run + 1) * per);
   float s = 0.0f;
   if (c < cols)
 #pragma unroll 8
-    for (int k = wave * per; k < end; ++k) s += sums[(int64_t)k * cols + c];
-  run[wave][lane] = s;
+    for (int k = run * per; k < end; ++k) s += sums[(int64_t)k * cols + c];
+  s += lane_xor<16>(s);
+  s += lane_xor<32>(s);
+  if (threadIdx.x % kWave < 16) part[wave][lane] = s;
   __syncthreads();
-  if (wave == 0 && c < cols) {
+  if (run == 0 && c < cols) {
 #pragma unroll
-    for (int k = 1; k < 16; ++k) s += run[k][lane];
+    for (int k = 1; k < 16; ++k) s += part[k][lane];
     dgain[c] = s;
   }
 }
@@ -307,9 +348,12 @@ int check(const tsenor_norm_backward_problem* p) {
 constexpr int kLongRow = 16384;  // columns that the registers of 1024 threads hold, 16 to a thread
 inline size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// workgroups that share the rows of a backward pass: each leaves a sum of dgain
+// Workgroups that share the rows of a backward pass: each leaves a sum of dgain, which costs a write and a read of its columns; fewer than
+// one to a CU leave the memory idle.  (bf16 4096 x 8192 256 of them 56.9 us, 512 64.0; 2000 x 14336 55.8, 63.7; 8000 x 512 with 2048
+// 14.4, with 512 18.2.)
 inline int64_t backward_groups(const tsenor_norm_backward_problem& p) {
-  const int64_t most = p.cols <= kLongRow ? 512 : std::max<int64_t>(1, 1024 / ((p.cols + kSlab - 1) / kSlab));
+  const int64_t most = p.cols <= kLongRow ? std::clamp<int64_t>(((int64_t)1 << 20) / std::max<int64_t>(p.cols, 1), 256, 2048)
+                                          : std::max<int64_t>(1, 1024 / ((p.cols + kSlab - 1) / kSlab));
   return std::max<int64_t>(1, std::min(p.rows, most));
 }
 struct BackwardLayout {
@@ -323,19 +367,21 @@ inline BackwardLayout layout_of(const tsenor_norm_backward_problem& p) {
   return l;
 }
 
+// One vector to a thread as long as a workgroup can have that many: 16 x 8192 3.5 us where 256 threads with four take 5.4, 2048 x 8192
+// 22.0 (22.6), 4096 x 4096 21.2 (512 with one) and 21.8 (256 with two).
 template <bool BF16>
 void launch_norm(const NormArgs& a, hipStream_t s) {
   const unsigned rows = (unsigned)a.rows;
   if (a.cols <= 512)
     norm_kernel<BF16, 64, 1><<<(rows + 3) / 4, 256, 0, s>>>(a);
   else if (a.cols <= 1024)
-    norm_kernel<BF16, 64, 2><<<(rows + 3) / 4, 256, 0, s>>>(a);
+    norm_kernel<BF16, 128, 1><<<rows, 128, 0, s>>>(a);
   else if (a.cols <= 2048)
     norm_kernel<BF16, 256, 1><<<rows, 256, 0, s>>>(a);
   else if (a.cols <= 4096)
-    norm_kernel<BF16, 256, 2><<<rows, 256, 0, s>>>(a);
+    norm_kernel<BF16, 512, 1><<<rows, 512, 0, s>>>(a);
   else if (a.cols <= 8192)
-    norm_kernel<BF16, 256, 4><<<rows, 256, 0, s>>>(a);
+    norm_kernel<BF16, 1024, 1><<<rows, 1024, 0, s>>>(a);
   else if (a.cols <= kLongRow)
     norm_kernel<BF16, 1024, 2><<<rows, 1024, 0, s>>>(a);
   else
@@ -345,15 +391,15 @@ void launch_norm(const NormArgs& a, hipStream_t s) {
 template <bool BF16>
 void launch_backward(const BackwardArgs& a, unsigned groups, float2* stats, hipStream_t s) {
   if (a.cols <= 512) {
-    norm_backward_kernel<BF16, 64, 1><<<groups, 64, 0, s>>>(a);
+    norm_backward_kernel<BF16, 64, 1, true><<<groups, 64, 0, s>>>(a);
   } else if (a.cols <= 2048) {
-    norm_backward_kernel<BF16, 256, 1><<<groups, 256, 0, s>>>(a);
+    norm_backward_kernel<BF16, 256, 1, true><<<groups, 256, 0, s>>>(a);
   } else if (a.cols <= 4096) {
-    norm_backward_kernel<BF16, 256, 2><<<groups, 256, 0, s>>>(a);
+    norm_backward_kernel<BF16, 512, 1, true><<<groups, 512, 0, s>>>(a);
   } else if (a.cols <= 8192) {
-    norm_backward_kernel<BF16, 512, 2><<<groups, 512, 0, s>>>(a);
+    norm_backward_kernel<BF16, 1024, 1, true><<<groups, 1024, 0, s>>>(a);
   } else if (a.cols <= kLongRow) {
-    norm_backward_kernel<BF16, 1024, 2><<<groups, 1024, 0, s>>>(a);
+    norm_backward_kernel<BF16, 1024, 2, false><<<groups, 1024, 0, s>>>(a);
   } else {
     if (a.rows > 0) backward_stats_kernel<BF16><<<(unsigned)a.rows, kLongThreads, 0, s>>>(a, stats);
     backward_apply_kernel<BF16><<<dim3((unsigned)((a.cols + kSlab - 1) / kSlab), groups), 256, 0, s>>>(a, stats);
@@ -396,6 +442,6 @@ extern "C" int tsenor_norm_backward(const tsenor_norm_backward_problem* p, void*
   hipStream_t s = static_cast<hipStream_t>(stream);
   float2* stats = reinterpret_cast<float2*>(ws);
   p->dtype == TSENOR_BF16 ? launch_backward<true>(a, (unsigned)groups, stats, s) : launch_backward<false>(a, (unsigned)groups, stats, s);
-  if (groups > 1) gather_dgain_kernel<<<(unsigned)((p->cols + kWave - 1) / kWave), 1024, 0, s>>>(a.dgain, groups, (int)p->cols, p->dgain_out);
+  if (groups > 1) gather_dgain_kernel<<<(unsigned)((p->cols + 15) / 16), 1024, 0, s>>>(a.dgain, groups, (int)p->cols, p->dgain_out);
   return status_of_launches();
 }
