@@ -19,21 +19,32 @@ using namespace tsenor_dev;
 constexpr int kThreads = 256;
 constexpr int kVectors = 2;                      // of 8 elements, that a thread has in flight
 constexpr int kChunk = kThreads * 8 * kVectors;  // elements
-constexpr int kMaxTensors = 100;                 // of a launch
+constexpr int kMaxTensors = 180;                 // of a launch
 constexpr int kMaxGroups = 2048;                 // workgroups of a launch, sums that it leaves
 
-struct ClipTensor {
-  const void* in;
-  void* out;
-  int64_t count;
-};
 struct ClipTable {
   int count;
   uint32_t first[kMaxTensors + 1];  // chunk that each tensor begins with
-  uint8_t bf16[kMaxTensors];
-  ClipTensor t[kMaxTensors];
+  uint16_t last[kMaxTensors];       // elements of its last chunk, and in the highest bit whether it is bf16
+  const void* in[kMaxTensors];
+  void* out[kMaxTensors];
 };
-static_assert(sizeof(ClipTable) <= 4000, "the table travels as a kernel argument");
+static_assert(sizeof(ClipTable) <= 4032, "the table travels as a kernel argument");
+static_assert(kChunk < 1 << 15);
+
+// A chunk of a tensor: where it begins and how many elements it has
+struct Chunk {
+  const char* in;
+  char* out;
+  int size;
+  bool bf16;
+};
+__device__ __forceinline__ Chunk chunk_of(const ClipTable& table, int k, uint32_t chunk) {
+  const bool bf16 = table.last[k] >> 15;
+  const int64_t at = (int64_t)(chunk - table.first[k]) * kChunk * (bf16 ? 2 : 4);
+  return {static_cast<const char*>(table.in[k]) + at, static_cast<char*>(table.out[k]) + at,
+          chunk + 1 < table.first[k + 1] ? kChunk : table.last[k] & 0x7FFF, bf16};
+}
 
 // tensor that a chunk belongs to (those without elements have none)
 __device__ __forceinline__ int tensor_of(const ClipTable& table, uint32_t chunk) {
@@ -119,14 +130,12 @@ __global__ __launch_bounds__(kThreads) void squares_kernel(ClipTable table, doub
   int k = tensor_of(table, blockIdx.x);
   for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
     while (table.first[k + 1] <= chunk) ++k;
-    const int64_t at = (int64_t)(chunk - table.first[k]) * kChunk;
-    const int size = (int)min(table.t[k].count - at, (int64_t)kChunk);
-    const char* in = static_cast<const char*>(table.t[k].in);
+    const Chunk c = chunk_of(table, k, chunk);
     // (a whole chunk's size is a constant: its loads have no conditions between them)
-    if (size == kChunk)
-      s = table.bf16[k] ? add_squares<true>(in + at * 2, kChunk, s) : add_squares<false>(in + at * 4, kChunk, s);
+    if (c.size == kChunk)
+      s = c.bf16 ? add_squares<true>(c.in, kChunk, s) : add_squares<false>(c.in, kChunk, s);
     else
-      s = table.bf16[k] ? add_squares<true>(in + at * 2, size, s) : add_squares<false>(in + at * 4, size, s);
+      s = c.bf16 ? add_squares<true>(c.in, c.size, s) : add_squares<false>(c.in, c.size, s);
   }
   s = group_sum(s);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
@@ -144,16 +153,12 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(ClipTable table, const 
   for (uint32_t back = blockIdx.x; back < chunks; back += gridDim.x) {
     const uint32_t chunk = chunks - 1 - back;
     while (table.first[k] > chunk) --k;
-    const ClipTensor t = table.t[k];
-    if (factor == 1.0f && t.in == t.out) continue;
-    const int64_t at = (int64_t)(chunk - table.first[k]) * kChunk;
-    const int size = (int)min(t.count - at, (int64_t)kChunk);
-    const char* in = static_cast<const char*>(t.in);
-    char* out = static_cast<char*>(t.out);
-    if (size == kChunk)
-      table.bf16[k] ? scale<true>(in + at * 2, out + at * 2, kChunk, factor) : scale<false>(in + at * 4, out + at * 4, kChunk, factor);
+    const Chunk c = chunk_of(table, k, chunk);
+    if (factor == 1.0f && c.in == c.out) continue;
+    if (c.size == kChunk)
+      c.bf16 ? scale<true>(c.in, c.out, kChunk, factor) : scale<false>(c.in, c.out, kChunk, factor);
     else
-      table.bf16[k] ? scale<true>(in + at * 2, out + at * 2, size, factor) : scale<false>(in + at * 4, out + at * 4, size, factor);
+      c.bf16 ? scale<true>(c.in, c.out, c.size, factor) : scale<false>(c.in, c.out, c.size, factor);
   }
 }
 
@@ -189,8 +194,8 @@ int fill_table(const tsenor_clip_problem& p, int k, ClipTable& table) {
     if (chunks + chunks_of(g.count) > kMaxChunks) break;
     const int i = table.count++;
     table.first[i] = (uint32_t)chunks;
-    table.bf16[i] = g.dtype == TSENOR_BF16;
-    table.t[i] = {g.in, g.out, g.count};
+    table.last[i] = (uint16_t)(((g.count - 1) % kChunk + 1) | (g.dtype == TSENOR_BF16 ? 1 << 15 : 0));
+    table.in[i] = g.in, table.out[i] = g.out;
     chunks += chunks_of(g.count);
   }
   table.first[table.count] = (uint32_t)chunks;

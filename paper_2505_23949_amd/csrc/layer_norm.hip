@@ -354,7 +354,7 @@ inline size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 inline int64_t backward_groups(const tsenor_norm_backward_problem& p) {
   const int64_t most = p.cols <= kLongRow ? std::clamp<int64_t>(((int64_t)1 << 20) / std::max<int64_t>(p.cols, 1), 256, 2048)
                                           : std::max<int64_t>(1, 1024 / ((p.cols + kSlab - 1) / kSlab));
-  return std::max<int64_t>(1, std::min(p.rows, most));
+  return std::max<int64_t>(1, std::min({p.rows, most, std::max<int64_t>(256, p.rows / 4)}));
 }
 struct BackwardLayout {
   size_t stats, sums, total;
@@ -392,6 +392,8 @@ template <bool BF16>
 void launch_backward(const BackwardArgs& a, unsigned groups, float2* stats, hipStream_t s) {
   if (a.cols <= 512) {
     norm_backward_kernel<BF16, 64, 1, true><<<groups, 64, 0, s>>>(a);
+  } else if (a.cols <= 1024) {
+    norm_backward_kernel<BF16, 128, 1, true><<<groups, 128, 0, s>>>(a);
   } else if (a.cols <= 2048) {
     norm_backward_kernel<BF16, 256, 1, true><<<groups, 256, 0, s>>>(a);
   } else if (a.cols <= 4096) {

@@ -238,8 +238,10 @@ __device__ __forceinline__ void write_piece(const ProductArgs& p, int m0, int n0
 }
 
 // SPLIT: p.splits workgroups share the columns of a tile, and each leaves its sums in p.parts, piece by piece.
+template <int TN, int TM, int BUFFERS>
+constexpr int kGroupsPerCu = BUFFERS * TileShape<TN, TM>::kBuffer <= 80 * 1024 ? 2 : 1;
 template <int TN, int TM, int BUFFERS, bool SPLIT>
-__global__ __launch_bounds__(256, 1) void tile_kernel(ProductArgs p) {
+__global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(ProductArgs p) {
   using Shape = TileShape<TN, TM>;
   __shared__ __align__(1024) uint8_t lds[BUFFERS * Shape::kBuffer];
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -428,19 +430,20 @@ int check(const tsenor_product_problem* p) {
 }
 
 // How a product is laid out.
-enum Kind { kNoColumns, kFewRows, kSmallTile, kTile, kWideTile, kLargeTile };
+enum Kind { kNoColumns, kFewRows, kSmallTile, kTile, kTilePairs, kWideTile, kLargeTile };
 struct Plan {
   Kind kind;
   int tiles_m, tiles_n, splits;
   size_t workspace;
 };
-// The kind whose steps take least: measured us of a step (a block of 128 columns) with one workgroup on each of up to 256 CUs, and
-// with all of them at work, where the matrix cores' clock or the L2 decide.  Whole calls, us (rows of a x rows of b x columns):
-//   64 x 128 / 128 x 128 / 256 x 128 / 256 x 256:
-//     48 x 14336 x 4096        14 / 17 / 26 / -          512 x 4096 x 4096       15 / 17 / 24 / 37
-//     1072 x 2928 x 4096       - / 18 / 26 / 40          1024 x 4096 x 8192      49 / 35 / 46 / 68
-//     1999 x 4096 x 14336      174 / 126 / 104 / 145     4096 x 4096 x 4096      101 / 72 / 63 / 54
-//     14336 x 4096 x 8192      733 / 485 / 393 / 357
+// The kind that takes least by measured us of a step (a block of 128 columns) and of what is around the steps of a tile (first loads,
+// results).  Whole calls, us (rows of a x rows of b x columns), by tiles of
+//   64 x 128 / 128 x 128 / the same, two workgroups to a CU / 256 x 128 / 256 x 256:
+//     48 x 14336 x 4096        14 / 17 / - / 26 / -          512 x 4096 x 4096       15 / 17 / - / 24 / 37
+//     1024 x 4096 x 8192       49 / 35 / 43 / 46 / 68        1999 x 4096 x 14336     174 / 126 / 103 / 104 / 145
+//     2327 x 6544 x 1413       40 / 39 / 33 / 47 / 48        2048 x 4096 x 512       13 / 13 / 11 / 11 / 14
+//     4096 x 4096 x 4096       101 / 72 / 62 / 63 / 54       8192 x 8192 x 128       54 / 59 / 39 / 46 / 36
+//     7569 x 8229 x 920        147 / 127 / 96 / 102 / 88     14336 x 4096 x 8192     733 / 485 / 475 / 393 / 357
 // Where the small tiles leave CUs idle, workgroups share the columns of a tile; what they leave costs 0.025 us each to write and add,
 // and a launch: 48 x 4096 x 14336 alone 35, two 22, four 16.5, eight 17.5; 128 x 4096 x 14336 35, 23, 19.
 // Up to 16 rows of a need no tiles: 1, 8 and 16 x 4096 x 14336 12.7, 14.0 and 15.7 (shared tiles 16); 16 x 4096 x 4096 8 (11); but 16 x
@@ -451,14 +454,15 @@ Plan plan_of(const tsenor_product_problem& p) {
   if (blocks == 0) return {kNoColumns, 0, 0, 1, 0};
   Plan best = {};
   double least = 0.0;
-  const auto consider = [&](Kind kind, int rows_m, int rows_n, double step, double full_step) {
+  // at_once: workgroups that run at a time, a whole number of rounds of them unless `fluid`
+  const auto consider = [&](Kind kind, int rows_m, int rows_n, double step, double around, int at_once, bool fluid) {
     const int64_t tiles_m = (m + rows_m - 1) / rows_m, tiles_n = (n + rows_n - 1) / rows_n, tiles = tiles_m * tiles_n;
-    const double rounds = (double)((tiles + kCus - 1) / kCus);
-    double us = rounds * (double)blocks * (tiles <= kCus ? step : full_step);
+    const double rounds = fluid ? std::max(0.5 + 0.5 * (double)tiles / at_once, (double)tiles / at_once) : (double)((tiles + at_once - 1) / at_once);
+    double us = rounds * ((double)blocks * step + around);
     int64_t splits = 1;
     if (kind == kSmallTile)
       for (int64_t k = 2; k <= blocks && k * tiles <= kCus; ++k) {
-        const double shared = (double)((blocks + k - 1) / k) * step + 1.0 + 0.025 * (double)(k * tiles);
+        const double shared = (double)((blocks + k - 1) / k) * step + around + 1.0 + 0.025 * (double)(k * tiles);
         if (shared < us) us = shared, splits = k;
       }
     if (best.tiles_m == 0 || us < least) {
@@ -466,11 +470,14 @@ Plan plan_of(const tsenor_product_problem& p) {
       least = us;
     }
   };
-  consider(kSmallTile, 64, 128, 0.27, 0.37);
+  consider(kSmallTile, 64, 128, (m + 63) / 64 * ((n + 127) / 128) <= kCus ? 0.27 : 0.37, 1.5, kCus, false);
   if (m <= 8 || (m <= 16 && best.splits > 1)) return {kFewRows, 0, 0, 1, 0};
-  consider(kTile, 128, 128, 0.43, 0.55);
-  consider(kWideTile, 256, 128, 0.9, 0.9);
-  consider(kLargeTile, 256, 256, 1.45, 1.45);
+  if ((m + 127) / 128 * ((n + 127) / 128) <= kCus)
+    consider(kTile, 128, 128, 0.43, 2.8, kCus, false);
+  else
+    consider(kTilePairs, 128, 128, 0.91, 3.0, 2 * kCus, true);
+  consider(kWideTile, 256, 128, 0.9, 4.0, kCus, false);
+  consider(kLargeTile, 256, 256, 1.45, 6.0, kCus, false);
   return best;
 }
 
@@ -504,6 +511,7 @@ extern "C" int tsenor_product(const tsenor_product_problem* p, void* workspace, 
       }
       break;
     case kTile: tile_kernel<2, 2, 4, false><<<groups, 256, 0, s>>>(a); break;
+    case kTilePairs: tile_kernel<2, 2, 2, false><<<tiles, 256, 0, s>>>(a); break;
     case kWideTile: tile_kernel<2, 4, 3, false><<<groups, 256, 0, s>>>(a); break;
     case kLargeTile: tile_kernel<4, 4, 2, false><<<groups, 256, 0, s>>>(a); break;
   }
