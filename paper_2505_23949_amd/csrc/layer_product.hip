@@ -113,6 +113,8 @@ __global__ __launch_bounds__(kWaves* kWave) void few_rows_kernel(ProductArgs p) 
 //   Rows past the last are read as the last one and not written.
 //   16-byte pieces: piece c of row r stands at place c ^ (r / 2 % 8), so that the 16 lanes that LDS serves at a time (other rows, the
 //   same piece) take all banks.  The loads write LDS in order, so it is the lanes' addresses in memory that are permuted.
+//   Loads are spread evenly: those of a block over the second half of a step and, with more than two buffers, the first of the next
+//   (all in one half: 5-10 % slower).
 //   Waits: by the middle of a step every wave has the rest of the current block in registers; after a barrier there its buffer is
 //   loaded anew, and the second half of the step reads the beginning of the next block.
 //
@@ -290,12 +292,14 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
 #pragma unroll
       for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.0f;
 
-  // (a block past the last is the last one again, which nothing uses)
+  // With more than two buffers the loads of a block are spread over the second half of a step and the first of the next.
+  // (A block past the last is the last one again, which nothing uses.)
+  constexpr int kEarly = BUFFERS > 2 ? (Shape::kPieces + 1) / 2 : Shape::kPieces;  // loads of a block in the second half
 #pragma unroll
   for (int k = 0; k < BUFFERS; ++k)
 #pragma unroll
-    for (int piece = 0; piece < Shape::kPieces; ++piece) load(k * Shape::kBuffer, piece, min(first + k, last));
-  meet<(BUFFERS - 1) * Shape::kPieces>();
+    for (int piece = 0; piece < (k == BUFFERS - 1 ? kEarly : Shape::kPieces); ++piece) load(k * Shape::kBuffer, piece, min(first + k, last));
+  meet<(BUFFERS - 2) * Shape::kPieces + kEarly>();
   int scale_b = load_scales<TN>(scales_b), scale_a = load_scales<TM>(scales_a), next_b, next_a;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -313,16 +317,17 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   TSENOR_IN_ORDER();
 #define FETCH_B(rows, t, h) b[t][h] = fetch(rows##_b, t, h); TSENOR_IN_ORDER();
 #define FETCH_A(rows, t, h) a[t][h] = fetch(rows##_a, t, h); TSENOR_IN_ORDER();
-#define LOAD(piece) load(buffer, piece, ahead); TSENOR_IN_ORDER();
+#define LOAD(piece) if constexpr (piece < kEarly) { load(buffer, piece, ahead); TSENOR_IN_ORDER(); }
+#define LATE(piece) if constexpr (piece >= kEarly) { load(old_buffer, piece, ahead_of_old); TSENOR_IN_ORDER(); }
 #define FETCH_SCALES()                                                                                        \
   next_b = load_scales<TN>(scales_b + next_buffer), next_a = load_scales<TM>(scales_a + next_buffer);         \
   TSENOR_IN_ORDER();
   constexpr int kPending = (BUFFERS - 2) * Shape::kPieces;  // loads of the blocks after the next
-  int buffer = 0, next_buffer = Shape::kBuffer;
+  int buffer = 0, next_buffer = Shape::kBuffer, old_buffer = (BUFFERS - 1) * Shape::kBuffer;
   for (int block = first; block <= last; ++block) {
     const uint8_t *const this_b = rows_b + buffer, *const this_a = rows_a + buffer;
     const uint8_t *const next_rows_b = rows_b + next_buffer, *const next_rows_a = rows_a + next_buffer;
-    const int ahead = min(block + BUFFERS, last);
+    const int ahead = min(block + BUFFERS, last), ahead_of_old = min(block + BUFFERS - 1, last);
     TSENOR_IN_ORDER();
     if constexpr (TN == 4 && TM == 4) {
       MULTIPLY(0, 0, 0) FETCH_A(this, 1, 0) MULTIPLY(1, 0, 0) FETCH_A(this, 1, 1) MULTIPLY(0, 0, 1) FETCH_A(this, 2, 0)
@@ -340,35 +345,35 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
       MULTIPLY(2, 1, 0) FETCH_A(next_rows, 0, 0) LOAD(12) MULTIPLY(3, 1, 0) FETCH_A(next_rows, 0, 1) LOAD(13)
       MULTIPLY(2, 1, 1) FETCH_SCALES() LOAD(14) MULTIPLY(3, 1, 1) LOAD(15) LOAD(16)
     } else if constexpr (TN == 2 && TM == 4) {
-      MULTIPLY(0, 0, 0) FETCH_B(this, 1, 0) MULTIPLY(0, 1, 0) FETCH_B(this, 1, 1) MULTIPLY(0, 0, 1) FETCH_A(this, 2, 0)
-      MULTIPLY(0, 1, 1) FETCH_A(this, 2, 1) MULTIPLY(1, 0, 0) FETCH_A(this, 3, 0) MULTIPLY(1, 1, 0) FETCH_A(this, 3, 1)
-      MULTIPLY(1, 0, 1) MULTIPLY(1, 1, 1)
+      MULTIPLY(0, 0, 0) FETCH_B(this, 1, 0) MULTIPLY(0, 1, 0) FETCH_B(this, 1, 1) LATE(7) MULTIPLY(0, 0, 1) FETCH_A(this, 2, 0) LATE(8)
+      MULTIPLY(0, 1, 1) FETCH_A(this, 2, 1) LATE(9) MULTIPLY(1, 0, 0) FETCH_A(this, 3, 0) LATE(10) MULTIPLY(1, 1, 0) FETCH_A(this, 3, 1) LATE(11)
+      MULTIPLY(1, 0, 1) LATE(12) MULTIPLY(1, 1, 1)
       meet<kPending>();
-      MULTIPLY(0, 2, 0) LOAD(0) FETCH_A(next_rows, 0, 0) MULTIPLY(0, 3, 0) LOAD(1) LOAD(2)
-      MULTIPLY(0, 2, 1) LOAD(3) FETCH_A(next_rows, 0, 1) MULTIPLY(0, 3, 1) LOAD(4) LOAD(5) FETCH_SCALES()
-      MULTIPLY(1, 2, 0) LOAD(6) FETCH_B(next_rows, 0, 0) MULTIPLY(1, 3, 0) LOAD(7) LOAD(8) FETCH_B(next_rows, 0, 1)
-      MULTIPLY(1, 2, 1) LOAD(9) LOAD(10) FETCH_A(next_rows, 1, 0) MULTIPLY(1, 3, 1) LOAD(11) LOAD(12) FETCH_A(next_rows, 1, 1)
+      MULTIPLY(0, 2, 0) LOAD(0) FETCH_A(next_rows, 0, 0) MULTIPLY(0, 3, 0) LOAD(1) MULTIPLY(0, 2, 1) LOAD(2) FETCH_A(next_rows, 0, 1)
+      MULTIPLY(0, 3, 1) LOAD(3) FETCH_SCALES() MULTIPLY(1, 2, 0) LOAD(4) FETCH_B(next_rows, 0, 0)
+      MULTIPLY(1, 3, 0) LOAD(5) FETCH_B(next_rows, 0, 1) MULTIPLY(1, 2, 1) LOAD(6) FETCH_A(next_rows, 1, 0) MULTIPLY(1, 3, 1) FETCH_A(next_rows, 1, 1)
     } else if constexpr (TN == 2 && TM == 2) {
-      MULTIPLY(0, 0, 0) FETCH_A(this, 1, 0) FETCH_A(this, 1, 1) MULTIPLY(0, 0, 1) FETCH_B(this, 1, 0) FETCH_B(this, 1, 1)
-      MULTIPLY(0, 1, 0) MULTIPLY(0, 1, 1)
+      MULTIPLY(0, 0, 0) FETCH_A(this, 1, 0) FETCH_A(this, 1, 1) LATE(5) MULTIPLY(0, 0, 1) FETCH_B(this, 1, 0) FETCH_B(this, 1, 1) LATE(6)
+      MULTIPLY(0, 1, 0) LATE(7) LATE(8) MULTIPLY(0, 1, 1)
       meet<kPending>();
       MULTIPLY(1, 0, 0) LOAD(0) LOAD(1) FETCH_B(next_rows, 0, 0) MULTIPLY(1, 0, 1) LOAD(2) LOAD(3) FETCH_B(next_rows, 0, 1) FETCH_SCALES()
       MULTIPLY(1, 1, 0) LOAD(4) LOAD(5) FETCH_A(next_rows, 0, 0) MULTIPLY(1, 1, 1) LOAD(6) LOAD(7) LOAD(8) FETCH_A(next_rows, 0, 1)
     } else {
       static_assert(TN == 2 && TM == 1);
-      MULTIPLY(0, 0, 0) FETCH_B(this, 1, 0) FETCH_B(this, 1, 1) MULTIPLY(0, 0, 1)
+      MULTIPLY(0, 0, 0) FETCH_B(this, 1, 0) FETCH_B(this, 1, 1) LATE(4) LATE(5) LATE(6) MULTIPLY(0, 0, 1)
       meet<kPending>();
-      MULTIPLY(1, 0, 0) LOAD(0) LOAD(1) LOAD(2) LOAD(3) FETCH_B(next_rows, 0, 0) FETCH_B(next_rows, 0, 1) FETCH_SCALES()
-      MULTIPLY(1, 0, 1) LOAD(4) LOAD(5) LOAD(6) FETCH_A(next_rows, 0, 0) FETCH_A(next_rows, 0, 1)
+      MULTIPLY(1, 0, 0) LOAD(0) LOAD(1) FETCH_B(next_rows, 0, 0) FETCH_B(next_rows, 0, 1) FETCH_SCALES()
+      MULTIPLY(1, 0, 1) LOAD(2) LOAD(3) FETCH_A(next_rows, 0, 0) FETCH_A(next_rows, 0, 1)
     }
     scale_b = next_b, scale_a = next_a;
-    buffer = next_buffer, next_buffer += Shape::kBuffer;
+    old_buffer = buffer, buffer = next_buffer, next_buffer += Shape::kBuffer;
     if (next_buffer == BUFFERS * Shape::kBuffer) next_buffer = 0;
   }
 #undef MULTIPLY
 #undef FETCH_B
 #undef FETCH_A
 #undef LOAD
+#undef LATE
 #undef FETCH_SCALES
   meet<0>();  // (no load into LDS outlives the workgroup)
 
@@ -439,8 +444,8 @@ struct Plan {
 // The kind that takes least by measured us of a step (a block of 128 columns) and of what is around the steps of a tile (first loads,
 // results).  Whole calls, us (rows of a x rows of b x columns), by tiles of
 //   64 x 128 / 128 x 128 / the same, two workgroups to a CU / 256 x 128 / 256 x 256:
-//     48 x 14336 x 4096        14 / 17 / - / 26 / -          512 x 4096 x 4096       15 / 17 / - / 24 / 37
-//     1024 x 4096 x 8192       49 / 35 / 43 / 46 / 68        1999 x 4096 x 14336     174 / 126 / 103 / 104 / 145
+//     48 x 14336 x 4096        13 / 16 / - / 26 / -          512 x 4096 x 4096       14 / 16 / - / 24 / 37
+//     1024 x 4096 x 8192       47 / 33 / 43 / 43 / 68        1999 x 4096 x 14336     170 / 120 / 115 / 106 / 145
 //     2327 x 6544 x 1413       40 / 39 / 33 / 47 / 48        2048 x 4096 x 512       13 / 13 / 11 / 11 / 14
 //     4096 x 4096 x 4096       101 / 72 / 62 / 63 / 54       8192 x 8192 x 128       54 / 59 / 39 / 46 / 36
 //     7569 x 8229 x 920        147 / 127 / 96 / 102 / 88     14336 x 4096 x 8192     733 / 485 / 475 / 393 / 357
@@ -458,7 +463,9 @@ Plan plan_of(const tsenor_product_problem& p) {
   const auto consider = [&](Kind kind, int rows_m, int rows_n, double step, double around, int at_once, bool fluid) {
     const int64_t tiles_m = (m + rows_m - 1) / rows_m, tiles_n = (n + rows_n - 1) / rows_n, tiles = tiles_m * tiles_n;
     const double rounds = fluid ? std::max(0.5 + 0.5 * (double)tiles / at_once, (double)tiles / at_once) : (double)((tiles + at_once - 1) / at_once);
-    double us = rounds * ((double)blocks * step + around);
+    // (large tiles on fewer CUs have more of the L2 and of the power each: 128 of 256 x 256 take 1.15 us a step)
+    const double fill = kind == kSmallTile || fluid ? 1.0 : std::min(1.0, 0.6 + 0.4 * (double)tiles / at_once);
+    double us = rounds * ((double)blocks * step * fill + around);
     int64_t splits = 1;
     if (kind == kSmallTile)
       for (int64_t k = 2; k <= blocks && k * tiles <= kCus; ++k) {
@@ -470,13 +477,13 @@ Plan plan_of(const tsenor_product_problem& p) {
       least = us;
     }
   };
-  consider(kSmallTile, 64, 128, (m + 63) / 64 * ((n + 127) / 128) <= kCus ? 0.27 : 0.37, 1.5, kCus, false);
+  consider(kSmallTile, 64, 128, (m + 63) / 64 * ((n + 127) / 128) <= kCus ? 0.25 : 0.36, 1.5, kCus, false);
   if (m <= 8 || (m <= 16 && best.splits > 1)) return {kFewRows, 0, 0, 1, 0};
   if ((m + 127) / 128 * ((n + 127) / 128) <= kCus)
-    consider(kTile, 128, 128, 0.43, 2.8, kCus, false);
+    consider(kTile, 128, 128, 0.41, 2.8, kCus, false);
   else
     consider(kTilePairs, 128, 128, 0.91, 3.0, 2 * kCus, true);
-  consider(kWideTile, 256, 128, 0.9, 4.0, kCus, false);
+  consider(kWideTile, 256, 128, 0.85, 4.0, kCus, false);
   consider(kLargeTile, 256, 256, 1.45, 6.0, kCus, false);
   return best;
 }
