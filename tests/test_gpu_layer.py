@@ -380,6 +380,59 @@ def test_clip_of_norms_that_are_not_finite_and_of_nothing(layer):
     assert abs(got[0] / (1e30 * math.sqrt(1000)) - 1) < 1e-6 and abs(float(g.double().norm()) - 1) < 1e-6
 
 
+# ---- no rows, and offsets beyond 32 bits ------------------------------------------------------------------------------------
+
+def test_matrices_without_rows(layer):
+    none, gain = torch.empty(0, 300, device="cuda"), torch.ones(300, device="cuda")
+    q, qt = layer.empty_scaled(0, 300, "cuda"), layer.empty_scaled(300, 0, "cuda")
+    layer.tsenor_quantize(layer.make_quantize(none, out=q, out_t=qt))
+    layer.tsenor_norm(layer.make_norm(none, gain, EPS, residual=none, out=q, sum_out=none.clone(), y_out=none.clone()))
+    dgain = torch.full((300,), 7.0, device="cuda")
+    p = layer.make_norm_backward(none, gain, EPS, none, dh=none.clone(), dgain=dgain)
+    layer.tsenor_norm_backward(p, torch.empty(max(1, layer.tsenor_norm_backward_workspace_bytes(p)), dtype=torch.uint8, device="cuda"))
+    assert not dgain.any()
+    w = scaled_from(layer, torch.randn(40, 300).double())
+    product(layer, q, w, torch.empty(0, 40, dtype=torch.bfloat16, device="cuda"))
+    product(layer, w, q, torch.empty(40, 0, dtype=torch.bfloat16, device="cuda"))
+    # a weight gradient over no tokens
+    got = product(layer, qt, layer.empty_scaled(50, 0, "cuda"), torch.full((300, 50), 3.0, dtype=torch.bfloat16, device="cuda"))
+    assert not got.any()
+    torch.cuda.synchronize()
+
+
+def test_rows_far_apart(layer):
+    gen = torch.Generator().manual_seed(9)
+    ld = 2 ** 30 + 24                                    # three rows: offsets up to 2^32 bytes
+    wide = torch.empty(3, ld, dtype=torch.bfloat16, device="cuda")
+    x = wide[:, 11:311]
+    x.copy_(rand(gen, 3, 300))
+    q, qt = layer.empty_scaled(3, 300, "cuda"), layer.empty_scaled(300, 3, "cuda")
+    layer.tsenor_quantize(layer.make_quantize(x, out=q, out_t=qt))
+    check_quantized(q, x.cpu().double(), False)
+    check_quantized(qt, x.cpu().double().t(), False)
+    gain, y = torch.ones(300, device="cuda"), torch.empty(3, 300, dtype=torch.bfloat16, device="cuda")
+    layer.tsenor_norm(layer.make_norm(x, gain, EPS, y_out=y))
+    same = torch.empty_like(y)
+    layer.tsenor_norm(layer.make_norm(x.contiguous(), gain, EPS, y_out=same))
+    assert torch.equal(y, same)
+    for m in (3, 200):                                   # results of one token, and of tiles
+        q = scaled_from(layer, rand(gen, m, 300))
+        w = scaled_from(layer, rand(gen, 100, 300))
+        want = product(layer, q, w, torch.empty(m, 100, dtype=torch.bfloat16, device="cuda"))
+        out = torch.empty(3 * ld, dtype=torch.bfloat16, device="cuda").as_strided((m, 100), (3 * ld // m, 1))
+        assert torch.equal(product(layer, q, w, out), want)
+
+
+def test_a_gradient_of_more_than_2_to_the_32_elements(layer):
+    count = 2 ** 32 + 5000
+    g = torch.full((count,), 2.0 ** -10, dtype=torch.bfloat16, device="cuda")
+    got = clip(layer, [g], 1.0)
+    norm = 2.0 ** -10 * math.sqrt(count)
+    assert abs(got[0] - norm) <= 1e-7 * norm and abs(got[1] * norm - 1) <= 1e-6
+    first = g[:1].clone()
+    assert bool((g == first).all()) and abs(float(first) * 2 ** 10 * norm - 1) <= 2.0 ** -8
+
+
 # ---- streams and graphs -----------------------------------------------------------------------------------------------------
 
 def test_calls_on_another_stream_and_in_a_graph(layer):
