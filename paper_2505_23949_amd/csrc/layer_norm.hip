@@ -2,8 +2,8 @@
 //
 // Both need a sum over the row before the first result, and both keep the row in registers meanwhile, so that it is read once:
 // THREADS threads to a row, VECTORS vectors of 8 to a thread, 128 columns on 16 neighbouring lanes, whose maximum is the scale's.
-// Rows too long for that are read twice.  Bound by memory: bf16 4096 x 8192 with residual, sum, norm and its 8-bit form 59 us
-// (5.1 TB/s), single precision 4096 x 4096 42 us (5.2); a single row by the launch (2.7 us).
+// Rows too long for that are read twice.  Bound by memory: bf16 4096 x 8192 with residual, sum, norm and its 8-bit form 57 us
+// (5.3 TB/s), single precision 4096 x 4096 42 us (5.2); a single row by the launch (2.7 us).
 #include <algorithm>
 #include <cmath>
 

@@ -21,7 +21,7 @@ struct ProductArgs {
   tsenor_scaled a, b;
   uint16_t* out;
   const uint8_t* mask;
-  int64_t out_ld;
+  int64_t out_ld, mask_ld;
   int m, n, blocks;      // blocks of 128 columns
   int tiles_m, tiles_n;  // of the tile kernel
   int splits;            // workgroups that share the columns of a tile: each leaves its sums in `parts`
@@ -46,7 +46,7 @@ __device__ __forceinline__ intx8 load_operand(const uint8_t* row) {
 __device__ __forceinline__ void write4(const ProductArgs& a, int i, int j, float (&v)[4]) {
   if (i >= a.m || j >= a.n) return;
   if (a.mask) {
-    const uint8_t* m = a.mask + (int64_t)i * a.n + j;
+    const uint8_t* m = a.mask + i * a.mask_ld + j;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (j + k < a.n && !m[k]) v[k] = 0.0f;
@@ -206,7 +206,7 @@ __device__ __forceinline__ void write_results(const ProductArgs& p, int64_t row,
   if (row >= p.m) return;
   const bool whole = col + 4 * T <= p.n;
   if (p.mask) {
-    const uint8_t* mask = p.mask + row * p.n + col;
+    const uint8_t* mask = p.mask + row * p.mask_ld + col;
     uint8_t keep[4 * T];
     if (whole) {
       __builtin_memcpy(keep, mask, 4 * T);
@@ -434,12 +434,25 @@ int check(const tsenor_product_problem* p) {
   return aligned_to(p->out, 2) ? TSENOR_OK : TSENOR_ERR_ALIGN;
 }
 
-// How a product is laid out.
+// How the rows of a and b from m0 and n0 on are multiplied.
 enum Kind { kNoColumns, kFewRows, kSmallTile, kTile, kTilePairs, kWideTile, kLargeTile };
-struct Plan {
+struct Part {
   Kind kind;
+  int64_t m0, n0, m, n;
   int tiles_m, tiles_n, splits;
+  double us;  // estimated
+};
+struct Plan {
+  int count;
+  Part parts[2];
   size_t workspace;
+};
+struct Cost {
+  Kind kind;
+  int rows_m, rows_n;
+  double step, around;
+  int at_once;  // workgroups that run at a time, a whole number of rounds of them unless `fluid`
+  bool fluid;
 };
 // The kind that takes least by measured us of a step (a block of 128 columns) and of what is around the steps of a tile (first loads,
 // results).  Whole calls, us (rows of a x rows of b x columns), by tiles of
@@ -454,38 +467,97 @@ struct Plan {
 // Up to 16 rows of a need no tiles: 1, 8 and 16 x 4096 x 14336 12.7, 14.0 and 15.7 (shared tiles 16); 16 x 4096 x 4096 8 (11); but 16 x
 // 14336 x 4096 18 where unshared tiles take 13, and 16 x 28672 x 8192 58 (51).  (Weights that no cache holds: 1, 8 and
 // 16 x 14336 x 4096 15, 16.6 and 19, tiles 17.)
+//
+// What does not fill a round of large or wide tiles can go to a launch of its own, with the kind that takes least for it (us, one
+// launch and two): 4096 x 14336 x 4096 222, 207 (large tiles, then wide ones); 5000 x 5000 x 5000 143, 134 (then 128 x 128); 14336 x
+// 4096 x 8192 413, 407 (power is what counts there); but 5000 x 5000 x 2000 59.8, 65.3.
+constexpr double kSecond = 5.0;  // us that a second launch has to save
+Part part_of(const Cost& c, int64_t m0, int64_t n0, int64_t m, int64_t n, int64_t blocks) {
+  const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n, tiles = tiles_m * tiles_n;
+  const double steps = (double)blocks * c.step;
+  double us;
+  if (c.fluid) {
+    const double share = (double)tiles / c.at_once;
+    us = std::max(0.5 + 0.5 * share, share) * (steps + c.around);
+  } else {
+    // (large tiles on fewer CUs have more of the L2 and of the power each: 128 of 256 x 256 take 1.15 us a step)
+    const int64_t rest = tiles % c.at_once;
+    const double fill = c.kind == kSmallTile ? 1.0 : 0.6 + 0.4 * (double)rest / c.at_once;
+    us = (double)(tiles / c.at_once) * (steps + c.around) + (rest ? steps * fill + c.around : 0.0);
+  }
+  int64_t splits = 1;
+  if (c.kind == kSmallTile)
+    for (int64_t k = 2; k <= blocks && k * tiles <= kCus; ++k) {
+      const double shared = (double)((blocks + k - 1) / k) * c.step + c.around + 1.0 + 0.025 * (double)(k * tiles);
+      if (shared < us) us = shared, splits = k;
+    }
+  return {c.kind, m0, n0, m, n, (int)tiles_m, (int)tiles_n, (int)splits, us};
+}
+
+constexpr Cost kWide = {kWideTile, 256, 128, 0.85, 4.0, kCus, false}, kLarge = {kLargeTile, 256, 256, 1.45, 6.0, kCus, false};
+
+// the kind that takes least for all rows from m0 and n0 on
+Part part_of(int64_t m0, int64_t n0, int64_t m, int64_t n, int64_t blocks) {
+  const bool few = (m + 63) / 64 * ((n + 127) / 128) <= kCus, pairs = (m + 127) / 128 * ((n + 127) / 128) > kCus;
+  Part best = part_of({kSmallTile, 64, 128, few ? 0.25 : 0.36, 1.5, kCus, false}, m0, n0, m, n, blocks);
+  if (m <= 8 || (m <= 16 && best.splits > 1)) {
+    best.kind = kFewRows, best.splits = 1;
+    return best;
+  }
+  for (const Cost& c : {pairs ? Cost{kTilePairs, 128, 128, 0.91, 3.0, 2 * kCus, true} : Cost{kTile, 128, 128, 0.41, 2.8, kCus, false}, kWide, kLarge}) {
+    const Part part = part_of(c, m0, n0, m, n, blocks);
+    if (part.us < best.us) best = part;
+  }
+  return best;
+}
+
 Plan plan_of(const tsenor_product_problem& p) {
   const int64_t m = p.a.rows, n = p.b.rows, blocks = blocks_of(p.a.cols);
-  if (blocks == 0) return {kNoColumns, 0, 0, 1, 0};
-  Plan best = {};
-  double least = 0.0;
-  // at_once: workgroups that run at a time, a whole number of rounds of them unless `fluid`
-  const auto consider = [&](Kind kind, int rows_m, int rows_n, double step, double around, int at_once, bool fluid) {
-    const int64_t tiles_m = (m + rows_m - 1) / rows_m, tiles_n = (n + rows_n - 1) / rows_n, tiles = tiles_m * tiles_n;
-    const double rounds = fluid ? std::max(0.5 + 0.5 * (double)tiles / at_once, (double)tiles / at_once) : (double)((tiles + at_once - 1) / at_once);
-    // (large tiles on fewer CUs have more of the L2 and of the power each: 128 of 256 x 256 take 1.15 us a step)
-    const double fill = kind == kSmallTile || fluid ? 1.0 : std::min(1.0, 0.6 + 0.4 * (double)tiles / at_once);
-    double us = rounds * ((double)blocks * step * fill + around);
-    int64_t splits = 1;
-    if (kind == kSmallTile)
-      for (int64_t k = 2; k <= blocks && k * tiles <= kCus; ++k) {
-        const double shared = (double)((blocks + k - 1) / k) * step + around + 1.0 + 0.025 * (double)(k * tiles);
-        if (shared < us) us = shared, splits = k;
-      }
-    if (best.tiles_m == 0 || us < least) {
-      best = {kind, (int)tiles_m, (int)tiles_n, (int)splits, splits > 1 ? (size_t)(splits * tiles) * 64 * 128 * sizeof(float) : 0};
-      least = us;
+  if (m == 0 || n == 0) return {};
+  if (blocks == 0) return {1, {{kNoColumns, 0, 0, m, n, 0, 0, 1, 0.0}}, 0};
+  Plan best = {1, {part_of(0, 0, m, n, blocks)}, 0};
+  double least = best.parts[0].us;
+  for (const Cost& c : {kWide, kLarge}) {
+    const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n;
+    const int64_t whole = tiles_m * tiles_n / kCus * kCus;  // tiles of the whole rounds
+    for (int of_b = 0; of_b < 2; ++of_b) {
+      const int64_t m1 = of_b ? m : whole / tiles_n * c.rows_m, n1 = of_b ? whole / tiles_m * c.rows_n : n;
+      if (m1 <= 0 || n1 <= 0 || m1 > m || n1 > n || (m1 == m && n1 == n)) continue;
+      const Part first = part_of(c, 0, 0, m1, n1, blocks);
+      const Part rest = of_b ? part_of(0, n1, m, n - n1, blocks) : part_of(m1, 0, m - m1, n, blocks);
+      if (first.us + rest.us + kSecond < least) best = {2, {first, rest}, 0}, least = first.us + rest.us + kSecond;
     }
-  };
-  consider(kSmallTile, 64, 128, (m + 63) / 64 * ((n + 127) / 128) <= kCus ? 0.25 : 0.36, 1.5, kCus, false);
-  if (m <= 8 || (m <= 16 && best.splits > 1)) return {kFewRows, 0, 0, 1, 0};
-  if ((m + 127) / 128 * ((n + 127) / 128) <= kCus)
-    consider(kTile, 128, 128, 0.41, 2.8, kCus, false);
-  else
-    consider(kTilePairs, 128, 128, 0.91, 3.0, 2 * kCus, true);
-  consider(kWideTile, 256, 128, 0.85, 4.0, kCus, false);
-  consider(kLargeTile, 256, 256, 1.45, 6.0, kCus, false);
+  }
+  for (int k = 0; k < best.count; ++k)
+    if (best.parts[k].splits > 1)
+      best.workspace = (size_t)best.parts[k].splits * best.parts[k].tiles_m * best.parts[k].tiles_n * 64 * 128 * sizeof(float);
   return best;
+}
+
+void launch(const tsenor_product_problem& p, const Part& part, void* workspace, hipStream_t s) {
+  ProductArgs a = {};
+  a.a = p.a, a.b = p.b, a.out = static_cast<uint16_t*>(p.out) + part.m0 * p.out_ld + part.n0, a.out_ld = p.out_ld;
+  a.a.values += part.m0 * p.a.ld, a.a.scales += part.m0, a.b.values += part.n0 * p.b.ld, a.b.scales += part.n0;
+  a.mask = p.mask ? p.mask + part.m0 * p.b.rows + part.n0 : nullptr, a.mask_ld = p.b.rows;
+  a.m = (int)part.m, a.n = (int)part.n, a.blocks = (int)blocks_of(p.a.cols);
+  a.tiles_m = part.tiles_m, a.tiles_n = part.tiles_n, a.splits = part.splits, a.parts = static_cast<floatx4*>(workspace);
+  const unsigned tiles = (unsigned)(part.tiles_m * part.tiles_n), groups = tiles * (unsigned)part.splits;
+  switch (part.kind) {
+    case kNoColumns: zero_kernel<<<(unsigned)std::min<int64_t>(((int64_t)a.m * a.n + 255) / 256, 65536), 256, 0, s>>>(a); break;
+    case kFewRows: few_rows_kernel<<<(unsigned)((a.n + 15) / 16), kWaves * kWave, 0, s>>>(a); break;
+    case kSmallTile:
+      if (part.splits > 1) {
+        tile_kernel<2, 1, 6, true><<<groups, 256, 0, s>>>(a);
+        join_kernel<2, 1><<<tiles * 4, 256, 0, s>>>(a);
+      } else {
+        tile_kernel<2, 1, 6, false><<<groups, 256, 0, s>>>(a);
+      }
+      break;
+    case kTile: tile_kernel<2, 2, 4, false><<<groups, 256, 0, s>>>(a); break;
+    case kTilePairs: tile_kernel<2, 2, 2, false><<<groups, 256, 0, s>>>(a); break;
+    case kWideTile: tile_kernel<2, 4, 3, false><<<groups, 256, 0, s>>>(a); break;
+    case kLargeTile: tile_kernel<4, 4, 2, false><<<groups, 256, 0, s>>>(a); break;
+  }
 }
 
 }  // namespace
@@ -497,30 +569,8 @@ extern "C" size_t tsenor_product_workspace_bytes(const tsenor_product_problem* p
 extern "C" int tsenor_product(const tsenor_product_problem* p, void* workspace, size_t workspace_bytes, tsenor_stream_t stream) {
   const int rc = check(p);
   if (rc != TSENOR_OK) return rc;
-  if (p->a.rows == 0 || p->b.rows == 0) return TSENOR_OK;
   const Plan plan = plan_of(*p);
   if (plan.workspace && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < plan.workspace)) return TSENOR_ERR_WORKSPACE;
-  ProductArgs a = {};
-  a.a = p->a, a.b = p->b, a.out = static_cast<uint16_t*>(p->out), a.mask = p->mask, a.out_ld = p->out_ld;
-  a.m = (int)p->a.rows, a.n = (int)p->b.rows, a.blocks = (int)blocks_of(p->a.cols);
-  a.tiles_m = plan.tiles_m, a.tiles_n = plan.tiles_n, a.splits = plan.splits, a.parts = static_cast<floatx4*>(workspace);
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  const unsigned tiles = (unsigned)(plan.tiles_m * plan.tiles_n), groups = tiles * (unsigned)plan.splits;
-  switch (plan.kind) {
-    case kNoColumns: zero_kernel<<<(unsigned)std::min<int64_t>(((int64_t)a.m * a.n + 255) / 256, 65536), 256, 0, s>>>(a); break;
-    case kFewRows: few_rows_kernel<<<(unsigned)((a.n + 15) / 16), kWaves * kWave, 0, s>>>(a); break;
-    case kSmallTile:
-      if (plan.splits > 1) {
-        tile_kernel<2, 1, 6, true><<<groups, 256, 0, s>>>(a);
-        join_kernel<2, 1><<<tiles * 4, 256, 0, s>>>(a);
-      } else {
-        tile_kernel<2, 1, 6, false><<<groups, 256, 0, s>>>(a);
-      }
-      break;
-    case kTile: tile_kernel<2, 2, 4, false><<<groups, 256, 0, s>>>(a); break;
-    case kTilePairs: tile_kernel<2, 2, 2, false><<<tiles, 256, 0, s>>>(a); break;
-    case kWideTile: tile_kernel<2, 4, 3, false><<<groups, 256, 0, s>>>(a); break;
-    case kLargeTile: tile_kernel<4, 4, 2, false><<<groups, 256, 0, s>>>(a); break;
-  }
+  for (int k = 0; k < plan.count; ++k) launch(*p, plan.parts[k], workspace, static_cast<hipStream_t>(stream));
   return status_of_launches();
 }

@@ -305,6 +305,21 @@ def test_product(layer, m, n, k, square):
     assert (got - want).norm() <= 2.5e-3 * want.norm() + 2.0 ** -14 * sizes.norm()
 
 
+# enough tiles that the last round of them is left to a launch of its own, by rows of a or of b
+@pytest.mark.parametrize("m,n,k", [(4096, 14336, 640), (9001, 4100, 2500), (4100, 9001, 2500), (5001, 5003, 3900), (4200, 4300, 4000)])
+def test_large_product_of_small_whole_numbers(layer, m, n, k):
+    gen = torch.Generator("cuda").manual_seed(m + n + k)
+    a = torch.randint(-4, 5, (m, k), generator=gen, device="cuda").float()
+    b = torch.randint(-4, 5, (n, k), generator=gen, device="cuda").float() * 0.5
+    qa, qb = scaled_from(layer, a), scaled_from(layer, b)
+    mask = (torch.rand(m, n, generator=gen, device="cuda") > 0.25).to(torch.uint8)
+    wide = torch.full((m, n + 5), 7.0, dtype=torch.bfloat16, device="cuda")
+    product(layer, qa, qb, wide[:, 3:3 + n], mask)
+    want = (a @ b.t()).bfloat16() * mask                 # (halves of whole numbers below 2^18: sums in single precision are exact)
+    assert torch.equal(wide[:, 3:3 + n], want)
+    assert (wide[:, :3] == 7).all() and (wide[:, 3 + n:] == 7).all()
+
+
 def test_product_without_columns_is_zero(layer):
     a, b = layer.empty_scaled(5, 0, "cuda"), layer.empty_scaled(9, 0, "cuda")
     assert not product(layer, a, b, torch.full((5, 9), 3.0, dtype=torch.bfloat16, device="cuda")).any()
