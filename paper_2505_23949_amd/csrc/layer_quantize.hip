@@ -4,9 +4,9 @@
 // A workgroup takes a tile of 128 x 128: a block of either direction lies within it, so x is read once whatever is wanted.  A
 // thread holds 4 x 8 of it: the row maxima are found over 16 lanes, the column maxima over 4 rows, 4 lanes and 8 waves,
 // the tile's over all.  Its 4 rows of a column are one 4-byte piece of the transposed tile, which goes through LDS so that both
-// results leave in whole 128-byte rows.  Bound by memory: 28672 x 8192 in single precision with a mask, both ways, 320 us
-// (5.15 TB/s), bf16 4096 x 14336 both ways 58 us (4.05); a few tiles by the chain of load, maximum and store: 1024 x 4096 7.4 us.
-// (8 x 8 to a thread, half as many waves: 327, 65 and 10.6.)
+// results leave in whole 128-byte rows.  Bound by memory: 28672 x 8192 in single precision with a mask, both ways, 317 us
+// (5.2 TB/s), bf16 4096 x 14336 both ways 51 us (4.6); a few tiles by the chain of load, maximum and store: 1024 x 4096 6.7 us,
+// 7.2 where the loads of a row wait for those of the one before.  (8 x 8 to a thread, half as many waves, took 2, 12 and 43 % more.)
 #include "layer.hpp"
 
 namespace {
@@ -33,29 +33,50 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantizeArgs a) {
   const int64_t row0 = (int64_t)tile_row * kBlock + lane_row;
   const int col0 = tile_col * kBlock + lane_col;
 
+  // All loads of a thread are asked for before the first is waited for: those of rows past the last read the last one.
+  Raw8<BF16> raw[kRows];
+  uint32_t keep[kRows][2];
+  const bool whole = col0 + 8 <= a.cols;
+  const auto row_of = [&](int r) { return min(row0 + r, (int64_t)a.rows - 1); };
+  const auto values_of = [&](int r) { return static_cast<const char*>(a.x) + row_of(r) * a.ld * (BF16 ? 2 : 4); };
+  if (whole) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) __builtin_memcpy(raw[r].w, values_of(r) + (int64_t)col0 * (BF16 ? 2 : 4), sizeof(raw[r].w));
+  } else {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) raw[r] = load_raw8<BF16>(values_of(r), col0, a.cols);
+  }
+  if (a.mask) {
+    const uint8_t* const mask = a.mask + col0;
+    if (whole) {
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) __builtin_memcpy(keep[r], mask + row_of(r) * a.cols, 8);
+    } else {
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        keep[r][0] = keep[r][1] = 0u;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (col0 + c < a.cols) keep[r][c / 4] |= (uint32_t)mask[row_of(r) * a.cols + c] << (c % 4 * 8);
+      }
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+
   float x[kRows][8];
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
-    const bool inside = row0 + r < a.rows;
-    const char* row = static_cast<const char*>(a.x) + (inside ? row0 + r : 0) * a.ld * (BF16 ? 2 : 4);
-    load_row8<BF16>(row, col0, inside ? a.cols : 0, x[r]);
+    widen8<BF16>(raw[r], x[r]);
+    if (row0 + r >= a.rows) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) x[r][c] = 0.0f;
+    }
   }
   if (a.mask) {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      if (row0 + r >= a.rows) continue;
-      const uint8_t* m = a.mask + (row0 + r) * a.cols;
-      if (col0 + 8 <= a.cols) {
-        uint32_t w[2];
-        __builtin_memcpy(w, m + col0, 8);
+    for (int r = 0; r < kRows; ++r)
 #pragma unroll
-        for (int c = 0; c < 8; ++c) x[r][c] = (w[c / 4] >> (c % 4 * 8) & 0xFFu) ? x[r][c] : 0.0f;
-      } else {
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-          if (col0 + c < a.cols && !m[col0 + c]) x[r][c] = 0.0f;
-      }
-    }
+      for (int c = 0; c < 8; ++c) x[r][c] = (keep[r][c / 4] >> (c % 4 * 8) & 0xFFu) ? x[r][c] : 0.0f;
   }
 
   uint32_t of_row[kRows], of_col[8];
