@@ -570,6 +570,7 @@ extern "C" int tsenor_product(const tsenor_product_problem* p, void* workspace, 
   const int rc = check(p);
   if (rc != TSENOR_OK) return rc;
   const Plan plan = plan_of(*p);
+  if (plan.count == 0) return TSENOR_OK;
   if (plan.workspace && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < plan.workspace)) return TSENOR_ERR_WORKSPACE;
   for (int k = 0; k < plan.count; ++k) launch(*p, plan.parts[k], workspace, static_cast<hipStream_t>(stream));
   return status_of_launches();
