@@ -20,11 +20,11 @@ inline bool aligned_to(const void* p, size_t to) { return reinterpret_cast<uintp
 inline size_t size_of(int dtype) { return dtype == TSENOR_BF16 ? 2 : 4; }
 inline bool known(int dtype) { return dtype == TSENOR_F32 || dtype == TSENOR_BF16; }
 inline int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
-// (rows: the last row of a tile of 256 still has a 32-bit number; tiles: a grid of one workgroup of 256 threads each counts fewer than
-// 2^32 threads)
+// (rows: the last row of a tile of 256 still has a 32-bit number; tiles: a grid counts fewer than 2^32 threads, and takes
+// 512 for each tile to quantise it, 256 for each half of one in a product)
 constexpr int64_t kMaxRows = INT32_MAX - 255;
 inline bool shape_ok(int64_t rows, int64_t cols) {
-  return rows >= 0 && rows <= kMaxRows && cols >= 0 && cols <= (int64_t)1 << 24 && blocks_of(rows) * blocks_of(cols) < (int64_t)1 << 24;
+  return rows >= 0 && rows <= kMaxRows && cols >= 0 && cols <= (int64_t)1 << 24 && blocks_of(rows) * blocks_of(cols) < (int64_t)1 << 23;
 }
 constexpr int64_t kMaxLd = (int64_t)1 << 40;  // (products with a row number stay far below 2^63 + bytes per element)
 inline bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld <= kMaxLd; }

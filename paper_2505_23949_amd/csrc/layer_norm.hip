@@ -23,10 +23,10 @@ struct NormArgs {
   bool gain_bf16;
 };
 
-__device__ __forceinline__ const void* at_row(const void* p, int64_t row, int64_t ld, bool bf16) {
+__host__ __device__ __forceinline__ const void* at_row(const void* p, int64_t row, int64_t ld, bool bf16) {
   return static_cast<const char*>(p) + row * ld * (bf16 ? 2 : 4);
 }
-__device__ __forceinline__ void* at_row(void* p, int64_t row, int64_t ld, bool bf16) {
+__host__ __device__ __forceinline__ void* at_row(void* p, int64_t row, int64_t ld, bool bf16) {
   return static_cast<char*>(p) + row * ld * (bf16 ? 2 : 4);
 }
 __device__ __forceinline__ void load_gain8(const void* gain, bool bf16, int c, int cols, float (&g)[8]) {
@@ -345,6 +345,7 @@ int check(const tsenor_norm_backward_problem* p) {
   return TSENOR_OK;
 }
 
+constexpr int64_t kLaunchRows = 1 << 21;  // of up to 1024 threads: a grid counts fewer than 2^32 threads
 constexpr int kLongRow = 16384;  // columns that the registers of 1024 threads hold, 16 to a thread
 inline size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -403,7 +404,11 @@ void launch_backward(const BackwardArgs& a, unsigned groups, float2* stats, hipS
   } else if (a.cols <= kLongRow) {
     norm_backward_kernel<BF16, 1024, 2, false><<<groups, 1024, 0, s>>>(a);
   } else {
-    if (a.rows > 0) backward_stats_kernel<BF16><<<(unsigned)a.rows, kLongThreads, 0, s>>>(a, stats);
+    BackwardArgs part = a;
+    for (int64_t row = 0; row < a.rows; row += kLaunchRows) {
+      part.h = at_row(a.h, row, a.ld, BF16), part.dy = at_row(a.dy, row, a.dy_ld, BF16);
+      backward_stats_kernel<BF16><<<(unsigned)std::min(a.rows - row, kLaunchRows), kLongThreads, 0, s>>>(part, stats + row);
+    }
     backward_apply_kernel<BF16><<<dim3((unsigned)((a.cols + kSlab - 1) / kSlab), groups), 256, 0, s>>>(a, stats);
   }
 }
@@ -416,11 +421,20 @@ extern "C" int tsenor_norm(const tsenor_norm_problem* p, tsenor_stream_t stream)
   if (p->rows == 0 || p->cols == 0) return TSENOR_OK;
   NormArgs a = {};
   a.x = p->x, a.residual = p->residual, a.gain = p->gain, a.sum_out = p->sum_out, a.y_out = p->y_out;
-  a.ld = p->ld, a.residual_ld = p->residual_ld, a.rows = (int)p->rows, a.cols = (int)p->cols, a.eps = (float)p->eps;
+  a.ld = p->ld, a.residual_ld = p->residual_ld, a.cols = (int)p->cols, a.eps = (float)p->eps;
   a.out = p->out;
   a.gain_bf16 = p->gain_dtype == TSENOR_BF16;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  p->dtype == TSENOR_BF16 ? launch_norm<true>(a, s) : launch_norm<false>(a, s);
+  const bool bf16 = p->dtype == TSENOR_BF16;
+  for (int64_t row = 0; row < p->rows; row += kLaunchRows) {
+    a.rows = (int)std::min(p->rows - row, kLaunchRows);
+    bf16 ? launch_norm<true>(a, s) : launch_norm<false>(a, s);
+    a.x = at_row(a.x, a.rows, a.ld, bf16);
+    if (a.residual) a.residual = at_row(a.residual, a.rows, a.residual_ld, bf16);
+    if (a.sum_out) a.sum_out = at_row(a.sum_out, a.rows, a.cols, bf16);
+    if (a.y_out) a.y_out = at_row(a.y_out, a.rows, a.cols, bf16);
+    if (a.out.values) a.out.values += a.rows * a.out.ld, a.out.scales += a.rows;
+  }
   return status_of_launches();
 }
 

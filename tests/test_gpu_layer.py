@@ -438,6 +438,29 @@ def test_rows_far_apart(layer):
         assert torch.equal(product(layer, q, w, out), want)
 
 
+@pytest.mark.parametrize("rows,cols", [(2 ** 26 + 5, 1), (2 ** 22 + 3, 1030)])
+def test_more_rows_than_a_grid_has_threads_for(layer, rows, cols):
+    gen = torch.Generator("cuda").manual_seed(rows)
+    some = torch.randn(1009, cols, generator=gen, device="cuda").bfloat16()     # a row's number modulo a prime: shifted rows differ
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[:1009], at = some, 1009
+    while at < rows:                                     # copies double
+        x[at:2 * at] = x[:min(at, rows - at)]
+        at *= 2
+    whole = rows // 1009 * 1009
+    gain = torch.ones(cols, device="cuda")
+    y, q = torch.zeros_like(x), layer.empty_scaled(rows, cols, "cuda")
+    layer.tsenor_norm(layer.make_norm(x, gain, EPS, y_out=y, out=q))
+    want, want_q = torch.empty_like(some), layer.empty_scaled(1009, cols, "cuda")
+    layer.tsenor_norm(layer.make_norm(some, gain, EPS, y_out=want, out=want_q))
+    assert torch.equal(x[whole - 1009:whole], some)
+    for first in (0, 2 ** 21 // 1009 * 1009, whole // 2 // 1009 * 1009, whole - 1009):
+        assert torch.equal(y[first:first + 1009], want)
+        assert torch.equal(q.values[first:first + 1009].view(torch.uint8), want_q.values.view(torch.uint8))
+        assert torch.equal(q.scales.view(torch.uint8)[:, first:first + 1009], want_q.scales.view(torch.uint8)[:, :1009])
+    assert torch.equal(y[whole:], want[:rows - whole])
+
+
 def test_a_gradient_of_more_than_2_to_the_32_elements(layer):
     count = 2 ** 32 + 5000
     g = torch.full((count,), 2.0 ** -10, dtype=torch.bfloat16, device="cuda")
