@@ -166,6 +166,8 @@ def scaled_matrix(values, scales, cols: int) -> ScaledMatrix:
 
     if values.dtype != torch.float8_e4m3fn or scales.dtype not in (torch.float8_e8m0fnu, torch.uint8):
         raise TypeError(f"values must be float8_e4m3fn and scales float8_e8m0fnu or uint8, got {values.dtype} and {scales.dtype}")
+    if values.device != scales.device:
+        raise ValueError("values and scales must be on one device")
     if values.dim() != 2 or scales.dim() != 2 or values.stride(1) != 1 or scales.stride(1) != 1:
         raise ValueError("values and scales must be 2-D tensors with unit column stride")
     if values.shape[1] < _round_up(cols, TSENOR_SCALE_BLOCK):

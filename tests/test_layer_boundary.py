@@ -198,3 +198,11 @@ def test_python_checks():
         l.make_clip([x], 1.0, norm_out=torch.zeros(1))
     with pytest.raises(ValueError, match="contiguous"):
         l.make_clip([x.t()], 1.0, norm_out=torch.zeros(2))
+
+
+def test_scaled_matrix_on_two_devices():
+    from paper_2505_23949_amd import layer as l
+
+    values = torch.zeros(4, 256).to(torch.float8_e4m3fn)
+    with pytest.raises(ValueError, match="one device"):
+        l.scaled_matrix(values, torch.zeros(2, 16, dtype=torch.uint8, device="meta"), 200)
