@@ -67,7 +67,15 @@ template <bool BF16>
 __device__ __forceinline__ double add_squares(const char* in, int size, double s) {
   float x[kVectors][8];
 #pragma unroll
-  for (int v = 0; v < kVectors; ++v) load_row8<BF16>(in, element_of(v), size, x[v]);
+  for (int v = 0; v < kVectors; ++v) {
+    if (size == kChunk) {
+      Raw8<BF16> raw;
+      __builtin_memcpy(raw.w, in + element_of(v) * (BF16 ? 2 : 4), sizeof(raw.w));
+      widen8<BF16>(raw, x[v]);
+    } else {
+      load_row8<BF16>(in, element_of(v), size, x[v]);
+    }
+  }
 #pragma unroll
   for (int v = 0; v < kVectors; ++v)
 #pragma unroll

@@ -47,10 +47,14 @@ __device__ __forceinline__ float inverse_root(float x) {
 // h of 8 columns of a row: x, or its sum with the residual as it is stored
 template <bool BF16>
 __device__ __forceinline__ void load_sum8(const NormArgs& a, int64_t row, int c, float (&h)[8]) {
-  load_row8<BF16>(at_row(a.x, row, a.ld, BF16), c, a.cols, h);
-  if (!a.residual) return;
+  const Raw8<BF16> x = load_raw8<BF16>(at_row(a.x, row, a.ld, BF16), c, a.cols);
+  if (!a.residual) {
+    widen8<BF16>(x, c, a.cols, h);
+    return;
+  }
+  const Raw8<BF16> residual = load_raw8<BF16>(at_row(a.residual, row, a.residual_ld, BF16), c, a.cols);
   float r[8];
-  load_row8<BF16>(at_row(a.residual, row, a.residual_ld, BF16), c, a.cols, r);
+  widen8<BF16>(x, c, a.cols, h), widen8<BF16>(residual, c, a.cols, r);
 #pragma unroll
   for (int k = 0; k < 8; ++k) h[k] = h[k] + r[k];
   if constexpr (BF16) {
@@ -202,7 +206,8 @@ __device__ __forceinline__ void load_backward(const BackwardArgs& a, int64_t row
   }
 }
 
-// A workgroup takes every gridDim.x-th row, asks for the next before it works on one (AHEAD: where the registers hold both), and keeps
+// A workgroup takes every gridDim.x-th row, asks for the next before it works on one (AHEAD: where the registers hold both, which 1024
+// threads have for bf16 only), and keeps
 // its sum of dgain in registers.  Bound by memory: 2047 x 4096 in single precision 31 us (4.35 TB/s), bf16 4096 x 4096 with dsum 33
 // (45 where each row was asked for when its turn came).
 template <bool BF16, int THREADS, int VECTORS, bool AHEAD>
@@ -217,7 +222,8 @@ __global__ __launch_bounds__(THREADS) void norm_backward_kernel(BackwardArgs a) 
     float squares = 0.0f, along = 0.0f;
 #pragma unroll
     for (int v = 0; v < VECTORS; ++v) {
-      widen8<BF16>(x.h[v], h[v]), widen8<BF16>(x.dy[v], dy[v]);
+      const int c = (v * THREADS + t) * 8;
+      widen8<BF16>(x.h[v], c, a.cols, h[v]), widen8<BF16>(x.dy[v], c, a.cols, dy[v]);
 #pragma unroll
       for (int k = 0; k < 8; ++k) squares = fmaf(h[v][k], h[v][k], squares), along = fmaf(g[v][k] * dy[v][k], h[v][k], along);
     }
@@ -228,7 +234,7 @@ __global__ __launch_bounds__(THREADS) void norm_backward_kernel(BackwardArgs a) 
     for (int v = 0; v < VECTORS; ++v) {
       const int c = (v * THREADS + t) * 8;
       float d[8] = {};
-      if (a.dsum) widen8<BF16>(AHEAD ? x.dsum[v] : load_raw8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols), d);
+      if (a.dsum) widen8<BF16>(AHEAD ? x.dsum[v] : load_raw8<BF16>(at_row(a.dsum, row, a.dsum_ld, BF16), c, a.cols), c, a.cols, d);
       write_backward8<BF16>(a, row, c, inverse, toward, h[v], dy[v], g[v], d, dg[v]);
     }
   };
@@ -400,7 +406,7 @@ void launch_backward(const BackwardArgs& a, unsigned groups, float2* stats, hipS
   } else if (a.cols <= 4096) {
     norm_backward_kernel<BF16, 512, 1, true><<<groups, 512, 0, s>>>(a);
   } else if (a.cols <= 8192) {
-    norm_backward_kernel<BF16, 1024, 1, true><<<groups, 1024, 0, s>>>(a);
+    norm_backward_kernel<BF16, 1024, 1, BF16><<<groups, 1024, 0, s>>>(a);
   } else if (a.cols <= kLongRow) {
     norm_backward_kernel<BF16, 1024, 2, false><<<groups, 1024, 0, s>>>(a);
   } else {

@@ -35,29 +35,28 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantizeArgs a) {
 
   // All loads of a thread are asked for before the first is waited for: those of rows past the last read the last one.
   Raw8<BF16> raw[kRows];
-  uint32_t keep[kRows][2];
-  const bool whole = col0 + 8 <= a.cols;
+  uint64_t keep[kRows];
   const auto row_of = [&](int r) { return min(row0 + r, (int64_t)a.rows - 1); };
-  const auto values_of = [&](int r) { return static_cast<const char*>(a.x) + row_of(r) * a.ld * (BF16 ? 2 : 4); };
-  if (whole) {
+  const int before = max(col0 + 8 - a.cols, 0);  // columns before col0 that the last 8 of a row begin with
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) __builtin_memcpy(raw[r].w, values_of(r) + (int64_t)col0 * (BF16 ? 2 : 4), sizeof(raw[r].w));
-  } else {
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) raw[r] = load_raw8<BF16>(values_of(r), col0, a.cols);
+  for (int r = 0; r < kRows; ++r) {
+    const char* const row = static_cast<const char*>(a.x) + row_of(r) * a.ld * (BF16 ? 2 : 4);
+    if (a.cols >= 8)  // (without a condition of each thread's own: 1072 x 2928 6.6 us, with one 7.3)
+      __builtin_memcpy(raw[r].w, row + (int64_t)(col0 - before) * (BF16 ? 2 : 4), sizeof(raw[r].w));
+    else
+      raw[r] = load_raw8<BF16>(row, col0, a.cols);
   }
   if (a.mask) {
-    const uint8_t* const mask = a.mask + col0;
-    if (whole) {
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) __builtin_memcpy(keep[r], mask + row_of(r) * a.cols, 8);
-    } else {
-#pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        keep[r][0] = keep[r][1] = 0u;
+    for (int r = 0; r < kRows; ++r) {
+      const uint8_t* const mask = a.mask + row_of(r) * a.cols;
+      if (a.cols >= 8) {
+        __builtin_memcpy(&keep[r], mask + (col0 - before), 8);
+      } else {
+        keep[r] = 0u;
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-          if (col0 + c < a.cols) keep[r][c / 4] |= (uint32_t)mask[row_of(r) * a.cols + c] << (c % 4 * 8);
+          if (col0 + c < a.cols) keep[r] |= (uint64_t)mask[col0 + c] << (c * 8);
       }
     }
   }
@@ -66,17 +65,19 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantizeArgs a) {
   float x[kRows][8];
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
-    widen8<BF16>(raw[r], x[r]);
-    if (row0 + r >= a.rows) {
+    widen8<BF16>(raw[r], col0, a.cols, x[r]);
+    if (row0 + r >= a.rows || col0 >= a.cols) {
 #pragma unroll
       for (int c = 0; c < 8; ++c) x[r][c] = 0.0f;
     }
   }
   if (a.mask) {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
+    for (int r = 0; r < kRows; ++r) {
+      if (a.cols >= 8) keep[r] >>= before % 8 * 8;  // (past the last column x is 0 whatever it says)
 #pragma unroll
-      for (int c = 0; c < 8; ++c) x[r][c] = (keep[r][c / 4] >> (c % 4 * 8) & 0xFFu) ? x[r][c] : 0.0f;
+      for (int c = 0; c < 8; ++c) x[r][c] = (keep[r] >> (c * 8) & 0xFFu) ? x[r][c] : 0.0f;
+    }
   }
 
   uint32_t of_row[kRows], of_col[8];
