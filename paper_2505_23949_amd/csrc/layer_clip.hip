@@ -6,7 +6,7 @@
 // atomics, nothing to clear, and no launch between the two.  Bound by memory.  The second pass goes through the chunks from the
 // last to the first, what the first one read last being still in the cache of the memory side (2 % for a layer of 436 MB), and
 // its accesses are marked as the last ones to what they touch, so that results do not drive out what is still to be read: the
-// gradients of a layer of 4096 (218 M in bf16) 215 us, 243 without the mark.  (8 or 4 vectors in flight and half as many
+// gradients of a layer of 4096 (218 M in bf16) 210-215 us, 243 without the mark.  (8 or 4 vectors in flight and half as many
 // workgroups: 241, 227.)
 #include <algorithm>
 

@@ -206,10 +206,10 @@ __device__ __forceinline__ void load_backward(const BackwardArgs& a, int64_t row
   }
 }
 
-// A workgroup takes every gridDim.x-th row, asks for the next before it works on one (AHEAD: where the registers hold both, which 1024
-// threads have for bf16 only), and keeps
-// its sum of dgain in registers.  Bound by memory: 2047 x 4096 in single precision 31 us (4.35 TB/s), bf16 4096 x 4096 with dsum 33
-// (45 where each row was asked for when its turn came).
+// A workgroup takes every gridDim.x-th row, asks for the next before it works on one (AHEAD: where the registers hold both, which those
+// of 1024 threads do for bf16 only), and keeps its sum of dgain in registers.  Bound by memory: 2047 x 4096 in single precision 31 us
+// (4.3 TB/s), bf16 4096 x 4096 with dsum 33 (45 where each row was asked for when its turn came); single precision 2048 x 8192 55,
+// with the next row asked for 55.6 and, where that spills, 2000 x 5001 53 for 47.
 template <bool BF16, int THREADS, int VECTORS, bool AHEAD>
 __global__ __launch_bounds__(THREADS) void norm_backward_kernel(BackwardArgs a) {
   __shared__ float part[2][16][2];
