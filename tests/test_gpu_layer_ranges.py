@@ -1,0 +1,47 @@
+"""The layer operators where intermediate results could leave the range of single precision though the formula's do not:
+against 64 bits."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF_ULP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def layer():
+    from paper_2505_23949_amd import layer as module
+
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return module
+
+
+def rand(gen, *shape):
+    return torch.randn(*shape, generator=gen, dtype=torch.float64)
+
+
+# ---- norm ---------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size,eps", [(1e15, 1e-5), (1e17, 1e-5), (1e-14, 0.0), (1e-17, 0.0)])
+@pytest.mark.parametrize("rows,cols", [(5, 300), (3, 4096), (2, 16000), (3, 17000)])
+def test_norm_backward_of_large_and_small_rows(layer, rows, cols, size, eps, dtype):
+    gen = torch.Generator().manual_seed(rows + cols)
+    unit = rand(gen, rows, cols)
+    h = (size * unit).to(DTYPES[dtype]).cuda()
+    dy = (unit + 0.5 * rand(gen, rows, cols)).to(DTYPES[dtype]).cuda()      # (along h, so that the second term is as large as the first)
+    gain = (1 + 0.3 * rand(gen, cols)).float().cuda()
+    dh, dgain = torch.empty_like(h), torch.empty(cols, device="cuda")
+    p = layer.make_norm_backward(h, gain, eps, dy, dh=dh, dgain=dgain)
+    layer.tsenor_norm_backward(p, torch.empty(layer.tsenor_norm_backward_workspace_bytes(p), dtype=torch.uint8, device="cuda"))
+    x, g, d = h.cpu().double(), gain.cpu().double(), dy.cpu().double()
+    c = 1.0 / torch.sqrt(x.square().mean(1, keepdim=True) + eps)
+    a = g * d
+    want = c * a - x * c ** 3 * (a * x).mean(1, keepdim=True)
+    # rounding errors as at any other size: 2^-24 of the sizes of the terms for each of the additions in a row and the few products
+    terms = c * a.abs() + x.abs() * c ** 3 * (a * x).abs().mean(1, keepdim=True)
+    near = 2.0 ** -24 * (cols / 512 + 41) * terms
+    assert ((dh.cpu().double() - want).abs() <= near + HALF_ULP[dtype] * want.abs() * 1.01).all()
+    sizes = (d * x * c).abs().sum(0)
+    assert ((dgain.cpu().double() - (d * x * c).sum(0)).abs() <= 2.0 ** -24 * (rows / 16 + cols / 512 + 60) * sizes).all()
