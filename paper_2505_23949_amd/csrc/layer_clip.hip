@@ -3,11 +3,13 @@
 // A tensor is cut into chunks of 4096 elements; the chunks of up to kMaxTensors tensors share a launch, whose table is a kernel
 // argument, and workgroups take every gridDim.x-th of them, so that what is read at a time lies together.  In the first pass each
 // leaves one sum of squares in double, and each of the second adds all of those in the same order before it scales: no
-// atomics, nothing to clear, and no launch between the two.  Bound by memory.  The second pass goes through the chunks from the
-// last to the first, what the first one read last being still in the cache of the memory side (2 % for a layer of 436 MB), and
-// its accesses are marked as the last ones to what they touch, so that results do not drive out what is still to be read: the
-// gradients of a layer of 4096 (218 M in bf16) 210-215 us, 243 without the mark.  (8 or 4 vectors in flight and half as many
-// workgroups: 241, 227.)
+// atomics, nothing to clear, and no launch between the two.  Workgroups of one number share a sum over all launches, so that what a
+// workgroup adds does not grow with the tensors (4000 of 50 000 floats: 0.78 ms, 1.90 with sums of their own for each launch).
+//
+// Bound by memory.  The second pass goes through the chunks from the last to the first, what the first one read last being still
+// in the cache of the memory side (2 % for a layer of 436 MB), and its accesses are marked as the last ones to what they touch, so
+// that results do not drive out what is still to be read: the gradients of a layer of 4096 (218 M in bf16) 210-215 us, 243 without
+// the mark.  (8 or 4 vectors in flight and half as many workgroups: 241, 227.)
 #include <algorithm>
 
 #include "layer.hpp"
@@ -132,7 +134,8 @@ __device__ __forceinline__ double group_sum(double s) {
   return part[0] + part[1] + part[2] + part[3];
 }
 
-__global__ __launch_bounds__(kThreads) void squares_kernel(ClipTable table, double* sums) {
+// (the first `begun` sums hold what earlier launches found)
+__global__ __launch_bounds__(kThreads) void squares_kernel(ClipTable table, double* sums, unsigned begun) {
   double s = 0.0;
   const uint32_t chunks = table.first[table.count];
   int k = tensor_of(table, blockIdx.x);
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(kThreads) void squares_kernel(ClipTable table, doub
       s = c.bf16 ? add_squares<true>(c.in, c.size, s) : add_squares<false>(c.in, c.size, s);
   }
   s = group_sum(s);
-  if (threadIdx.x == 0) sums[blockIdx.x] = s;
+  if (threadIdx.x == 0) sums[blockIdx.x] = blockIdx.x < begun ? sums[blockIdx.x] + s : s;
 }
 
 __global__ __launch_bounds__(kThreads) void scale_kernel(ClipTable table, const double* sums, int count, double max_norm, float* norm_out) {
@@ -215,12 +218,12 @@ inline unsigned groups_of(const ClipTable& table) { return std::min<unsigned>(ta
 
 extern "C" size_t tsenor_clip_workspace_bytes(const tsenor_clip_problem* p) {
   if (check(p) != TSENOR_OK) return 0;
-  // (as many launches as tensors at most, each with at least one tensor; 256 bytes where there is none)
+  // (a sum for each workgroup of the largest launch; 256 bytes where there is none)
   ClipTable table;
   size_t sums = 0;
   for (int k = 0; k < p->count;) {
     k = fill_table(*p, k, table);
-    sums += groups_of(table);
+    sums = std::max<size_t>(sums, groups_of(table));
   }
   return std::max<size_t>(256, (sums * sizeof(double) + 255) / 256 * 256);
 }
@@ -232,13 +235,13 @@ extern "C" int tsenor_clip(const tsenor_clip_problem* p, void* workspace, size_t
   hipStream_t s = static_cast<hipStream_t>(stream);
   double* sums = static_cast<double*>(workspace);
   ClipTable table;
-  int count = 0;
+  unsigned count = 0;
   for (int k = 0; k < p->count;) {
     k = fill_table(*p, k, table);
     const unsigned groups = groups_of(table);
     if (groups == 0) continue;
-    squares_kernel<<<groups, kThreads, 0, s>>>(table, sums + count);
-    count += (int)groups;
+    squares_kernel<<<groups, kThreads, 0, s>>>(table, sums, count);
+    count = std::max(count, groups);
   }
   // norm and factor are written by the first launch of the second pass, which there is also without gradients
   float* norm_out = p->norm_out;
@@ -246,7 +249,7 @@ extern "C" int tsenor_clip(const tsenor_clip_problem* p, void* workspace, size_t
     k = fill_table(*p, k, table);
     const unsigned groups = groups_of(table);
     if (groups == 0 && (!norm_out || k < p->count)) continue;
-    scale_kernel<<<std::max(groups, 1u), kThreads, 0, s>>>(table, sums, count, p->max_norm, norm_out);
+    scale_kernel<<<std::max(groups, 1u), kThreads, 0, s>>>(table, sums, (int)count, p->max_norm, norm_out);
     norm_out = nullptr;
   }
   return status_of_launches();

@@ -1,5 +1,7 @@
-"""The layer operators where intermediate results could leave the range of single precision though the formula's do not:
-against 64 bits."""
+"""The layer operators where intermediate results could leave the range of single precision though the formula's do not, and with more
+tensors than a launch of clipping takes: against 64 bits."""
+import math
+
 import pytest
 import torch
 
@@ -45,3 +47,29 @@ def test_norm_backward_of_large_and_small_rows(layer, rows, cols, size, eps, dty
     assert ((dh.cpu().double() - want).abs() <= near + HALF_ULP[dtype] * want.abs() * 1.01).all()
     sizes = (d * x * c).abs().sum(0)
     assert ((dgain.cpu().double() - (d * x * c).sum(0)).abs() <= 2.0 ** -24 * (rows / 16 + cols / 512 + 60) * sizes).all()
+
+
+# ---- clipping -----------------------------------------------------------------------------------------------------------
+
+def clip(layer, grads, largest):
+    norm = torch.empty(2, device="cuda")
+    p = layer.make_clip(grads, largest, norm_out=norm)
+    layer.tsenor_clip(p, torch.empty(layer.tsenor_clip_workspace_bytes(p), dtype=torch.uint8, device="cuda").fill_(255))
+    return norm.cpu().double()
+
+
+def test_clip_of_many_tensors_in_launches_of_all_sizes(layer):
+    # launches of few and of many chunks in turn, so that the later ones add to the sums of some workgroups and begin those of others
+    gen = torch.Generator("cuda").manual_seed(2)
+    sizes = [7] * 250 + [5_000_000, 4097] + [3] * 500 + [9_000_001] * 2 + [64] * 181 + [4096] * 1000
+    grads = [torch.randn(n, device="cuda", generator=gen).to(torch.bfloat16 if k % 3 else torch.float32) for k, n in enumerate(sizes)]
+    before = [g.clone() for g in grads]
+    norm = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    got = clip(layer, grads, 0.25 * norm)
+    assert abs(got[0] - norm) <= 1e-7 * norm and abs(got[1] - 0.25) <= 1e-7
+    factor = float(got[1])
+    for g, b in zip(grads, before):
+        assert torch.equal(g, (b.float() * factor).to(g.dtype))
+    # the same bits again
+    again = [b.clone() for b in before]
+    assert torch.equal(clip(layer, again, 0.25 * norm), got)
