@@ -16,9 +16,9 @@
  * workspace, and every call can be captured in a HIP graph.  Besides:
  *   - rows, columns and counts may be zero (no tokens this time): outputs that have elements are still written, and pointers to
  *     matrices without elements may be NULL.
- *   - Matrices have at most 2^31 - 256 rows, 2^24 columns and 2^23 - 1 tiles of 128 x 128, else TSENOR_ERR_SHAPE.  Rows need
- *     not be aligned (matrices whose rows all begin at multiples of 16 bytes are read and written faster); scaled matrices
- *     have to be, see below.
+ *   - Matrices have at most 2^31 - 256 rows, 2^24 columns, 2^23 - 1 tiles of 128 x 128 and a leading dimension of at most 2^40 (times
+ *     the rows 2^60), else TSENOR_ERR_SHAPE.  Rows need not be aligned (matrices whose rows all begin at multiples of 16 bytes are
+ *     read and written faster); scaled matrices have to be, see below.
  *   - A misaligned pointer or leading dimension is TSENOR_ERR_ALIGN (pointers: to their elements, workspaces to 256 bytes).
  *   - Results do not depend on what else runs, nor on earlier calls: sums have a fixed order, and there are no atomics.
  *   - Infinities and NaN are inputs like others.

@@ -26,11 +26,12 @@ constexpr int64_t kMaxRows = INT32_MAX - 255;
 inline bool shape_ok(int64_t rows, int64_t cols) {
   return rows >= 0 && rows <= kMaxRows && cols >= 0 && cols <= (int64_t)1 << 24 && blocks_of(rows) * blocks_of(cols) < (int64_t)1 << 23;
 }
-constexpr int64_t kMaxLd = (int64_t)1 << 40;  // (products with a row number stay far below 2^63 + bytes per element)
-inline bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld <= kMaxLd; }
+// (the offset of every row, in elements, is below 2^60: bytes have 63 bits)
+constexpr int64_t kMaxLd = (int64_t)1 << 40, kMaxElements = (int64_t)1 << 60;
+inline bool ld_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= cols && ld <= kMaxLd && (rows == 0 || ld <= kMaxElements / rows); }
 inline int check_scaled(const tsenor_scaled& s) {
   if (s.rows != 0 && s.cols != 0 && (!s.values || !s.scales)) return TSENOR_ERR_NULL;
-  if (!shape_ok(s.rows, s.cols) || !ld_ok(s.ld, s.cols) || !ld_ok(s.scale_ld, s.rows)) return TSENOR_ERR_SHAPE;
+  if (!shape_ok(s.rows, s.cols) || !ld_ok(s.ld, s.rows, s.cols) || !ld_ok(s.scale_ld, blocks_of(s.cols), s.rows)) return TSENOR_ERR_SHAPE;
   if (s.ld < blocks_of(s.cols) * kBlock) return TSENOR_ERR_SHAPE;
   if (!aligned_to(s.values, 16) || !aligned_to(s.scales, 16) || s.ld % kBlock || s.scale_ld % 16) return TSENOR_ERR_ALIGN;
   return TSENOR_OK;

@@ -329,7 +329,9 @@ int check(const tsenor_norm_problem* p) {
   if (!p) return TSENOR_ERR_NULL;
   if (p->rows != 0 && p->cols != 0 && (!p->x || !p->gain || (!p->sum_out && !p->y_out && !p->out.values))) return TSENOR_ERR_NULL;
   if (!known(p->dtype) || !known(p->gain_dtype)) return TSENOR_ERR_UNSUPPORTED;
-  if (!shape_ok(p->rows, p->cols) || !ld_ok(p->ld, p->cols) || (p->residual && !ld_ok(p->residual_ld, p->cols))) return TSENOR_ERR_SHAPE;
+  if (!shape_ok(p->rows, p->cols) || !ld_ok(p->ld, p->rows, p->cols) ||
+      (p->residual && !ld_ok(p->residual_ld, p->rows, p->cols)))
+    return TSENOR_ERR_SHAPE;
   if (!(p->eps >= 0.0) || !std::isfinite((float)p->eps)) return TSENOR_ERR_PARAM;
   const size_t e = size_of(p->dtype);
   if (!aligned_to(p->x, e) || !aligned_to(p->residual, e) || !aligned_to(p->sum_out, e) || !aligned_to(p->y_out, e) ||
@@ -344,7 +346,8 @@ int check(const tsenor_norm_backward_problem* p) {
   if (!p) return TSENOR_ERR_NULL;
   if (p->cols != 0 && (!p->gain || !p->dgain_out || (p->rows != 0 && (!p->h || !p->dy || !p->dh_out)))) return TSENOR_ERR_NULL;
   if (!known(p->dtype) || !known(p->gain_dtype)) return TSENOR_ERR_UNSUPPORTED;
-  if (!shape_ok(p->rows, p->cols) || !ld_ok(p->ld, p->cols) || !ld_ok(p->dy_ld, p->cols) || (p->dsum && !ld_ok(p->dsum_ld, p->cols)))
+  if (!shape_ok(p->rows, p->cols) || !ld_ok(p->ld, p->rows, p->cols) || !ld_ok(p->dy_ld, p->rows, p->cols) ||
+      (p->dsum && !ld_ok(p->dsum_ld, p->rows, p->cols)))
     return TSENOR_ERR_SHAPE;
   if (!(p->eps >= 0.0) || !std::isfinite((float)p->eps)) return TSENOR_ERR_PARAM;
   const size_t e = size_of(p->dtype);

@@ -426,7 +426,7 @@ int check(const tsenor_product_problem* p) {
   if (rc != TSENOR_OK) return rc;
   rc = check_scaled(p->b);
   if (rc != TSENOR_OK) return rc;
-  if (p->a.cols != p->b.cols || p->b.rows > (int64_t)1 << 24 || !ld_ok(p->out_ld, p->b.rows) || !shape_ok(p->a.rows, p->b.rows))
+  if (p->a.cols != p->b.cols || p->b.rows > (int64_t)1 << 24 || !shape_ok(p->a.rows, p->b.rows) || !ld_ok(p->out_ld, p->a.rows, p->b.rows))
     return TSENOR_ERR_SHAPE;
   const int64_t blocks = blocks_of(p->a.cols);
   for (const tsenor_scaled* s : {&p->a, &p->b})

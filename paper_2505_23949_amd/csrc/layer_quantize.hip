@@ -179,7 +179,7 @@ int check(const tsenor_quantize_problem* p) {
   if (!p) return TSENOR_ERR_NULL;
   if (p->rows != 0 && p->cols != 0 && (!p->x || (!p->out.values && !p->out_t.values))) return TSENOR_ERR_NULL;
   if (!known(p->dtype) || (p->square != 0 && p->square != 1)) return TSENOR_ERR_UNSUPPORTED;
-  if (!shape_ok(p->rows, p->cols) || !ld_ok(p->ld, p->cols)) return TSENOR_ERR_SHAPE;
+  if (!shape_ok(p->rows, p->cols) || !ld_ok(p->ld, p->rows, p->cols)) return TSENOR_ERR_SHAPE;
   if (p->out_t.values && p->rows > (int64_t)1 << 24) return TSENOR_ERR_SHAPE;
   if (!aligned_to(p->x, size_of(p->dtype))) return TSENOR_ERR_ALIGN;
   if (p->out.values) {
