@@ -46,7 +46,8 @@ class MaskedLayer:
         layer.tsenor_quantize(self._quantize_weights)
 
     def forward(self, x, residual=None, *, training: bool = False):
-        """(out, h): the layer's output and the residual stream behind the addition (x itself without residual)."""
+        """(out, h): the layer's output and the residual stream behind the addition (x itself without residual).  A training pass
+        keeps h and the norm's output for ``backward``, in the place of the last one's; other passes leave them alone."""
         import torch
 
         tokens, cols = x.shape
@@ -56,17 +57,22 @@ class MaskedLayer:
         layer.tsenor_norm(layer.make_norm(x, self.gain, self.eps, residual=residual, out=y8, y_out=y, sum_out=None if residual is None else h))
         out = torch.empty((tokens, self.weight.shape[0]), dtype=torch.bfloat16, device=x.device)
         self._product(y8, self.weights8, out)
-        self._kept = (h, y) if training else None
+        if training:
+            self._kept = (h, y)
         return out, h
 
     def backward(self, dout, dsum=None):
         """dL/dh of the last training forward pass (the gradient of x and of the residual alike), from dL/dout and what reaches h
-        past this layer; leaves ``dweight`` and ``dgain``."""
+        past this layer; writes ``dweight`` and ``dgain`` (they are not added to)."""
         import torch
 
+        if self._kept is None:
+            raise RuntimeError("backward needs a forward pass with training=True before it")
         h, y = self._kept
         tokens, cols = h.shape
         rows = self.weight.shape[0]
+        if dout.shape != (tokens, rows):
+            raise ValueError(f"dout must be {tokens} x {rows}, as the output of the last training pass")
         d8, d8_t = layer.empty_scaled(tokens, rows, h.device), layer.empty_scaled(rows, tokens, h.device)
         y8_t = layer.empty_scaled(cols, tokens, h.device)
         layer.tsenor_quantize(layer.make_quantize(dout, out=d8, out_t=d8_t))

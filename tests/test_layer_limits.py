@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 
 @pytest.fixture(scope="module")
@@ -49,3 +50,12 @@ def test_rows_too_far_apart_to_address(lib):
         f = getattr(lib, name)
         scratch = (ctypes.c_void_p(0x100000), 1 << 40) if len(f.argtypes) == 4 else ()
         assert f(ctypes.byref(p), *scratch, None) == b.TSENOR_ERR_SHAPE, name
+
+
+def test_backward_without_a_training_pass():
+    from paper_2505_23949_amd.masked_layer import MaskedLayer
+
+    one = MaskedLayer.__new__(MaskedLayer)
+    one._kept = None
+    with pytest.raises(RuntimeError, match="training"):
+        one.backward(torch.zeros(4, 4))
