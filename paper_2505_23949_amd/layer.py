@@ -2,7 +2,8 @@
 floating point, root-mean-square norm, 8-bit product, gradient clipping.
 
 As in ``binding``: argument marshalling only, ``make_*`` describes a call once (no copies; the tensors must outlive it), the
-function named like the C entry point enqueues it on the current stream as often as wanted.
+function named like the C entry point enqueues it as often as wanted, on the current stream of the GPU that the tensors are on
+(on ``stream`` if given, which has to be one of that GPU).
 """
 from __future__ import annotations
 
@@ -10,7 +11,7 @@ import ctypes
 from dataclasses import dataclass
 from typing import Any
 
-from .binding import TSENOR_BF16, TSENOR_F32, TSENOR_OK, TsenorError, _stream_handle, load
+from .binding import TSENOR_BF16, TSENOR_F32, TSENOR_OK, TsenorError, current_device, current_stream, load
 
 TSENOR_SCALE_BLOCK = 128
 
@@ -26,7 +27,11 @@ class tsenor_scaled(ctypes.Structure):
     ]
 
 
-class tsenor_quantize_problem(ctypes.Structure):
+class _Problem(ctypes.Structure):
+    device = None  # GPU of the tensors: make_* knows it (None, of a struct filled by hand: the current one)
+
+
+class tsenor_quantize_problem(_Problem):
     _fields_ = [
         ("x", ctypes.c_void_p),
         ("dtype", ctypes.c_int32),
@@ -40,7 +45,7 @@ class tsenor_quantize_problem(ctypes.Structure):
     ]
 
 
-class tsenor_norm_problem(ctypes.Structure):
+class tsenor_norm_problem(_Problem):
     _fields_ = [
         ("x", ctypes.c_void_p),
         ("residual", ctypes.c_void_p),
@@ -58,7 +63,7 @@ class tsenor_norm_problem(ctypes.Structure):
     ]
 
 
-class tsenor_norm_backward_problem(ctypes.Structure):
+class tsenor_norm_backward_problem(_Problem):
     _fields_ = [
         ("h", ctypes.c_void_p),
         ("gain", ctypes.c_void_p),
@@ -77,7 +82,7 @@ class tsenor_norm_backward_problem(ctypes.Structure):
     ]
 
 
-class tsenor_product_problem(ctypes.Structure):
+class tsenor_product_problem(_Problem):
     _fields_ = [
         ("a", tsenor_scaled),
         ("b", tsenor_scaled),
@@ -96,7 +101,7 @@ class tsenor_gradient(ctypes.Structure):
     ]
 
 
-class tsenor_clip_problem(ctypes.Structure):
+class tsenor_clip_problem(_Problem):
     _fields_ = [
         ("gradients", ctypes.POINTER(tsenor_gradient)),
         ("count", ctypes.c_int32),
@@ -219,10 +224,11 @@ def _mask(mask, shape) -> None:
         raise ValueError("mask must be a contiguous uint8 or bool matrix of the shape it applies to")
 
 
-def _one_device(**tensors) -> None:
+def _one_device(**tensors) -> int:
     where = {name: t.device for name, t in tensors.items() if t is not None}
     if any(d.type != "cuda" for d in where.values()) or len(set(where.values())) > 1:
         raise ValueError(f"all tensors must be on one GPU, got {where}")
+    return next(iter(where.values())).index
 
 
 def make_quantize(x, *, out: ScaledMatrix | None = None, out_t: ScaledMatrix | None = None, mask=None,
@@ -231,13 +237,14 @@ def make_quantize(x, *, out: ScaledMatrix | None = None, out_t: ScaledMatrix | N
     _matrix(x, "x")
     if mask is not None:
         _mask(mask, x.shape)
-    _one_device(x=x, mask=mask, out=out and out.values, out_t=out_t and out_t.values)
+    device = _one_device(x=x, mask=mask, out=out and out.values, out_t=out_t and out_t.values)
     p = tsenor_quantize_problem(x=x.data_ptr(), dtype=_code(x, "x"), square=int(square), rows=x.shape[0], cols=x.shape[1], ld=_ld(x),
                                 mask=None if mask is None else mask.data_ptr())
     if out is not None:
         p.out = out.struct()
     if out_t is not None:
         p.out_t = out_t.struct()
+    p.device = device
     return p
 
 
@@ -251,7 +258,7 @@ def make_norm(x, gain, eps: float, *, residual=None, out: ScaledMatrix | None = 
     for t, name in ((sum_out, "sum_out"), (y_out, "y_out")):
         if t is not None:
             _whole(t, name, x)
-    _one_device(x=x, gain=gain, residual=residual, sum_out=sum_out, y_out=y_out, out=out and out.values)
+    device = _one_device(x=x, gain=gain, residual=residual, sum_out=sum_out, y_out=y_out, out=out and out.values)
     p = tsenor_norm_problem(x=x.data_ptr(), gain=gain.data_ptr(), dtype=_code(x, "x"), gain_dtype=_code(gain, "gain"),
                             rows=x.shape[0], cols=x.shape[1], ld=_ld(x), eps=float(eps))
     if residual is not None:
@@ -260,6 +267,7 @@ def make_norm(x, gain, eps: float, *, residual=None, out: ScaledMatrix | None = 
     p.y_out = None if y_out is None else y_out.data_ptr()
     if out is not None:
         p.out = out.struct()
+    p.device = device
     return p
 
 
@@ -277,12 +285,13 @@ def make_norm_backward(h, gain, eps: float, dy, *, dh, dgain, dsum=None) -> tsen
     _whole(dh, "dh", h)
     if dsum is not None:
         _matrix(dsum, "dsum", h)
-    _one_device(h=h, gain=gain, dy=dy, dh=dh, dgain=dgain, dsum=dsum)
+    device = _one_device(h=h, gain=gain, dy=dy, dh=dh, dgain=dgain, dsum=dsum)
     p = tsenor_norm_backward_problem(h=h.data_ptr(), gain=gain.data_ptr(), dy=dy.data_ptr(), dtype=_code(h, "h"),
                                      gain_dtype=_code(gain, "gain"), rows=h.shape[0], cols=h.shape[1], ld=_ld(h), dy_ld=_ld(dy),
                                      eps=float(eps), dh_out=dh.data_ptr(), dgain_out=dgain.data_ptr())
     if dsum is not None:
         p.dsum, p.dsum_ld = dsum.data_ptr(), _ld(dsum)
+    p.device = device
     return p
 
 
@@ -297,9 +306,11 @@ def make_product(a: ScaledMatrix, b: ScaledMatrix, *, out, mask=None) -> tsenor_
         raise ValueError("a and b must have the same number of columns")
     if mask is not None:
         _mask(mask, out.shape)
-    _one_device(a=a.values, a_scales=a.scales, b=b.values, b_scales=b.scales, out=out, mask=mask)
-    return tsenor_product_problem(a=a.struct(), b=b.struct(), out=out.data_ptr(), out_ld=_ld(out),
-                                  mask=None if mask is None else mask.data_ptr())
+    device = _one_device(a=a.values, a_scales=a.scales, b=b.values, b_scales=b.scales, out=out, mask=mask)
+    p = tsenor_product_problem(a=a.struct(), b=b.struct(), out=out.data_ptr(), out_ld=_ld(out),
+                               mask=None if mask is None else mask.data_ptr())
+    p.device = device
+    return p
 
 
 def make_clip(gradients, max_norm: float, *, norm_out, out=None) -> tsenor_clip_problem:
@@ -318,26 +329,41 @@ def make_clip(gradients, max_norm: float, *, norm_out, out=None) -> tsenor_clip_
             raise ValueError("gradients and out must be contiguous, with the same elements and dtypes")
         _one_device(gradient=g, out=o, norm_out=norm_out)
         table[k] = tsenor_gradient(g.data_ptr(), o.data_ptr(), g.numel(), _code(g, "gradient"))
-    return tsenor_clip_problem(gradients=table, count=len(gradients), max_norm=float(max_norm), norm_out=norm_out.data_ptr())
+    p = tsenor_clip_problem(gradients=table, count=len(gradients), max_norm=float(max_norm), norm_out=norm_out.data_ptr())
+    p.device = _one_device(norm_out=norm_out)
+    return p
 
 
 # ---- the calls ------------------------------------------------------------------------------------------------------------
 
-def _check(rc: int, where: str) -> None:
+def _enqueue(name: str, problem, stream, *scratch) -> None:
+    here = current_device()
+    device = here if problem.device is None else problem.device
+    if device != here:  # a launch goes to the current GPU
+        import torch
+
+        with torch.cuda.device(device):
+            _enqueue(name, problem, stream, *scratch)
+        return
+    rc = getattr(load(), name)(ctypes.byref(problem), *scratch, current_stream(device) if stream is None else stream.cuda_stream)
     if rc != TSENOR_OK:
-        raise TsenorError(rc, where)
+        raise TsenorError(rc, name)
 
 
-def _scratch(workspace):
-    return (None, 0) if workspace is None else (ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size())
+def _scratch(workspace, problem):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous() or workspace.get_device() != (current_device() if problem.device is None else problem.device):
+        raise ValueError("workspace must be contiguous and on the GPU of the tensors")
+    return ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size()
 
 
 def tsenor_quantize(problem: tsenor_quantize_problem, stream=None) -> None:
-    _check(load().tsenor_quantize(ctypes.byref(problem), _stream_handle(stream)), "tsenor_quantize")
+    _enqueue("tsenor_quantize", problem, stream)
 
 
 def tsenor_norm(problem: tsenor_norm_problem, stream=None) -> None:
-    _check(load().tsenor_norm(ctypes.byref(problem), _stream_handle(stream)), "tsenor_norm")
+    _enqueue("tsenor_norm", problem, stream)
 
 
 def tsenor_norm_backward_workspace_bytes(problem: tsenor_norm_backward_problem) -> int:
@@ -345,7 +371,7 @@ def tsenor_norm_backward_workspace_bytes(problem: tsenor_norm_backward_problem) 
 
 
 def tsenor_norm_backward(problem: tsenor_norm_backward_problem, workspace=None, stream=None) -> None:
-    _check(load().tsenor_norm_backward(ctypes.byref(problem), *_scratch(workspace), _stream_handle(stream)), "tsenor_norm_backward")
+    _enqueue("tsenor_norm_backward", problem, stream, *_scratch(workspace, problem))
 
 
 def tsenor_product_workspace_bytes(problem: tsenor_product_problem) -> int:
@@ -353,7 +379,7 @@ def tsenor_product_workspace_bytes(problem: tsenor_product_problem) -> int:
 
 
 def tsenor_product(problem: tsenor_product_problem, workspace=None, stream=None) -> None:
-    _check(load().tsenor_product(ctypes.byref(problem), *_scratch(workspace), _stream_handle(stream)), "tsenor_product")
+    _enqueue("tsenor_product", problem, stream, *_scratch(workspace, problem))
 
 
 def tsenor_clip_workspace_bytes(problem: tsenor_clip_problem) -> int:
@@ -361,4 +387,4 @@ def tsenor_clip_workspace_bytes(problem: tsenor_clip_problem) -> int:
 
 
 def tsenor_clip(problem: tsenor_clip_problem, workspace, stream=None) -> None:
-    _check(load().tsenor_clip(ctypes.byref(problem), *_scratch(workspace), _stream_handle(stream)), "tsenor_clip")
+    _enqueue("tsenor_clip", problem, stream, *_scratch(workspace, problem))

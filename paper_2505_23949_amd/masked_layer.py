@@ -30,7 +30,8 @@ class MaskedLayer:
         import torch
 
         self.weight, self.gain, self.eps = weight, gain, eps
-        self.mask = binding.solve(weight, N, M, tau, iters, col_scale=col_scale, tau_mode=binding.TSENOR_TAU_REL_MATRIX_MAX)["mask"]
+        with torch.cuda.device(weight.device):  # (the mask finder goes to the current GPU)
+            self.mask = binding.solve(weight, N, M, tau, iters, col_scale=col_scale, tau_mode=binding.TSENOR_TAU_REL_MATRIX_MAX)["mask"]
         rows, cols = weight.shape
         device = weight.device
         self.weights8 = layer.empty_scaled(rows, cols, device)

@@ -59,3 +59,93 @@ def test_backward_without_a_training_pass():
     one._kept = None
     with pytest.raises(RuntimeError, match="training"):
         one.backward(torch.zeros(4, 4))
+
+
+class FakeCuda:
+    """Two GPUs as the binding sees them: the current one, its stream, and a library that notes what was current at each call."""
+
+    def __init__(self, monkeypatch):
+        from paper_2505_23949_amd import binding, layer
+
+        self.current, self.calls = 0, []
+        fake = self
+
+        class Guard:
+            def __init__(self, device):
+                self.device = torch.device(device).index if isinstance(device, (str, torch.device)) else device
+
+            def __enter__(self):
+                self.before, fake.current = fake.current, self.device
+
+            def __exit__(self, *_):
+                fake.current = self.before
+
+        class Library:
+            def __getattr__(self, name):
+                def call(problem, *rest):
+                    fake.calls.append((name, fake.current, rest[-1]))
+                    return 0
+                return call
+
+        monkeypatch.setattr(torch.cuda, "device", Guard)
+        monkeypatch.setattr(torch.cuda, "init", lambda: None)
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: fake.current, raising=False)
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
+        for name in ("_current_device", "_raw_stream"):
+            monkeypatch.setattr(binding, name, None)
+        monkeypatch.setattr(layer, "load", lambda: Library())
+
+
+class OnDevice:
+    """A workspace on a GPU."""
+
+    def __init__(self, index):
+        self.index = index
+
+    def get_device(self):
+        return self.index
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x100000
+
+    def numel(self):
+        return 4096
+
+    def element_size(self):
+        return 1
+
+
+def test_calls_go_to_the_gpu_of_their_tensors(monkeypatch):
+    from paper_2505_23949_amd import layer as l
+
+    fake = FakeCuda(monkeypatch)
+    monkeypatch.setattr(l, "_one_device", lambda **_: 1)
+    x, bf16 = torch.zeros(4, 256), torch.zeros(4, 4).bfloat16()
+    q, norm = l.empty_scaled(4, 256, "cpu"), torch.zeros(2)
+    gain = torch.zeros(256)
+    calls = [(l.tsenor_quantize, l.make_quantize(x, out=q)), (l.tsenor_norm, l.make_norm(x, gain, 1e-5, out=q)),
+             (l.tsenor_norm_backward, l.make_norm_backward(x, gain, 1e-5, x, dh=x.clone(), dgain=gain.clone())),
+             (l.tsenor_product, l.make_product(q, q, out=bf16)), (l.tsenor_clip, l.make_clip([x], 1.0, norm_out=norm))]
+    for current in (0, 1):
+        fake.current = current
+        for call, p in calls:
+            call(p, *(() if call in (l.tsenor_quantize, l.tsenor_norm) else (OnDevice(1),)))
+            assert fake.calls[-1] == (call.__name__, 1, 101) and fake.current == current
+    # a problem that was filled by hand goes to the current one
+    fake.current = 0
+    l.tsenor_quantize(l.tsenor_quantize_problem())
+    assert fake.calls[-1] == ("tsenor_quantize", 0, 100)
+
+
+def test_workspaces_elsewhere_are_refused(monkeypatch):
+    from paper_2505_23949_amd import layer as l
+
+    FakeCuda(monkeypatch)
+    monkeypatch.setattr(l, "_one_device", lambda **_: 0)
+    p = l.make_clip([torch.zeros(4)], 1.0, norm_out=torch.zeros(2))
+    for workspace in (torch.zeros(4096, dtype=torch.uint8), OnDevice(1)):      # in host memory, and on another GPU
+        with pytest.raises(ValueError, match="workspace"):
+            l.tsenor_clip(p, workspace)
