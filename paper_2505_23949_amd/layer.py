@@ -217,6 +217,12 @@ def _whole(t, name: str, like) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
+def _scaled(q, name: str, rows: int, cols: int) -> None:
+    # (one without elements would have no address, which stands for "not wanted")
+    if q is not None and (q.rows, q.cols) != (rows, cols):
+        raise ValueError(f"{name} must be a scaled matrix of {rows} x {cols}")
+
+
 def _mask(mask, shape) -> None:
     import torch
 
@@ -237,6 +243,8 @@ def make_quantize(x, *, out: ScaledMatrix | None = None, out_t: ScaledMatrix | N
     _matrix(x, "x")
     if mask is not None:
         _mask(mask, x.shape)
+    _scaled(out, "out", x.shape[0], x.shape[1])
+    _scaled(out_t, "out_t", x.shape[1], x.shape[0])
     device = _one_device(x=x, mask=mask, out=out and out.values, out_t=out_t and out_t.values)
     p = tsenor_quantize_problem(x=x.data_ptr(), dtype=_code(x, "x"), square=int(square), rows=x.shape[0], cols=x.shape[1], ld=_ld(x),
                                 mask=None if mask is None else mask.data_ptr())
@@ -258,6 +266,7 @@ def make_norm(x, gain, eps: float, *, residual=None, out: ScaledMatrix | None = 
     for t, name in ((sum_out, "sum_out"), (y_out, "y_out")):
         if t is not None:
             _whole(t, name, x)
+    _scaled(out, "out", x.shape[0], x.shape[1])
     device = _one_device(x=x, gain=gain, residual=residual, sum_out=sum_out, y_out=y_out, out=out and out.values)
     p = tsenor_norm_problem(x=x.data_ptr(), gain=gain.data_ptr(), dtype=_code(x, "x"), gain_dtype=_code(gain, "gain"),
                             rows=x.shape[0], cols=x.shape[1], ld=_ld(x), eps=float(eps))

@@ -61,6 +61,20 @@ def test_backward_without_a_training_pass():
         one.backward(torch.zeros(4, 4))
 
 
+def test_a_matrix_of_another_shape_is_not_one_that_is_not_wanted():
+    from paper_2505_23949_amd import layer as l
+
+    # (memory without elements has no address, which stands for "not wanted" in C)
+    x = torch.zeros(4, 256)
+    for one in (l.empty_scaled(0, 256, "cpu"), l.empty_scaled(4, 128, "cpu")):
+        with pytest.raises(ValueError, match="out must be a scaled matrix of 4 x 256"):
+            l.make_quantize(x, out=one)
+        with pytest.raises(ValueError, match="out must be a scaled matrix of 4 x 256"):
+            l.make_norm(x, torch.zeros(256), 1e-5, out=one, y_out=torch.zeros(4, 256))
+    with pytest.raises(ValueError, match="out_t must be a scaled matrix of 256 x 4"):
+        l.make_quantize(x, out=l.empty_scaled(4, 256, "cpu"), out_t=l.empty_scaled(0, 4, "cpu"))
+
+
 class FakeCuda:
     """Two GPUs as the binding sees them: the current one, its stream, and a library that notes what was current at each call."""
 
