@@ -145,9 +145,8 @@ class ScaledMatrix:
         """The values that the matrix stands for, float32 (a convenience of torch operations, for checks)."""
         import torch
 
-        wide = self.values[:, :self.cols].float()
-        exponent = self.scales[:, :self.rows].view(torch.uint8).t().to(torch.int32) - 127
-        return torch.ldexp(wide, exponent.repeat_interleave(TSENOR_SCALE_BLOCK, 1)[:, :self.cols])
+        scales = self.scales[:, :self.rows].view(torch.float8_e8m0fnu).float().t()
+        return self.values[:, :self.cols].float() * scales.repeat_interleave(TSENOR_SCALE_BLOCK, 1)[:, :self.cols]
 
 
 def _round_up(n: int, to: int) -> int:

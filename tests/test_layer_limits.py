@@ -75,6 +75,16 @@ def test_a_matrix_of_another_shape_is_not_one_that_is_not_wanted():
         l.make_quantize(x, out=l.empty_scaled(4, 256, "cpu"), out_t=l.empty_scaled(0, 4, "cpu"))
 
 
+def test_what_a_scale_byte_stands_for():
+    from paper_2505_23949_amd import layer as l
+
+    values = torch.full((4, 128), 1.5).to(torch.float8_e4m3fn)
+    scales = torch.tensor([[0, 1, 254, 255] + [127] * 12], dtype=torch.uint8)
+    wide = l.scaled_matrix(values, scales, 128).dequantize()
+    assert (wide[0] == 1.5 * 2.0 ** -127).all() and (wide[1] == 1.5 * 2.0 ** -126).all() and (wide[2] == 1.5 * 2.0 ** 127).all()
+    assert torch.isnan(wide[3]).all()
+
+
 class FakeCuda:
     """Two GPUs as the binding sees them: the current one, its stream, and a library that notes what was current at each call."""
 
