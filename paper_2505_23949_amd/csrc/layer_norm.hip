@@ -66,13 +66,18 @@ __device__ __forceinline__ void load_sum8(const NormArgs& a, int64_t row, int c,
   }
 }
 
-// y of 8 columns from h, written as asked for
+// y of 8 columns from h, written as asked for.  h comes near 1 by a power of two first, so that its product with the gain is in range
+// where y is; nothing is rounded then, and in bf16 not in that product either.
 template <bool BF16>
 __device__ __forceinline__ void write_norm8(const NormArgs& a, int64_t row, int c, float inverse, float (&h)[8]) {
   float g[8];
   load_gain8(a.gain, a.gain_bf16, c, a.cols, g);
+  const bool ordinary = inverse > 0.0f && inverse < __builtin_inff();  // (not where the row has no norm)
+  const uint32_t bits = __float_as_uint(inverse);
+  const float power = ordinary ? __uint_as_float(bits & kInfinityBits) : 1.0f;
+  const float rest = ordinary ? __uint_as_float((bits & ~kInfinityBits) | 0x3F800000u) : inverse;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) h[k] = c + k < a.cols ? h[k] * g[k] * inverse : 0.0f;  // (h g is exact in bf16)
+  for (int k = 0; k < 8; ++k) h[k] = c + k < a.cols ? h[k] * power * g[k] * rest : 0.0f;
   if (a.y_out) store_row8<BF16>(at_row(a.y_out, row, a.cols, BF16), c, a.cols, h);
   if (a.out.values) {
     uint32_t m = 0;

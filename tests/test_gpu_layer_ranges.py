@@ -49,6 +49,21 @@ def test_norm_backward_of_large_and_small_rows(layer, rows, cols, size, eps, dty
     assert ((dgain.cpu().double() - (d * x * c).sum(0)).abs() <= 2.0 ** -24 * (rows / 16 + cols / 512 + 60) * sizes).all()
 
 
+@pytest.mark.parametrize("size,gain_size,eps", [(1e18, 1e26, 1e-5), (1e-17, 1e-25, 0.0)])
+@pytest.mark.parametrize("rows,cols", [(4, 200), (2, 5000), (2, 17000)])
+def test_norm_of_large_and_small_rows_and_gains(layer, rows, cols, size, gain_size, eps):
+    gen = torch.Generator().manual_seed(cols)
+    size = size / math.sqrt(cols)                            # (the sum of squares stays in range)
+    x = (size * rand(gen, rows, cols)).float().cuda()
+    gain = (gain_size * (1 + 0.3 * rand(gen, cols))).float().cuda()
+    y, q = torch.empty_like(x), layer.empty_scaled(rows, cols, "cuda")
+    layer.tsenor_norm(layer.make_norm(x, gain, eps, y_out=y, out=q))
+    h = x.cpu().double()
+    want = h / torch.sqrt(h.square().mean(1, keepdim=True) + eps) * gain.cpu().double()
+    near = 2.0 ** -24 * (cols / 512 + 32) * want.abs()
+    assert ((y.cpu().double() - want).abs() <= near + HALF_ULP["f32"] * want.abs() * 1.01).all()
+
+
 # ---- clipping -----------------------------------------------------------------------------------------------------------
 
 def clip(layer, grads, largest):
