@@ -117,7 +117,7 @@ int tsenor_product(const tsenor_product_problem* p, void* workspace, size_t work
 
 /* Norm and clipping of gradients: norm = sqrt(sum of squares over all tensors), summed in double;
  *   factor = max_norm / norm where norm is finite and larger than max_norm, 1 otherwise;  out = in * factor, rounded to its dtype.
- * A norm that is not finite leaves the gradients as they are: norm_out says so, and the caller drops the step. */
+ * A norm that is not finite, in single precision, leaves the gradients as they are: norm_out says so, and the caller drops the step. */
 typedef struct tsenor_gradient {
   const void* in;         /* count elements of `dtype`, in any order */
   void* out;              /* the same; in itself, or memory that overlaps no gradient */

@@ -156,7 +156,8 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(ClipTable table, const 
   double s = 0.0;
   for (int k = (int)threadIdx.x; k < count; k += kThreads) s += sums[k];
   const double norm = sqrt(group_sum(s));
-  const float factor = norm > max_norm && norm <= 1.7976931348623157e308 ? (float)(max_norm / norm) : 1.0f;
+  // (what is not finite goes by the norm as it is reported)
+  const float factor = norm > max_norm && (float)norm < __builtin_inff() ? (float)(max_norm / norm) : 1.0f;
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) norm_out[0] = (float)norm, norm_out[1] = factor;
   const uint32_t chunks = table.first[table.count];
   if (blockIdx.x >= chunks) return;

@@ -73,6 +73,13 @@ def clip(layer, grads, largest):
     return norm.cpu().double()
 
 
+def test_a_norm_beyond_single_precision_leaves_the_gradients(layer):
+    # finite in double, infinite where it is reported: the caller is told to drop the step, and finds the gradients as they were
+    g = torch.full((5,), 3e38, device="cuda")
+    kept = g.clone()
+    assert clip(layer, [g], 1.0).tolist() == [math.inf, 1.0] and torch.equal(g, kept)
+
+
 def test_clip_of_many_tensors_in_launches_of_all_sizes(layer):
     # launches of few and of many chunks in turn, so that the later ones add to the sums of some workgroups and begin those of others
     gen = torch.Generator("cuda").manual_seed(2)
