@@ -86,8 +86,9 @@ __device__ __forceinline__ double add_squares(const char* in, int size, double s
 }
 
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4), aligned(2)));
+// `size` elements times factor times `power`, a power of two
 template <bool BF16>
-__device__ __forceinline__ void scale(const char* in, char* out, int size, float factor) {
+__device__ __forceinline__ void scale(const char* in, char* out, int size, float factor, float power) {
   float x[kVectors][8];
 #pragma unroll
   for (int v = 0; v < kVectors; ++v) {
@@ -109,7 +110,7 @@ __device__ __forceinline__ void scale(const char* in, char* out, int size, float
   for (int v = 0; v < kVectors; ++v) {
     const int at = element_of(v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[v][j] *= factor;
+    for (int j = 0; j < 8; ++j) x[v][j] = x[v][j] * factor * power;
     if (size != kChunk) {
       store_row8<BF16>(out, at, size, x[v]);
     } else if constexpr (BF16) {
@@ -157,8 +158,11 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(ClipTable table, const 
   for (int k = (int)threadIdx.x; k < count; k += kThreads) s += sums[k];
   const double norm = sqrt(group_sum(s));
   // (what is not finite goes by the norm as it is reported)
-  const float factor = norm > max_norm && (float)norm < __builtin_inff() ? (float)(max_norm / norm) : 1.0f;
-  if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) norm_out[0] = (float)norm, norm_out[1] = factor;
+  const double exact = norm > max_norm && (float)norm < __builtin_inff() ? max_norm / norm : 1.0;
+  if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) norm_out[0] = (float)norm, norm_out[1] = (float)exact;
+  // (below 2^-126 a factor has fewer bits than its results: those of gradients of 1e38)
+  const bool tiny = exact < 0x1p-126;
+  const float factor = (float)(tiny ? exact * 0x1p126 : exact), power = tiny ? 0x1p-126f : 1.0f;
   const uint32_t chunks = table.first[table.count];
   if (blockIdx.x >= chunks) return;
   int k = tensor_of(table, chunks - 1 - blockIdx.x);
@@ -168,9 +172,9 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(ClipTable table, const 
     const Chunk c = chunk_of(table, k, chunk);
     if (factor == 1.0f && c.in == c.out) continue;
     if (c.size == kChunk)
-      c.bf16 ? scale<true>(c.in, c.out, kChunk, factor) : scale<false>(c.in, c.out, kChunk, factor);
+      c.bf16 ? scale<true>(c.in, c.out, kChunk, factor, power) : scale<false>(c.in, c.out, kChunk, factor, power);
     else
-      c.bf16 ? scale<true>(c.in, c.out, c.size, factor) : scale<false>(c.in, c.out, c.size, factor);
+      c.bf16 ? scale<true>(c.in, c.out, c.size, factor, power) : scale<false>(c.in, c.out, c.size, factor, power);
   }
 }
 

@@ -80,6 +80,18 @@ def test_a_norm_beyond_single_precision_leaves_the_gradients(layer):
     assert clip(layer, [g], 1.0).tolist() == [math.inf, 1.0] and torch.equal(g, kept)
 
 
+def test_factors_below_the_normal_numbers(layer):
+    # the factor is 5e-43 (357 steps of the smallest number), the results 5e-5: as exact as any others
+    for dtype in ("f32", "bf16"):
+        g = (1e38 * torch.tensor([1.0, -1.1, 0.9, 0.7])).to(DTYPES[dtype]).cuda()
+        wide = g.cpu().double()
+        norm = float(wide.norm())
+        got = clip(layer, [g], 1e-4)
+        assert abs(got[0] - norm) <= 1e-7 * norm and abs(got[1] - 1e-4 / norm) <= 2.0 ** -149
+        want = wide * (1e-4 / norm)
+        assert ((g.cpu().double() - want).abs() <= (HALF_ULP[dtype] * 1.01 + 2.0 ** -23) * want.abs()).all()
+
+
 def test_clip_of_many_tensors_in_launches_of_all_sizes(layer):
     # launches of few and of many chunks in turn, so that the later ones add to the sums of some workgroups and begin those of others
     gen = torch.Generator("cuda").manual_seed(2)
