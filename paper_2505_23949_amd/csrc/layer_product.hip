@@ -143,11 +143,11 @@ __device__ __forceinline__ intx4 resource_of(const void* base, int64_t bytes) {
 // instruction before such a load.)
 __device__ __forceinline__ void load_to_lds(uint32_t to, int lane_offset, const intx4& from, int offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(lane_offset), "s"(from), "s"(offset)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void load_dword_to_lds(uint32_t to, int lane_offset, const intx4& from, int offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(lane_offset), "s"(from), "s"(offset)
-               : "memory");
+               : "memory", "m0");
 }
 // waits for what this wave has asked of LDS (with LDS), and of memory but for the last PENDING loads, then for the other waves
 template <int PENDING, bool LDS = true>
@@ -155,6 +155,7 @@ __device__ __forceinline__ void meet() {
   static_assert(PENDING < 64);
   __builtin_amdgcn_s_waitcnt((LDS ? 0x0070 : 0x0F70) | (PENDING & 15) | (PENDING >> 4) << 14);
   __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");  // (neither of the two keeps a read of LDS behind it)
   TSENOR_IN_ORDER();
 }
 constexpr int kAnyPending = 63;

@@ -1,8 +1,12 @@
 """CPU-only checks of the layer operators at the edges of what they accept (no launches)."""
 import ctypes
+import re
+from pathlib import Path
 
 import pytest
 import torch
+
+ROOT = Path(__file__).resolve().parent.parent
 
 
 @pytest.fixture(scope="module")
@@ -173,3 +177,14 @@ def test_workspaces_elsewhere_are_refused(monkeypatch):
     for workspace in (torch.zeros(4096, dtype=torch.uint8), OnDevice(1)):      # in host memory, and on another GPU
         with pytest.raises(ValueError, match="workspace"):
             l.tsenor_clip(p, workspace)
+
+
+def test_assembly_names_the_registers_and_memory_it_changes():
+    # a statement that writes m0 says so: the compiler may keep an address or a lane number there
+    found = 0
+    for source in sorted((ROOT / "paper_2505_23949_amd" / "csrc").glob("*.h*p*")):
+        for statement in re.findall(r"asm volatile\((.*?)\);", source.read_text(), re.S):
+            if re.search(r"s_mov_b32 m0", statement):
+                found += 1
+                assert '"m0"' in statement.split(":")[-1], (source.name, statement)
+    assert found
