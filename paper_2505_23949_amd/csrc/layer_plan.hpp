@@ -38,7 +38,7 @@ struct Cost {
 //     4096 x 4096 x 4096       101 / 72 / 62 / 63 / 54       8192 x 8192 x 128       54 / 59 / 39 / 46 / 36
 //     7569 x 8229 x 920        147 / 127 / 96 / 102 / 88     14336 x 4096 x 8192     733 / 485 / 475 / 393 / 357
 // Where the small tiles leave CUs idle, workgroups share the columns of a tile; what they leave costs 0.025 us each to write and add,
-// and a launch: 48 x 4096 x 14336 alone 35, two 22, four 16.5, eight 17.5; 128 x 4096 x 14336 35, 23, 19.
+// and a launch: 48 x 4096 x 14336 alone 35, two 22, four 16.5, six (its choice) 16.1-16.6, eight 17.5; 128 x 4096 x 14336 35, 23, 19.
 // Up to 16 rows of a need no tiles: 1, 8 and 16 x 4096 x 14336 12.7, 14.0 and 15.7 (shared tiles 16); 16 x 4096 x 4096 8 (11); but 16 x
 // 14336 x 4096 18 where unshared tiles take 13, and 16 x 28672 x 8192 58 (51).  (Weights that no cache holds: 1, 8 and
 // 16 x 14336 x 4096 15, 16.6 and 19, tiles 17.)

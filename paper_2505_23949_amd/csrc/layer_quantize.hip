@@ -5,8 +5,9 @@
 // thread holds 4 x 8 of it: the row maxima are found over 16 lanes, the column maxima over 4 rows, 4 lanes and 8 waves,
 // the tile's over all.  Its 4 rows of a column are one 4-byte piece of the transposed tile, which goes through LDS so that both
 // results leave in whole 128-byte rows.  Bound by memory: 28672 x 8192 in single precision with a mask, both ways, 317 us
-// (5.2 TB/s), bf16 4096 x 14336 both ways 51 us (4.6); a few tiles by the chain of load, maximum and store: 1024 x 4096 6.8 us,
-// 7.2 where the loads of a row wait for those of the one before.  (8 x 8 to a thread, half as many waves, took 2, 12 and 43 % more.)
+// (5.2 TB/s), bf16 4096 x 14336 both ways 51 us (4.6); one tile to a CU, 1024 x 4096, 6.8 us, 7.2 where
+// the loads of a row wait for those of the one before; the 4-byte writes of the transposed tile conflict four ways in LDS.
+// (8 x 8 to a thread, half as many waves, took 2, 12 and 43 % more.)
 #include "layer.hpp"
 
 namespace {
