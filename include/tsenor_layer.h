@@ -22,6 +22,7 @@
  *   - A misaligned pointer or leading dimension is TSENOR_ERR_ALIGN (pointers: to their elements, workspaces to 256 bytes).
  *   - Results do not depend on what else runs, nor on earlier calls: sums have a fixed order, and there are no atomics.
  *   - Infinities and NaN are inputs like others.
+ *   - The GPU of the pointers and of the stream is the calling thread's current one (layer.py makes it current).
  */
 #ifndef TSENOR_LAYER_H
 #define TSENOR_LAYER_H
