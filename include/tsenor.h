@@ -61,7 +61,7 @@ typedef enum tsenor_status {
   TSENOR_ERR_WORKSPACE = -6,   /* workspace NULL, misaligned (256 B) or smaller than tsenor_workspace_bytes */
   TSENOR_ERR_HIP = -7,         /* a HIP call failed; tsenor_last_hip_error() returns the runtime's error code */
   TSENOR_ERR_TOO_LARGE = -8,   /* tsenor_mask_ex_static only: the problem needs more than TSENOR_STATIC_SCRATCH_BYTES */
-  TSENOR_ERR_ALIGN = -9        /* tsenor_layer.h only: a pointer or leading dimension is not aligned as stated there */
+  TSENOR_ERR_ALIGN = -9        /* tsenor_layer.h and tsenor_loss.h only: a pointer or leading dimension is not aligned as stated there */
 } tsenor_status;
 
 enum { TSENOR_F32 = 0, TSENOR_BF16 = 1 }; /* storage type of W; bf16 is widened exactly */

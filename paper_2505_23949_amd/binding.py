@@ -47,6 +47,8 @@ EXPORTS = (
     # layer.py
     "tsenor_quantize", "tsenor_norm", "tsenor_norm_backward_workspace_bytes", "tsenor_norm_backward",
     "tsenor_product_workspace_bytes", "tsenor_product", "tsenor_clip_workspace_bytes", "tsenor_clip",
+    # loss.py
+    "tsenor_cross_entropy_workspace_bytes", "tsenor_cross_entropy", "tsenor_distill_workspace_bytes", "tsenor_distill",
 )
 
 
@@ -122,9 +124,10 @@ def load() -> ctypes.CDLL:
         lib.tsenor_status_string.restype = ctypes.c_char_p
         lib.tsenor_version.restype = ctypes.c_int
         lib.tsenor_last_hip_error.restype = ctypes.c_int
-        from . import layer  # (which imports from here: not at the top)
+        from . import layer, loss  # (which import from here: not at the top)
 
         layer.declare(lib)
+        loss.declare(lib)
         _lib = lib
     return _lib
 

@@ -1,0 +1,354 @@
+// tsenor_cross_entropy, tsenor_distill: host side, and the kernels that go through tokens (the products: loss_product.hip).
+#include <algorithm>
+
+#include "loss.hpp"
+
+namespace {
+
+using namespace tsenor_dev;
+
+constexpr int kThreads = 256;
+constexpr int kMaxEntries = TSENOR_LOSS_MAX_ENTRIES;
+
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, lane_xor<1>(v)), v = fmaxf(v, lane_xor<2>(v)), v = fmaxf(v, lane_xor<7>(v));
+  v = fmaxf(v, lane_xor<15>(v)), v = fmaxf(v, lane_xor<16>(v));
+  return fmaxf(v, lane_xor<32>(v));
+}
+
+// logit of an entry by the teacher, over the temperature; -infinity where it takes no part
+__device__ __forceinline__ float teacher_of(const LossCall& c, int64_t token, int i) {
+  const int64_t id = c.ids[token * c.ids_ld + i];
+  if (id < 0 || id >= c.vocab) return -__builtin_inff();
+  const int64_t at = token * c.teacher_ld + i;
+  const float u = c.teacher_bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(c.teacher)[at] << 16) : static_cast<const float*>(c.teacher)[at];
+  return u * c.inverse_temperature;
+}
+
+// which tokens have an entry that takes part: a wave to a token
+__global__ __launch_bounds__(kThreads) void counts_kernel(LossCall c) {
+  const int token = (int)blockIdx.x * (kThreads / kWave) + (int)threadIdx.x / kWave, lane = (int)threadIdx.x % kWave;
+  if (token >= c.tokens) return;
+  bool any = false;
+  for (int i = lane; i < c.k; i += kWave) any |= teacher_of(c, token, i) != -__builtin_inff();  // (NaN does)
+  any = __any(any);
+  if (lane == 0) c.counts[token] = any;
+}
+
+// one workgroup: a thread takes 8 tokens at a time
+constexpr int kOrderThreads = 1024;
+__global__ __launch_bounds__(kOrderThreads) void order_kernel(LossCall c) {
+  __shared__ int before[kOrderThreads / kWave];
+  const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+  int done = 0;
+  for (int t0 = 0; t0 < c.tokens; t0 += kOrderThreads * 8) {
+    const int begin = t0 + (int)threadIdx.x * 8;
+    unsigned bits = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int t = begin + e;
+      if (t < c.tokens && (c.teacher ? c.counts[t] != 0 : c.ids[t] >= 0 && c.ids[t] < c.vocab)) bits |= 1u << e;
+    }
+    int upto = __popc(bits);  // of the wave's threads up to this one
+#pragma unroll
+    for (int step = 1; step < kWave; step *= 2) {
+      const int v = __shfl_up(upto, step);
+      if (lane >= step) upto += v;
+    }
+    __syncthreads();
+    if (lane == kWave - 1) before[wave] = upto;
+    __syncthreads();
+    int at = done + upto - __popc(bits), all = 0;
+#pragma unroll
+    for (int w = 0; w < kOrderThreads / kWave; ++w) {
+      if (w < wave) at += before[w];
+      all += before[w];
+    }
+    for (int e = 0; e < 8 && begin + e < c.tokens; ++e) {
+      if (bits >> e & 1)
+        c.order[at++] = begin + e;
+      else
+        c.order[c.tokens - 1 - (begin + e - at)] = begin + e;  // (as many as are not counted stand before it)
+    }
+    done += all;
+  }
+  if (threadIdx.x == 0) *c.count = done;
+}
+
+// a workgroup to a row of the piece's states, and to one more for each that its last tile has
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
+  constexpr int kSize = BF16 ? 2 : 4;
+  const int row = (int)blockIdx.x, rows = rows_of(c);
+  char* const state = static_cast<char*>(c.states) + (int64_t)row * c.states_ld * kSize;
+  float x[8] = {};
+  if (row < rows) {
+    const char* const h = static_cast<const char*>(c.h) + (int64_t)c.order[c.first + row] * c.h_ld * kSize;
+    for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) {
+      load_row8<BF16>(h, k, c.width, x);
+      store_row8<BF16>(state, k, c.states_ld, x);
+    }
+    return;
+  }
+  for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) store_row8<BF16>(state, k, c.states_ld, x);
+  if (row >= c.rows) return;
+  const int token = c.order[c.first + row];
+  if (threadIdx.x == 0) {
+    c.loss[token] = 0.0f;
+    if (c.lse) c.lse[token] = 0.0f;
+  }
+  if (c.dh)
+    for (int k = (int)threadIdx.x * 8; k < c.width; k += kThreads * 8)
+      store_row8<BF16>(static_cast<char*>(c.dh) + (int64_t)token * c.width * kSize, k, c.width, x);
+}
+
+// A workgroup to a token: lse, the logits of its entries, loss; exponentials into dz.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
+  constexpr int kSize = BF16 ? 2 : 4;
+  constexpr int kWaves = kThreads / kWave;
+  __shared__ float part[kWaves], logits[kMaxEntries], q[kMaxEntries], dentry[kMaxEntries];
+  __shared__ int words[kMaxEntries];
+  const int row = (int)blockIdx.x, lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+  if (row >= rows_of(c)) return;
+  const int token = c.order[c.first + row];
+  const float2* const sums = c.sums + (int64_t)row * c.tiles;
+
+  float largest = -__builtin_inff();
+  for (int t = (int)threadIdx.x; t < c.tiles; t += kThreads) largest = fmaxf(largest, sums[t].x);
+  largest = wave_max(largest);
+  if (lane == 0) part[wave] = largest;
+  __syncthreads();
+  largest = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+  __syncthreads();
+  float total = 0.0f;
+  for (int t = (int)threadIdx.x; t < c.tiles; t += kThreads) total += sums[t].y * expf(sums[t].x - largest);
+  total = wave_sum(total);
+  if (lane == 0) part[wave] = total;
+
+  // entries: a wave to each in turn
+  for (int i = wave; i < c.k; i += kWaves) {
+    const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
+    const bool valid = id >= 0 && id < c.vocab;
+    float s = 0.0f;
+    if (valid) {
+      const char* const h = static_cast<const char*>(c.states) + (int64_t)row * c.states_ld * kSize;
+      const char* const w = static_cast<const char*>(c.weight) + id * c.weight_ld * kSize;
+      for (int k = lane * 8; k < c.width; k += kWave * 8) {
+        float x[8], y[8];
+        load_row8<BF16>(h, k, c.width, x);
+        load_row8<BF16>(w, k, c.width, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
+      }
+    }
+    s = wave_sum(s) * c.inverse_temperature;
+    if (lane == 0) logits[i] = s, words[i] = valid ? (int)id : -1;
+  }
+  __syncthreads();
+  const float lse = largest + logf(part[0] + part[1] + part[2] + part[3]);
+
+  const float weight = (c.dloss ? c.dloss[token] : 1.0f) * c.inverse_temperature;
+  if (wave == 0) {
+    float loss;
+    if (!c.teacher) {
+      loss = lse - logits[0];
+      if (lane == 0) q[0] = 1.0f;
+    } else {
+      float top = -__builtin_inff();
+      for (int i = lane; i < c.k; i += kWave) top = fmaxf(top, teacher_of(c, token, i));
+      top = wave_max(top);
+      float all = 0.0f;
+      for (int i = lane; i < c.k; i += kWave) all += expf(teacher_of(c, token, i) - top);
+      all = wave_sum(all);
+      const float log_all = logf(all);
+      loss = 0.0f;
+      for (int i = lane; i < c.k; i += kWave) {
+        const float u = teacher_of(c, token, i) - top, p = expf(u) / all;
+        q[i] = p;
+        if (p != 0.0f) loss = fmaf(p, u - log_all - (logits[i] - lse), loss);
+      }
+      loss = wave_sum(loss);
+    }
+    if (lane == 0) {
+      c.loss[token] = loss;
+      if (c.lse) c.lse[token] = lse;
+    }
+  }
+  if (!c.dz) return;
+  __syncthreads();
+  // (the same word twice: both write what belongs to both)
+  for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
+    float p = 0.0f;
+    for (int j = 0; j < c.k; ++j)
+      if (words[j] == words[i]) p += q[j];
+    dentry[i] = weight * (expf(logits[i] - lse) - p);
+  }
+  char* const dz = static_cast<char*>(c.dz) + (int64_t)row * c.dz_ld * kSize;
+  for (int k = (int)threadIdx.x * 8; k < c.dz_ld; k += kThreads * 8) {
+    const float scale = weight * expf(sums[k / kTileN].x - lse) * (BF16 ? 1.0f / kExpScale : 1.0f);
+    float x[8];
+    if constexpr (BF16) {
+      _Float16 y[8];
+      __builtin_memcpy(y, dz + k * 2, 16);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (float)y[e];
+    } else {
+      __builtin_memcpy(x, dz + k * 4, 32);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = k + e < c.vocab ? x[e] * scale : 0.0f;
+    store_row8<BF16>(dz, k, c.dz_ld, x);
+  }
+  __syncthreads();
+  for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
+    if (words[i] < 0) continue;
+    if constexpr (BF16)
+      reinterpret_cast<uint16_t*>(dz)[words[i]] = (uint16_t)pack_bf16(dentry[i], 0.0f);
+    else
+      reinterpret_cast<float*>(dz)[words[i]] = dentry[i];
+  }
+}
+
+// no token counts, or there is none: zeros
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void zero_kernel(void* out, int64_t count) {
+  for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < count; k += (int64_t)gridDim.x * kThreads) {
+    if constexpr (BF16)
+      static_cast<uint16_t*>(out)[k] = 0;
+    else
+      static_cast<uint32_t*>(out)[k] = 0;
+  }
+}
+void launch_zero(void* out, int64_t count, bool bf16, hipStream_t s) {
+  const unsigned groups = (unsigned)std::min<int64_t>((count + kThreads - 1) / kThreads, 65536);
+  if (count == 0) return;
+  bf16 ? zero_kernel<true><<<groups, kThreads, 0, s>>>(out, count) : zero_kernel<false><<<groups, kThreads, 0, s>>>(out, count);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+constexpr int64_t kMaxTokens = (int64_t)1 << 24, kMaxVocab = (int64_t)1 << 21, kMaxWidth = (int64_t)1 << 16;
+constexpr int64_t kPieceBytes = (int64_t)1 << 31;  // of dz; a tenth of it for the sums of the tiles of a piece
+constexpr int kPieceRows = 256;                    // pieces are a multiple of this
+
+int check(const tsenor_head& p) {
+  if (p.tokens < 0 || p.tokens > kMaxTokens || p.vocab < 0 || p.vocab > kMaxVocab || p.width < 0 || p.width > kMaxWidth) return TSENOR_ERR_SHAPE;
+  if (!known(p.dtype)) return TSENOR_ERR_UNSUPPORTED;
+  if (p.tokens && (!p.loss_out || (p.width && !p.h))) return TSENOR_ERR_NULL;
+  if (p.vocab && p.width && !p.weight) return TSENOR_ERR_NULL;
+  if (!ld_ok(p.h_ld, p.tokens, p.width) || !ld_ok(p.weight_ld, p.vocab, p.width)) return TSENOR_ERR_SHAPE;
+  for (const void* m : {p.h, p.weight, (const void*)p.dh_out, (const void*)p.dweight_out})
+    if (!aligned_to(m, size_of(p.dtype))) return TSENOR_ERR_ALIGN;
+  for (const float* v : {p.dloss, (const float*)p.loss_out, (const float*)p.lse_out})
+    if (!aligned_to(v, sizeof(float))) return TSENOR_ERR_ALIGN;
+  return TSENOR_OK;
+}
+int check(const tsenor_cross_entropy_problem* p) {
+  if (!p) return TSENOR_ERR_NULL;
+  const int rc = check(p->head);
+  if (rc != TSENOR_OK) return rc;
+  if (p->head.tokens && !p->targets) return TSENOR_ERR_NULL;
+  return aligned_to(p->targets, sizeof(int64_t)) ? TSENOR_OK : TSENOR_ERR_ALIGN;
+}
+int check(const tsenor_distill_problem* p) {
+  if (!p) return TSENOR_ERR_NULL;
+  const int rc = check(p->head);
+  if (rc != TSENOR_OK) return rc;
+  if (p->k < 0 || p->k > kMaxEntries || !ld_ok(p->ids_ld, p->head.tokens, p->k) || !ld_ok(p->logits_ld, p->head.tokens, p->k)) return TSENOR_ERR_SHAPE;
+  if (!known(p->logits_dtype)) return TSENOR_ERR_UNSUPPORTED;
+  if (!(p->temperature >= 0x1p-20 && p->temperature <= 0x1p20)) return TSENOR_ERR_PARAM;
+  if (p->head.tokens && p->k && (!p->ids || !p->logits)) return TSENOR_ERR_NULL;
+  return aligned_to(p->ids, sizeof(int64_t)) && aligned_to(p->logits, size_of(p->logits_dtype)) ? TSENOR_OK : TSENOR_ERR_ALIGN;
+}
+
+inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// describes a call to the kernels; the workspace begins at `workspace` (which may be NULL to ask for its size alone)
+size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c) {
+  const bool bf16 = p.dtype == TSENOR_BF16, gradients = p.dh_out || p.dweight_out;
+  const int64_t size = bf16 ? 2 : 4, line = 128 / size;
+  c.h = p.h, c.weight = p.weight, c.h_ld = p.h_ld, c.weight_ld = p.weight_ld;
+  c.dloss = p.dloss, c.loss = p.loss_out, c.lse = p.lse_out, c.dh = p.dh_out, c.dweight = p.dweight_out;
+  c.tokens = (int)p.tokens, c.vocab = (int)p.vocab, c.width = (int)p.width;
+  c.states_ld = (int)std::max(round_up(p.width, line), line), c.dz_ld = (int)round_up(p.vocab, line);
+  c.tiles = (int)((p.vocab + kTileN - 1) / kTileN);
+  const int64_t row_bytes = gradients ? c.dz_ld * size : (int64_t)c.tiles * 8 * 10;
+  const int64_t most = std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows);
+  const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
+  c.rows = (int)std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
+  size_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    char* const begin = workspace + at;
+    at += (size_t)round_up(bytes, 256);
+    return begin;
+  };
+  c.count = reinterpret_cast<int*>(take(4));
+  c.order = reinterpret_cast<int*>(take(p.tokens * 4));
+  c.counts = reinterpret_cast<uint8_t*>(c.teacher ? take(p.tokens) : nullptr);
+  c.states = take((int64_t)round_up(c.rows, line) * c.states_ld * size);
+  c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
+  c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * size) : nullptr;
+  c.dweight_sum = bf16 && p.dweight_out && c.rows < p.tokens ? reinterpret_cast<float*>(take(p.vocab * p.width * 4)) : nullptr;
+  return at;
+}
+
+int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_bytes, hipStream_t s) {
+  const bool bf16 = p.dtype == TSENOR_BF16;
+  const size_t need = lay_out(p, nullptr, c);
+  if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need) return TSENOR_ERR_WORKSPACE;
+  lay_out(p, static_cast<char*>(workspace), c);
+  if (p.vocab == 0 || p.tokens == 0 || c.k == 0) {
+    launch_zero(p.loss_out, p.tokens, false, s);
+    if (p.lse_out) launch_zero(p.lse_out, p.tokens, false, s);
+    if (p.dh_out) launch_zero(p.dh_out, p.tokens * p.width, bf16, s);
+    if (p.dweight_out) launch_zero(p.dweight_out, p.vocab * p.width, bf16, s);
+    return status_of_launches();
+  }
+  if (c.teacher) counts_kernel<<<(unsigned)((c.tokens + 3) / 4), kThreads, 0, s>>>(c);
+  order_kernel<<<1, kOrderThreads, 0, s>>>(c);
+  for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
+    LossCall piece = c;
+    piece.rows = std::min(c.rows, c.tokens - c.first), piece.last = c.first + piece.rows == c.tokens;
+    const unsigned padded = (unsigned)round_up(piece.rows, bf16 ? 64 : 32);
+    bf16 ? gather_kernel<true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false><<<padded, kThreads, 0, s>>>(piece);
+    launch_logits(piece, bf16, s);
+    bf16 ? rows_kernel<true><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece) : rows_kernel<false><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece);
+    if (c.dh && c.width) launch_dh(piece, bf16, s);
+    if (c.dweight && c.width) launch_dweight(piece, bf16, s);
+  }
+  return status_of_launches();
+}
+
+LossCall call_of(const tsenor_cross_entropy_problem& p) {
+  LossCall c = {};
+  c.ids = p.targets, c.ids_ld = 1, c.k = 1, c.inverse_temperature = 1.0f;
+  return c;
+}
+LossCall call_of(const tsenor_distill_problem& p) {
+  LossCall c = {};
+  c.ids = p.ids, c.ids_ld = p.ids_ld, c.teacher = p.logits, c.teacher_ld = p.logits_ld, c.teacher_bf16 = p.logits_dtype == TSENOR_BF16;
+  c.k = p.k, c.inverse_temperature = (float)(1.0 / p.temperature);
+  return c;
+}
+template <class Problem>
+size_t workspace_of(const Problem* p) {
+  if (check(p) != TSENOR_OK) return 0;
+  LossCall c = call_of(*p);
+  return lay_out(p->head, nullptr, c);
+}
+template <class Problem>
+int run(const Problem* p, void* workspace, size_t workspace_bytes, tsenor_stream_t stream) {
+  const int rc = check(p);
+  return rc != TSENOR_OK ? rc : run(p->head, call_of(*p), workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace
+
+extern "C" size_t tsenor_cross_entropy_workspace_bytes(const tsenor_cross_entropy_problem* p) { return workspace_of(p); }
+extern "C" int tsenor_cross_entropy(const tsenor_cross_entropy_problem* p, void* workspace, size_t workspace_bytes, tsenor_stream_t stream) {
+  return run(p, workspace, workspace_bytes, stream);
+}
+extern "C" size_t tsenor_distill_workspace_bytes(const tsenor_distill_problem* p) { return workspace_of(p); }
+extern "C" int tsenor_distill(const tsenor_distill_problem* p, void* workspace, size_t workspace_bytes, tsenor_stream_t stream) {
+  return run(p, workspace, workspace_bytes, stream);
+}

@@ -1,0 +1,53 @@
+// What the kernels of the losses (tsenor_loss.h) share.
+//
+// A call goes through its tokens in pieces:
+//   order     (once) the tokens that count in front, those left out behind them: the products then have no rows for nothing
+//   gather    the piece's hidden states, one behind the other; outputs of those left out are cleared
+//   logits    z = h W^T in tiles: of each tile's rows the largest logit and the sum of exponentials, and, where gradients are wanted,
+//             the exponentials
+//   rows      for each token: the sums of its tiles joined, the logits of its entries, its loss; the exponentials become dz
+//   products  dh = dz W, dW = dz^T h
+// How many tokens count is known on the GPU only.  Grids are made for all of them, and workgroups without work end at once.
+#pragma once
+#include "layer.hpp"
+#include "tsenor_loss.h"
+
+namespace tsenor_dev {
+
+struct LossCall {
+  const void *h, *weight;
+  int64_t h_ld, weight_ld;
+  const int64_t* ids;
+  const void* teacher;     // logits of the entries; NULL: one entry to a token, of weight 1
+  int64_t ids_ld, teacher_ld;
+  int teacher_bf16, k;
+  float inverse_temperature;
+  const float* dloss;
+  float *loss, *lse;
+  void *dh, *dweight;
+  int tokens, vocab, width;
+  // workspace
+  int* count;              // tokens that count
+  int* order;              // tokens that count, in order; the last ones left out
+  uint8_t* counts;         // of a token, where that takes more than a look at its target
+  void* states;            // hidden states of the piece, states_ld to a row, zeros behind the width and the last row
+  float2* sums;            // of each row and tile: largest logit, sum of exponentials
+  void* dz;                // of the piece, dz_ld to a row, zeros behind the vocabulary
+  float* dweight_sum;      // the head's gradient of the pieces so far (bf16 and more than one piece)
+  int states_ld, dz_ld, tiles;
+  // of the piece
+  int first, rows;         // of `order`
+  bool last;
+};
+
+// rows of the piece that there are
+__device__ __forceinline__ int rows_of(const LossCall& c) { return min(max(*c.count - c.first, 0), c.rows); }
+
+constexpr int kTileN = 128;  // words of a tile of logits
+constexpr float kExpScale = 32768.0f;  // of exponentials kept in fp16: 2^15 for the largest of a tile
+
+void launch_logits(const LossCall& c, bool bf16, hipStream_t s);
+void launch_dh(const LossCall& c, bool bf16, hipStream_t s);
+void launch_dweight(const LossCall& c, bool bf16, hipStream_t s);
+
+}  // namespace tsenor_dev
