@@ -9,6 +9,7 @@ using namespace tsenor_dev;
 
 constexpr int kThreads = 256;
 constexpr int kMaxEntries = TSENOR_LOSS_MAX_ENTRIES;
+constexpr float kLn2 = 0.693147180559945f;
 
 __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, lane_xor<1>(v)), v = fmaxf(v, lane_xor<2>(v)), v = fmaxf(v, lane_xor<7>(v));
@@ -39,6 +40,8 @@ __global__ __launch_bounds__(kThreads) void counts_kernel(LossCall c) {
 constexpr int kOrderThreads = 1024;
 __global__ __launch_bounds__(kOrderThreads) void order_kernel(LossCall c) {
   __shared__ int before[kOrderThreads / kWave];
+  __shared__ float weights[kOrderThreads / kWave];
+  float weight = 0.0f;
   const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
   int done = 0;
   for (int t0 = 0; t0 < c.tokens; t0 += kOrderThreads * 8) {
@@ -47,7 +50,11 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(LossCall c) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int t = begin + e;
-      if (t < c.tokens && (c.teacher ? c.counts[t] != 0 : c.ids[t] >= 0 && c.ids[t] < c.vocab)) bits |= 1u << e;
+      if (t < c.tokens && (c.teacher ? c.counts[t] != 0 : c.ids[t] >= 0 && c.ids[t] < c.vocab)) {
+        bits |= 1u << e;
+        const float w = c.dloss ? fabsf(c.dloss[t]) : 1.0f;
+        if (w < __builtin_inff()) weight = fmaxf(weight, w);
+      }
     }
     int upto = __popc(bits);  // of the wave's threads up to this one
 #pragma unroll
@@ -72,7 +79,13 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(LossCall c) {
     }
     done += all;
   }
-  if (threadIdx.x == 0) *c.count = done;
+  weight = wave_max(weight);
+  if (lane == 0) weights[wave] = weight;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kOrderThreads / kWave; ++w) weight = fmaxf(weight, weights[w]);
+    *c.count = done, c.largest_weight[0] = weight, c.largest_weight[1] = weight * c.inverse_temperature;
+  }
 }
 
 // a workgroup to a row of the piece's states, and to one more for each that its last tile has
@@ -122,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
   largest = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
   __syncthreads();
   float total = 0.0f;
-  for (int t = (int)threadIdx.x; t < c.tiles; t += kThreads) total += sums[t].y * expf(sums[t].x - largest);
+  for (int t = (int)threadIdx.x; t < c.tiles; t += kThreads) total += sums[t].y * __builtin_amdgcn_exp2f(sums[t].x - largest);
   total = wave_sum(total);
   if (lane == 0) part[wave] = total;
 
@@ -142,17 +155,19 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
         for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
       }
     }
-    s = wave_sum(s) * c.inverse_temperature;
-    if (lane == 0) logits[i] = s, words[i] = valid ? (int)id : -1;
+    s = wave_sum(s);
+    if (lane == 0) logits[i] = fmaf(s, c.scale, -largest), words[i] = valid ? (int)id : -1;
   }
   __syncthreads();
-  const float lse = largest + logf(part[0] + part[1] + part[2] + part[3]);
+  // from here on exponents of 2, counted from `largest`; lse is what they are all divided by
+  total = part[0] + part[1] + part[2] + part[3];
+  const float lse = log2f(total);
 
-  const float weight = (c.dloss ? c.dloss[token] : 1.0f) * c.inverse_temperature;
+  const float unit = c.largest_weight[0], weight = c.dloss ? (unit > 0.0f ? c.dloss[token] / unit : c.dloss[token]) : 1.0f;
   if (wave == 0) {
     float loss;
     if (!c.teacher) {
-      loss = lse - logits[0];
+      loss = (lse - logits[0]) * kLn2;
       if (lane == 0) q[0] = 1.0f;
     } else {
       float top = -__builtin_inff();
@@ -166,13 +181,13 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
       for (int i = lane; i < c.k; i += kWave) {
         const float u = teacher_of(c, token, i) - top, p = expf(u) / all;
         q[i] = p;
-        if (p != 0.0f) loss = fmaf(p, u - log_all - (logits[i] - lse), loss);
+        if (p != 0.0f) loss = fmaf(p, u - log_all + (lse - logits[i]) * kLn2, loss);
       }
       loss = wave_sum(loss);
     }
     if (lane == 0) {
       c.loss[token] = loss;
-      if (c.lse) c.lse[token] = lse;
+      if (c.lse) c.lse[token] = (largest + lse) * kLn2;
     }
   }
   if (!c.dz) return;
@@ -182,11 +197,12 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
     float p = 0.0f;
     for (int j = 0; j < c.k; ++j)
       if (words[j] == words[i]) p += q[j];
-    dentry[i] = weight * (expf(logits[i] - lse) - p);
+    dentry[i] = weight * (__builtin_amdgcn_exp2f(logits[i]) / total - p);
   }
+  const float share = weight / total;
   char* const dz = static_cast<char*>(c.dz) + (int64_t)row * c.dz_ld * kSize;
   for (int k = (int)threadIdx.x * 8; k < c.dz_ld; k += kThreads * 8) {
-    const float scale = weight * expf(sums[k / kTileN].x - lse) * (BF16 ? 1.0f / kExpScale : 1.0f);
+    const float scale = share * __builtin_amdgcn_exp2f(sums[k / c.tile_n].x - largest);
     float x[8];
     if constexpr (BF16) {
       _Float16 y[8];
@@ -229,6 +245,8 @@ void launch_zero(void* out, int64_t count, bool bf16, hipStream_t s) {
 // ---- host ------------------------------------------------------------------------------------------------------------------
 constexpr int64_t kMaxTokens = (int64_t)1 << 24, kMaxVocab = (int64_t)1 << 21, kMaxWidth = (int64_t)1 << 16;
 constexpr int64_t kPieceBytes = (int64_t)1 << 31;  // of dz; a tenth of it for the sums of the tiles of a piece
+constexpr int64_t kMaxTileLd = (int64_t)1 << 21;   // (the tile kernels' offsets within a tile have 31 bits)
+constexpr double kLog2e = 1.4426950408889634;
 constexpr int kPieceRows = 256;                    // pieces are a multiple of this
 
 int check(const tsenor_head& p) {
@@ -271,7 +289,9 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c) {
   c.dloss = p.dloss, c.loss = p.loss_out, c.lse = p.lse_out, c.dh = p.dh_out, c.dweight = p.dweight_out;
   c.tokens = (int)p.tokens, c.vocab = (int)p.vocab, c.width = (int)p.width;
   c.states_ld = (int)std::max(round_up(p.width, line), line), c.dz_ld = (int)round_up(p.vocab, line);
-  c.tiles = (int)((p.vocab + kTileN - 1) / kTileN);
+  c.aligned = p.width && p.width % line == 0 && p.weight_ld * size % 16 == 0 && p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
+  c.logits_tile = c.aligned ? tile_for(p.tokens) : 0, c.tile_n = c.logits_tile == 4 ? 256 : 128;
+  c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
   const int64_t row_bytes = gradients ? c.dz_ld * size : (int64_t)c.tiles * 8 * 10;
   const int64_t most = std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows);
   const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
@@ -282,7 +302,8 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c) {
     at += (size_t)round_up(bytes, 256);
     return begin;
   };
-  c.count = reinterpret_cast<int*>(take(4));
+  c.count = reinterpret_cast<int*>(take(12));
+  c.largest_weight = reinterpret_cast<float*>(c.count + 1);
   c.order = reinterpret_cast<int*>(take(p.tokens * 4));
   c.counts = reinterpret_cast<uint8_t*>(c.teacher ? take(p.tokens) : nullptr);
   c.states = take((int64_t)round_up(c.rows, line) * c.states_ld * size);
@@ -311,23 +332,23 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     piece.rows = std::min(c.rows, c.tokens - c.first), piece.last = c.first + piece.rows == c.tokens;
     const unsigned padded = (unsigned)round_up(piece.rows, bf16 ? 64 : 32);
     bf16 ? gather_kernel<true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false><<<padded, kThreads, 0, s>>>(piece);
-    launch_logits(piece, bf16, s);
+    (c.aligned ? launch_logits : launch_any_logits)(piece, bf16, s);
     bf16 ? rows_kernel<true><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece) : rows_kernel<false><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece);
-    if (c.dh && c.width) launch_dh(piece, bf16, s);
-    if (c.dweight && c.width) launch_dweight(piece, bf16, s);
+    if (c.dh && c.width) (c.aligned ? launch_dh : launch_any_dh)(piece, bf16, s);
+    if (c.dweight && c.width) (c.aligned ? launch_dweight : launch_any_dweight)(piece, bf16, s);
   }
   return status_of_launches();
 }
 
 LossCall call_of(const tsenor_cross_entropy_problem& p) {
   LossCall c = {};
-  c.ids = p.targets, c.ids_ld = 1, c.k = 1, c.inverse_temperature = 1.0f;
+  c.ids = p.targets, c.ids_ld = 1, c.k = 1, c.inverse_temperature = 1.0f, c.scale = (float)kLog2e;
   return c;
 }
 LossCall call_of(const tsenor_distill_problem& p) {
   LossCall c = {};
   c.ids = p.ids, c.ids_ld = p.ids_ld, c.teacher = p.logits, c.teacher_ld = p.logits_ld, c.teacher_bf16 = p.logits_dtype == TSENOR_BF16;
-  c.k = p.k, c.inverse_temperature = (float)(1.0 / p.temperature);
+  c.k = p.k, c.inverse_temperature = (float)(1.0 / p.temperature), c.scale = (float)(kLog2e / p.temperature);
   return c;
 }
 template <class Problem>

@@ -21,20 +21,23 @@ struct LossCall {
   const void* teacher;     // logits of the entries; NULL: one entry to a token, of weight 1
   int64_t ids_ld, teacher_ld;
   int teacher_bf16, k;
-  float inverse_temperature;
+  float inverse_temperature, scale;  // scale: 1 / (temperature ln 2), logits to exponents of 2
   const float* dloss;
   float *loss, *lse;
   void *dh, *dweight;
   int tokens, vocab, width;
   // workspace
   int* count;              // tokens that count
+  float* largest_weight;   // largest |dloss| of them (of the finite ones), and that over the temperature
   int* order;              // tokens that count, in order; the last ones left out
   uint8_t* counts;         // of a token, where that takes more than a look at its target
   void* states;            // hidden states of the piece, states_ld to a row, zeros behind the width and the last row
-  float2* sums;            // of each row and tile: largest logit, sum of exponentials
+  float2* sums;            // of each row and tile: an exponent of 2, the sum of 2^(z scale - exponent)
   void* dz;                // of the piece, dz_ld to a row, zeros behind the vocabulary
   float* dweight_sum;      // the head's gradient of the pieces so far (bf16 and more than one piece)
-  int states_ld, dz_ld, tiles;
+  int states_ld, dz_ld;
+  int logits_tile, tile_n, tiles;  // kind of the tiles of the logits, words of one, tiles of a row
+  bool aligned;            // the head's rows are whole lines of 128 bytes that begin at multiples of 16
   // of the piece
   int first, rows;         // of `order`
   bool last;
@@ -43,11 +46,19 @@ struct LossCall {
 // rows of the piece that there are
 __device__ __forceinline__ int rows_of(const LossCall& c) { return min(max(*c.count - c.first, 0), c.rows); }
 
-constexpr int kTileN = 128;  // words of a tile of logits
-constexpr float kExpScale = 32768.0f;  // of exponentials kept in fp16: 2^15 for the largest of a tile
+// An exponential is 2^15 for the largest of its row and tile: kept in fp16 (bf16 matrices) they then have 11 bits down to 2^-29 of
+// that one, and steps of 2^-39 of it below.
+constexpr float kExpBits = 15.0f;
 
+// 64 rows of an operand to a unit of a tile: 4 (256 x 256), 2 (128 x 128) or 1 (64 x 128); 0: any rows, 128 x 128
+inline int tile_for(int64_t m) { return m > 128 ? 4 : m > 64 ? 2 : 1; }
+
+// the products with the tile kernels (heads that are `aligned`), and for any others
 void launch_logits(const LossCall& c, bool bf16, hipStream_t s);
 void launch_dh(const LossCall& c, bool bf16, hipStream_t s);
 void launch_dweight(const LossCall& c, bool bf16, hipStream_t s);
+void launch_any_logits(const LossCall& c, bool bf16, hipStream_t s);
+void launch_any_dh(const LossCall& c, bool bf16, hipStream_t s);
+void launch_any_dweight(const LossCall& c, bool bf16, hipStream_t s);
 
 }  // namespace tsenor_dev

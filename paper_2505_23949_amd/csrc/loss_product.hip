@@ -1,17 +1,11 @@
-// The products of the losses: logits with their sums, and the gradients of hidden states and head.
-#include "loss.hpp"
+// The products of the losses for heads whose rows begin anywhere.
+#include "loss_tile.hpp"
 
 namespace {
 
 using namespace tsenor_dev;
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef float floatx8 __attribute__((ext_vector_type(8)));
-
-enum Use { kLogits, kStates, kHead };
 constexpr int kTile = 128, kStep = 32, kThreads = 256;
-static_assert(kTile == kTileN);
 
 template <bool BF16>
 struct Format {
@@ -64,7 +58,7 @@ __device__ __forceinline__ floatx4 multiply(const typename Format<BF16>::Element
 }
 
 template <bool BF16, int USE>
-__global__ __launch_bounds__(kThreads) void product_kernel(LossCall c) {
+__global__ __launch_bounds__(kThreads) void any_kernel(LossCall c) {
   using F = Format<BF16>;
   __shared__ __align__(16) typename F::Element rows_a[kTile * F::kLd], rows_b[kTile * F::kLd];
   const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave, r = lane % 16, q = lane / 16;
@@ -103,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(LossCall c) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[i][j][e] = col0 + 16 * i + e < n ? sum[i][j][e] * c.inverse_temperature : -__builtin_inff();
+        for (int e = 0; e < 4; ++e) sum[i][j][e] = col0 + 16 * i + e < n ? sum[i][j][e] : -__builtin_inff();
     float largest[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -118,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(LossCall c) {
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) largest[j] = fmaxf(part[0][wave / 2 * 64 + j * 16 + r], part[1][wave / 2 * 64 + j * 16 + r]);
+    for (int j = 0; j < 4; ++j) largest[j] = fmaxf(part[0][wave / 2 * 64 + j * 16 + r], part[1][wave / 2 * 64 + j * 16 + r]) * c.scale - kExpBits;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -128,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(LossCall c) {
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          sum[i][j][e] = expf(sum[i][j][e] - base);
+          sum[i][j][e] = __builtin_amdgcn_exp2f(fmaf(sum[i][j][e], c.scale, -base));
           v += sum[i][j][e];
         }
       v += lane_xor<16>(v);
@@ -150,7 +144,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(LossCall c) {
           const int col = col0 + 16 * i + e;
           if (col >= c.dz_ld) continue;
           if constexpr (BF16)
-            static_cast<_Float16*>(c.dz)[(int64_t)row * c.dz_ld + col] = (_Float16)(sum[i][j][e] * kExpScale);
+            static_cast<_Float16*>(c.dz)[(int64_t)row * c.dz_ld + col] = (_Float16)sum[i][j][e];
           else
             static_cast<float*>(c.dz)[(int64_t)row * c.dz_ld + col] = sum[i][j][e];
         }
@@ -167,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(LossCall c) {
         for (int e = 0; e < 4; ++e) {
           const int col = col0 + 16 * i + e;
           if (col >= n) continue;
-          float v = sum[i][j][e];
+          float v = sum[i][j][e] * c.largest_weight[1];
           if constexpr (USE == kHead) {
             float* const all = BF16 ? c.dweight_sum : static_cast<float*>(c.dweight);
             if (c.first > 0) v += all[at + col];
@@ -190,15 +184,15 @@ inline unsigned tiles_of(int m, int n) { return (unsigned)((m + kTile - 1) / kTi
 
 }  // namespace
 
-void tsenor_dev::launch_logits(const LossCall& c, bool bf16, hipStream_t s) {
+void tsenor_dev::launch_any_logits(const LossCall& c, bool bf16, hipStream_t s) {
   const unsigned tiles = tiles_of(c.rows, c.vocab);
-  bf16 ? product_kernel<true, kLogits><<<tiles, kThreads, 0, s>>>(c) : product_kernel<false, kLogits><<<tiles, kThreads, 0, s>>>(c);
+  bf16 ? any_kernel<true, kLogits><<<tiles, kThreads, 0, s>>>(c) : any_kernel<false, kLogits><<<tiles, kThreads, 0, s>>>(c);
 }
-void tsenor_dev::launch_dh(const LossCall& c, bool bf16, hipStream_t s) {
+void tsenor_dev::launch_any_dh(const LossCall& c, bool bf16, hipStream_t s) {
   const unsigned tiles = tiles_of(c.rows, c.width);
-  bf16 ? product_kernel<true, kStates><<<tiles, kThreads, 0, s>>>(c) : product_kernel<false, kStates><<<tiles, kThreads, 0, s>>>(c);
+  bf16 ? any_kernel<true, kStates><<<tiles, kThreads, 0, s>>>(c) : any_kernel<false, kStates><<<tiles, kThreads, 0, s>>>(c);
 }
-void tsenor_dev::launch_dweight(const LossCall& c, bool bf16, hipStream_t s) {
+void tsenor_dev::launch_any_dweight(const LossCall& c, bool bf16, hipStream_t s) {
   const unsigned tiles = tiles_of(c.vocab, c.width);
-  bf16 ? product_kernel<true, kHead><<<tiles, kThreads, 0, s>>>(c) : product_kernel<false, kHead><<<tiles, kThreads, 0, s>>>(c);
+  bf16 ? any_kernel<true, kHead><<<tiles, kThreads, 0, s>>>(c) : any_kernel<false, kHead><<<tiles, kThreads, 0, s>>>(c);
 }

@@ -1,0 +1,400 @@
+// The tile kernel of the losses' products, C[row][col] = sum_k a(row, k) b(col, k), in its three uses:
+//   kLogits   a: states   (along the sum)    b: head (along)        z = h W^T, its rows' sums and exponentials
+//   kStates   a: dz       (along)            b: head (across)       dh = dz W
+//   kHead     a: dz       (across)           b: states (across)     dW = dz^T h
+// "Along": a row of the operand lies along the sum in memory.  "Across": the sum goes from row to row of memory.
+#pragma once
+#include <algorithm>
+
+#include "loss.hpp"
+#include "tile_loads.hpp"
+
+namespace tsenor_dev {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+
+enum Use { kLogits, kStates, kHead };
+
+// A workgroup of four waves, two by two, takes 64 TN rows of b (columns of the result) and 64 TM rows of a; a wave 32 TN x 32 TM results
+// in accumulators, of the 32 x 32 matrix instructions whose first operand is b: a lane holds four neighbouring columns of a row.
+// What 128 bytes of a row hold (64 columns of the sum in bf16, 32 in fp32) is a block; blocks come into a ring of BUFFERS in LDS by
+// loads that go there directly.
+//   Along: 128 bytes of LDS to a row; piece c of 16 bytes of row r stands at place c ^ (r / 2 % 8), so that the lanes that LDS serves
+//   at a time take all banks.
+//   Across: a row of LDS holds one column of the sum for all rows of the operand.  In bf16, reads that transpose 4 x 16 values on the way
+//   give a lane four columns of the sum for its row; the 64-byte chunks of LDS rows k are exchanged by k % 4 (chunk c stands at
+//   c ^ (k % 4)), so that the four rows of such a read take different banks.  In fp32 a lane reads single values.
+//   The order of the columns in the sum is free as long as both operands agree on it: a lane of half q of the wave holds, of half h of a
+//   block, the 16 h' + 8 q .. (see `fetch`).
+template <int TN, int TM>
+struct TileShape {
+  static constexpr int kRowsB = 64 * TN, kRowsA = 64 * TM;
+  static constexpr int kBuffer = (kRowsB + kRowsA) * 128;  // bytes of a block; b's rows first
+  static constexpr int kPieces = 2 * TN + 2 * TM;          // loads that a wave makes for a block
+};
+
+// Loads a wave's share of 64 T rows of an operand.
+// INTERLEAVED: row 32 t + r of each 32 T rows of LDS is row T r + t of memory, so that a lane gets T times as many neighbouring columns.
+template <int T, bool INTERLEAVED>
+struct LoaderAlong {
+  intx4 from;
+  uint32_t to;
+  int lane[2 * T];
+  __device__ __forceinline__ LoaderAlong(const void* p, int64_t ld_bytes, int first, int rows, int lane_id, int wave, uint32_t lds) {
+    from = resource_of(static_cast<const char*>(p) + first * ld_bytes, min(64 * T, rows - first) * ld_bytes);
+    to = lds + wave * 16 * T * 128;
+#pragma unroll
+    for (int j = 0; j < 2 * T; ++j) {
+      const int at = wave * 16 * T + 8 * j + lane_id / 8;
+      const int row = INTERLEAVED ? at / (32 * T) * (32 * T) + at % 32 * T + at % (32 * T) / 32 : at;
+      lane[j] = min(row, rows - 1 - first) * (int)ld_bytes + (lane_id % 8 ^ at / 2 % 8) * 16;
+    }
+  }
+  __device__ __forceinline__ void load(int buffer, int j, int block) const { load_to_lds(to + buffer + j * 1024, lane[j], from, block * 128); }
+};
+
+// `count` columns of the sum, `row_bytes` bytes of operand in each.  What lies past either end is read as something inside: past the
+// last column the other operand is zero, and past the last row nothing is written.
+template <int T, int SIZE>
+struct LoaderAcross {
+  static constexpr int kRowBytes = 64 * T * SIZE, kAtOnce = 1024 / kRowBytes, kLine = 128 / SIZE;
+  static_assert(kRowBytes <= 1024);
+  const char* base;
+  int64_t ld_bytes, past;  // offset of the last 16 bytes
+  uint32_t to;
+  int lane, step;
+  __device__ __forceinline__ LoaderAcross(const void* p, int64_t ld_bytes_, int first, int row_bytes, int count, int lane_id, int wave, uint32_t lds) {
+    base = static_cast<const char*>(p), ld_bytes = ld_bytes_, past = (count - 1) * ld_bytes + row_bytes - 16;
+    to = lds + wave * 1024;
+    const int k = wave * kAtOnce + lane_id * 16 / kRowBytes, at = lane_id * 16 % kRowBytes;
+    const int swap = SIZE == 4 ? 0 : kRowBytes >= 256 ? k % 4 : k / 2 % 2;
+    lane = k * (int)ld_bytes + min(first * SIZE + (at ^ swap * 64), row_bytes - 16);
+    step = 4 * kAtOnce * (int)ld_bytes;
+  }
+  __device__ __forceinline__ void load(int buffer, int j, int block) const {
+    const int64_t begin = block * (kLine * ld_bytes);
+    const int limit = (int)min(past - begin, (int64_t)INT32_MAX - 16), offset = min(j * step, limit);
+    load_to_lds(to + buffer + j * 4096, min(lane, limit - offset), resource_of(base + begin, (int64_t)limit + 16), offset);
+  }
+};
+
+// Reads one of a wave's T tiles of 32 rows: half h of the sum's columns of a block.
+template <int T, bool ALONG, int SIZE>
+struct Reader {
+  static constexpr int kRowBytes = 64 * T * SIZE;
+  int place[ALONG ? 2 : T];
+  __device__ __forceinline__ Reader(int lane, int wave) {  // wave: which half of the 64 T rows
+    const int r = lane % 32, q = lane / 32;
+    if constexpr (ALONG) {
+      place[0] = wave * 32 * T * 128 + r * 128 + ((2 * q) ^ (r / 2 % 8)) * 16;
+      place[1] = wave * 32 * T * 128 + r * 128 + ((2 * q + 1) ^ (r / 2 % 8)) * 16;
+    } else if constexpr (SIZE == 2) {
+      const int i = lane % 16, k = 16 * q + i / 4, swap = kRowBytes >= 256 ? k % 4 : k / 2 % 2;
+#pragma unroll
+      for (int t = 0; t < T; ++t) place[t] = k * kRowBytes + ((wave * T + t) ^ swap) * 64 + lane / 16 % 2 * 32 + i % 4 * 8;
+    } else {
+#pragma unroll
+      for (int t = 0; t < T; ++t) place[t] = 8 * q * kRowBytes + (wave * 32 * T + 32 * t + r) * 4;
+    }
+  }
+  __device__ __forceinline__ intx8 fetch(const uint8_t* rows, int t, int h) const {
+    if constexpr (ALONG) {
+      const intx4 lo = *reinterpret_cast<const intx4*>(rows + t * 4096 + (place[0] ^ h * 64));
+      const intx4 hi = *reinterpret_cast<const intx4*>(rows + t * 4096 + (place[1] ^ h * 64));
+      return intx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    } else if constexpr (SIZE == 2) {
+      typedef __attribute__((address_space(3))) shortx4* Lds;
+      typedef int intx2 __attribute__((ext_vector_type(2)));
+      intx2 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        v[u] = __builtin_bit_cast(intx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(rows + place[t] + (32 * h + 4 * u) * kRowBytes)));
+      return intx8{v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
+    } else {
+      intx8 v;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const int*>(rows + place[t] + (16 * h + u) * kRowBytes);
+      return v;
+    }
+  }
+};
+
+template <bool BF16>
+__device__ __forceinline__ floatx16 multiply(const intx8& b, const intx8& a, floatx16 sum) {
+  if constexpr (BF16) {
+    const intx4 b0 = {b[0], b[1], b[2], b[3]}, b1 = {b[4], b[5], b[6], b[7]}, a0 = {a[0], a[1], a[2], a[3]}, a1 = {a[4], a[5], a[6], a[7]};
+    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b0), __builtin_bit_cast(bf16x8, a0), sum, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b1), __builtin_bit_cast(bf16x8, a1), sum, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(b[u]), __int_as_float(a[u]), sum, 0, 0, 0);
+    return sum;
+  }
+}
+
+// What a lane holds of tile t of b and j of a: element 4 g + e is row 8 g + 4 q + e of the tile of b.  Columns 32 t + 16 p .. of a wave go
+// out (p: pair of g), 8 of them from each lane (bf16: the halves of the wave exchange fours first) or twice four (fp32).
+template <bool BF16, int USE>
+__device__ __forceinline__ void write_gradient(const LossCall& c, int row, int64_t at, int col, floatx4 lo, floatx4 hi) {
+  // lo, hi: columns col + 4 q and col + 8 + 4 q of the row whose result begins at element `at`
+  const int q = (int)threadIdx.x / 32 % 2, n = c.width;
+  float* const sums = USE == kHead && BF16 ? c.dweight_sum : static_cast<float*>(c.dweight);
+  if (USE == kHead && (c.first > 0 || !c.last)) {  // sums of several pieces, in fp32
+    const auto add = [&](floatx4& v, int col) {
+      if (row < 0 || col >= n) return;
+      float* const to = sums + at + col;
+      if (c.first > 0) {
+        float old[4];
+        __builtin_memcpy(old, to, 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += old[e];
+      }
+      if (!BF16 || !c.last) __builtin_memcpy(to, &v, 16);
+    };
+    add(lo, col + 4 * q);
+    add(hi, col + 8 + 4 * q);
+    if (!BF16 || !c.last) return;
+  }
+  void* const out = USE == kStates ? c.dh : c.dweight;
+  if constexpr (BF16) {
+    uint32_t w[4] = {pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const auto r = __builtin_amdgcn_permlane32_swap(w[k], w[2 + k], false, false);
+      w[k] = r[0], w[2 + k] = r[1];
+    }
+    col += 8 * q;
+    if (row >= 0 && col < n) __builtin_memcpy(static_cast<uint16_t*>(out) + at + col, w, 16);
+  } else {
+    if (row >= 0 && col + 4 * q < n) __builtin_memcpy(static_cast<float*>(out) + at + col + 4 * q, &lo, 16);
+    if (row >= 0 && col + 8 + 4 * q < n) __builtin_memcpy(static_cast<float*>(out) + at + col + 8 + 4 * q, &hi, 16);
+  }
+}
+
+template <int TN, int TM, int BUFFERS>
+constexpr int kGroupsPerCu = BUFFERS * TileShape<TN, TM>::kBuffer <= 80 * 1024 ? 2 : 1;
+
+template <bool BF16, int USE, int TN, int TM, int BUFFERS>
+__global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
+  using Shape = TileShape<TN, TM>;
+  constexpr int kSize = BF16 ? 2 : 4, kLine = 128 / kSize;
+  constexpr bool kAlongB = USE == kLogits, kAlongA = USE != kHead;
+  __shared__ __align__(1024) uint8_t lds[BUFFERS * Shape::kBuffer];
+  const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
+  const int piece = __builtin_amdgcn_readfirstlane(rows_of(c));
+  const int m = USE == kHead ? c.vocab : piece, n = USE == kLogits ? c.vocab : c.width;
+  const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB;
+  if ((int)blockIdx.x >= tiles_m * tiles_n) return;
+  const int blocks = USE == kLogits ? c.states_ld / kLine : USE == kStates ? c.dz_ld / kLine : (piece + kLine - 1) / kLine;
+  if (USE == kHead && blocks == 0 && c.first > 0 && !c.last) return;
+  int tile_m, tile_n;
+  tile_of((int)blockIdx.x, tiles_m, tiles_n, tile_m, tile_n);
+  const int m0 = tile_m * Shape::kRowsA, n0 = tile_n * Shape::kRowsB, last = blocks - 1;
+
+  floatx16 sum[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.0f;
+
+  const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+  const auto of_b = [&] {
+    if constexpr (USE == kLogits)
+      return LoaderAlong<TN, true>(c.weight, c.weight_ld * kSize, n0, n, lane, wave, lds_at);
+    else if constexpr (USE == kStates)
+      return LoaderAcross<TN, kSize>(c.weight, c.weight_ld * kSize, n0, c.width * kSize, c.vocab, lane, wave, lds_at);
+    else
+      return LoaderAcross<TN, kSize>(c.states, c.states_ld * kSize, n0, c.states_ld * kSize, blocks * kLine, lane, wave, lds_at);
+  }();
+  const uint32_t lds_a = lds_at + Shape::kRowsB * 128;
+  const auto of_a = [&] {
+    if constexpr (USE == kLogits)
+      return LoaderAlong<TM, false>(c.states, c.states_ld * kSize, m0, m, lane, wave, lds_a);
+    else if constexpr (USE == kStates)
+      return LoaderAlong<TM, false>(c.dz, (int64_t)c.dz_ld * kSize, m0, m, lane, wave, lds_a);
+    else
+      return LoaderAcross<TM, kSize>(c.dz, (int64_t)c.dz_ld * kSize, m0, c.dz_ld * kSize, piece, lane, wave, lds_a);
+  }();
+  const auto load = [&](int buffer, int k, int block) {
+    if (k < 2 * TN)
+      of_b.load(buffer, k, block);
+    else
+      of_a.load(buffer, k - 2 * TN, block);
+  };
+  const Reader<TN, kAlongB, kSize> read_b(lane, wave_n);
+  const Reader<TM, kAlongA, kSize> read_a(lane, wave_m);
+  const uint8_t *const rows_b = lds, *const rows_a = lds + Shape::kRowsB * 128;
+
+  // With more than two buffers the loads of a block are spread over the second half of a step and the first of the next.
+  // (A block past the last is the last one again, which nothing uses.)
+  constexpr int kEarly = BUFFERS > 2 ? Shape::kPieces / 2 : Shape::kPieces;  // loads of a block in the second half
+  intx8 b[TN][2], a[TM][2];                                                   // tile, half of the columns
+  if (blocks > 0) {
+#pragma unroll
+    for (int k = 0; k < BUFFERS; ++k)
+#pragma unroll
+      for (int at = 0; at < (k == BUFFERS - 1 ? kEarly : Shape::kPieces); ++at) load(k * Shape::kBuffer, at, min(k, last));
+    meet<(BUFFERS - 2) * Shape::kPieces + kEarly>();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      b[0][h] = read_b.fetch(rows_b, 0, h), a[0][h] = read_a.fetch(rows_a, 0, h);
+      if constexpr (TN == 4) b[1][h] = read_b.fetch(rows_b, 1, h);
+    }
+  }
+
+// The instructions of a step stand in the order in which they are issued: reads of LDS, loads and multiplications are spread evenly.
+// (The statement behind each multiplication does nothing but keep it from being moved past the next.)
+#define MULTIPLY(i, j, h)                               \
+  sum[i][j] = multiply<BF16>(b[i][h], a[j][h], sum[i][j]); \
+  asm volatile("" : "+a"(sum[i][j]));                   \
+  TSENOR_IN_ORDER();
+#define FETCH_B(buffer, t, h) b[t][h] = read_b.fetch(rows_b + buffer, t, h); TSENOR_IN_ORDER();
+#define FETCH_A(buffer, t, h) a[t][h] = read_a.fetch(rows_a + buffer, t, h); TSENOR_IN_ORDER();
+#define LOAD(k) if constexpr (k < kEarly) { load(buffer, k, ahead); TSENOR_IN_ORDER(); }
+#define LATE(k) if constexpr (k >= kEarly) { load(old_buffer, k, ahead_of_old); TSENOR_IN_ORDER(); }
+  constexpr int kPending = (BUFFERS - 2) * Shape::kPieces;  // loads of the blocks after the next
+  int buffer = 0, next_buffer = Shape::kBuffer, old_buffer = (BUFFERS - 1) * Shape::kBuffer;
+  for (int block = 0; block <= last; ++block) {
+    const int ahead = min(block + BUFFERS, last), ahead_of_old = min(block + BUFFERS - 1, last);
+    TSENOR_IN_ORDER();
+    if constexpr (TN == 4 && TM == 4) {
+      MULTIPLY(0, 0, 0) FETCH_A(buffer, 1, 0) MULTIPLY(1, 0, 0) FETCH_A(buffer, 1, 1) MULTIPLY(0, 0, 1) FETCH_A(buffer, 2, 0)
+      MULTIPLY(1, 0, 1) FETCH_A(buffer, 2, 1) MULTIPLY(0, 1, 0) FETCH_A(buffer, 3, 0) MULTIPLY(1, 1, 0) FETCH_A(buffer, 3, 1)
+      MULTIPLY(0, 1, 1) FETCH_B(buffer, 2, 0) MULTIPLY(1, 1, 1) FETCH_B(buffer, 2, 1) MULTIPLY(0, 2, 0) FETCH_B(buffer, 3, 0)
+      MULTIPLY(1, 2, 0) FETCH_B(buffer, 3, 1) MULTIPLY(0, 2, 1) MULTIPLY(1, 2, 1)
+      MULTIPLY(0, 3, 0) MULTIPLY(1, 3, 0) MULTIPLY(0, 3, 1) MULTIPLY(1, 3, 1)
+      meet<kAnyPending>();
+      MULTIPLY(2, 2, 0) LOAD(0) MULTIPLY(3, 2, 0) LOAD(1) MULTIPLY(2, 2, 1) LOAD(2) MULTIPLY(3, 2, 1) LOAD(3)
+      MULTIPLY(2, 3, 0) LOAD(4) MULTIPLY(3, 3, 0) LOAD(5) MULTIPLY(2, 3, 1) LOAD(6) MULTIPLY(3, 3, 1) LOAD(7)
+      // only here the next block has to have come: a quarter of a step more for its loads, which two buffers leave little time
+      meet<8, false>();
+      MULTIPLY(2, 0, 0) FETCH_B(next_buffer, 0, 0) LOAD(8) MULTIPLY(3, 0, 0) FETCH_B(next_buffer, 1, 0) LOAD(9)
+      MULTIPLY(2, 0, 1) FETCH_B(next_buffer, 0, 1) LOAD(10) MULTIPLY(3, 0, 1) FETCH_B(next_buffer, 1, 1) LOAD(11)
+      MULTIPLY(2, 1, 0) FETCH_A(next_buffer, 0, 0) LOAD(12) MULTIPLY(3, 1, 0) FETCH_A(next_buffer, 0, 1) LOAD(13)
+      MULTIPLY(2, 1, 1) LOAD(14) MULTIPLY(3, 1, 1) LOAD(15)
+    } else if constexpr (TN == 2 && TM == 2) {
+      MULTIPLY(0, 0, 0) FETCH_A(buffer, 1, 0) FETCH_A(buffer, 1, 1) LATE(4) MULTIPLY(0, 0, 1) FETCH_B(buffer, 1, 0) FETCH_B(buffer, 1, 1) LATE(5)
+      MULTIPLY(0, 1, 0) LATE(6) LATE(7) MULTIPLY(0, 1, 1)
+      meet<kPending>();
+      MULTIPLY(1, 0, 0) LOAD(0) LOAD(1) FETCH_B(next_buffer, 0, 0) MULTIPLY(1, 0, 1) LOAD(2) LOAD(3) FETCH_B(next_buffer, 0, 1)
+      MULTIPLY(1, 1, 0) LOAD(4) LOAD(5) FETCH_A(next_buffer, 0, 0) MULTIPLY(1, 1, 1) LOAD(6) LOAD(7) FETCH_A(next_buffer, 0, 1)
+    } else {
+      static_assert(TN == 2 && TM == 1);
+      MULTIPLY(0, 0, 0) FETCH_B(buffer, 1, 0) FETCH_B(buffer, 1, 1) LATE(3) LATE(4) LATE(5) MULTIPLY(0, 0, 1)
+      meet<kPending>();
+      MULTIPLY(1, 0, 0) LOAD(0) LOAD(1) FETCH_B(next_buffer, 0, 0) LOAD(2) FETCH_B(next_buffer, 0, 1) LOAD(3)
+      MULTIPLY(1, 0, 1) LOAD(4) LOAD(5) FETCH_A(next_buffer, 0, 0) FETCH_A(next_buffer, 0, 1)
+    }
+    old_buffer = buffer, buffer = next_buffer, next_buffer += Shape::kBuffer;
+    if (next_buffer == BUFFERS * Shape::kBuffer) next_buffer = 0;
+  }
+#undef MULTIPLY
+#undef FETCH_B
+#undef FETCH_A
+#undef LOAD
+#undef LATE
+  meet<0>();  // (no load into LDS outlives the workgroup)
+
+  if constexpr (USE == kLogits) {
+    // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b
+    float* const part = reinterpret_cast<float*>(lds);  // [2][kRowsA]
+    const int col0 = n0 + wave_n * 32 * TN + 4 * TN * q;
+    const bool whole = n0 + Shape::kRowsB <= n;
+    float largest[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      float v = -__builtin_inff();
+#pragma unroll
+      for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if (!whole && col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
+          v = fmaxf(v, sum[t][j][e]);
+        }
+      v = fmaxf(v, lane_xor<32>(v));
+      if (q == 0) part[wave_n * Shape::kRowsA + (wave_m * TM + j) * 32 + r] = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int row = (wave_m * TM + j) * 32 + r;
+      largest[j] = fmaxf(part[row], part[Shape::kRowsA + row]) * c.scale - kExpBits;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int row = (wave_m * TM + j) * 32 + r;
+      const float base = largest[j] == -__builtin_inff() ? 0.0f : largest[j];
+      const int64_t at = (int64_t)(m0 + row) * c.dz_ld;
+      float v = 0.0f;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float x[4 * TN];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int t = 0; t < TN; ++t) {
+            x[e * TN + t] = __builtin_amdgcn_exp2f(fmaf(sum[t][j][4 * g + e], c.scale, -base));
+            v += x[e * TN + t];
+          }
+        const int col = col0 + 8 * TN * g;
+        if (c.dz && m0 + row < m && col < c.dz_ld) {
+          if constexpr (BF16) {
+            uint32_t w[2 * TN];
+#pragma unroll
+            for (int k = 0; k < 2 * TN; ++k)
+              w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{x[2 * k], x[2 * k + 1]}, halfx2));
+            __builtin_memcpy(__builtin_assume_aligned(static_cast<uint16_t*>(c.dz) + at + col, 16), w, 8 * TN);
+          } else {
+            __builtin_memcpy(__builtin_assume_aligned(static_cast<float*>(c.dz) + at + col, 16), x, 16 * TN);
+          }
+        }
+      }
+      v += lane_xor<32>(v);
+      if (q == 0) part[wave_n * Shape::kRowsA + row] = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int row = (wave_m * TM + j) * 32 + r;
+      if (q == 0 && wave_n == 0 && m0 + row < m)
+        c.sums[(int64_t)(m0 + row) * c.tiles + tile_n] = make_float2(largest[j], part[row] + part[Shape::kRowsA + row]);
+    }
+  } else {
+    const float scale = c.largest_weight[1];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int row = m0 + (wave_m * TM + j) * 32 + r;
+      const int64_t at = (int64_t)(row >= m ? 0 : USE == kStates ? c.order[c.first + row] : row) * c.width;
+#pragma unroll
+      for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          floatx4 lo, hi;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) lo[e] = sum[t][j][8 * p + e] * scale, hi[e] = sum[t][j][8 * p + 4 + e] * scale;
+          write_gradient<BF16, USE>(c, row < m ? row : -1, at, n0 + (wave_n * TN + t) * 32 + 16 * p, lo, hi);
+        }
+    }
+  }
+}
+
+// the kernel with the tiles that suit the rows of a
+template <bool BF16, int USE>
+void launch_tiles(const LossCall& c, hipStream_t s) {
+  const int64_t m = USE == kHead ? c.vocab : c.rows, n = USE == kLogits ? c.vocab : c.width;
+  const auto groups = [&](int tn, int tm) { return (unsigned)((m + 64 * tm - 1) / (64 * tm) * ((n + 64 * tn - 1) / (64 * tn))); };
+  switch (USE == kLogits ? c.logits_tile : tile_for(m)) {
+    case 4: tile_kernel<BF16, USE, 4, 4, 2><<<groups(4, 4), 256, 0, s>>>(c); break;
+    case 2: tile_kernel<BF16, USE, 2, 2, 4><<<groups(2, 2), 256, 0, s>>>(c); break;
+    default: tile_kernel<BF16, USE, 2, 1, 6><<<groups(2, 1), 256, 0, s>>>(c); break;
+  }
+}
+
+}  // namespace tsenor_dev
