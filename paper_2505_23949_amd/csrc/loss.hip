@@ -1,4 +1,4 @@
-// tsenor_cross_entropy, tsenor_distill: host side, and the kernels that go through tokens (the products: loss_product.hip).
+// tsenor_cross_entropy, tsenor_distill: host side, and the kernels that go through tokens (the products: loss_tile.hpp).
 #include <algorithm>
 
 #include "loss.hpp"
@@ -113,6 +113,19 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
   if (c.dh)
     for (int k = (int)threadIdx.x * 8; k < c.width; k += kThreads * 8)
       store_row8<BF16>(static_cast<char*>(c.dh) + (int64_t)token * c.width * kSize, k, c.width, x);
+}
+
+// the head with rows of whole lines: a workgroup to a row
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void head_kernel(const void* weight, int64_t ld, int width, void* head, int head_ld) {
+  constexpr int kSize = BF16 ? 2 : 4;
+  const char* const from = static_cast<const char*>(weight) + (int64_t)blockIdx.x * ld * kSize;
+  char* const to = static_cast<char*>(head) + (int64_t)blockIdx.x * head_ld * kSize;
+  for (int k = (int)threadIdx.x * 8; k < head_ld; k += kThreads * 8) {
+    float x[8];
+    load_row8<BF16>(from, k, width, x);
+    store_row8<BF16>(to, k, head_ld, x);
+  }
 }
 
 // A workgroup to a token: lse, the logits of its entries, loss; exponentials into dz.
@@ -281,21 +294,28 @@ int check(const tsenor_distill_problem* p) {
 
 inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
+struct Plans {
+  ProductPlan logits, dh, dweight;
+};
+
 // describes a call to the kernels; the workspace begins at `workspace` (which may be NULL to ask for its size alone)
-size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c) {
+size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans) {
   const bool bf16 = p.dtype == TSENOR_BF16, gradients = p.dh_out || p.dweight_out;
   const int64_t size = bf16 ? 2 : 4, line = 128 / size;
   c.h = p.h, c.weight = p.weight, c.h_ld = p.h_ld, c.weight_ld = p.weight_ld;
   c.dloss = p.dloss, c.loss = p.loss_out, c.lse = p.lse_out, c.dh = p.dh_out, c.dweight = p.dweight_out;
   c.tokens = (int)p.tokens, c.vocab = (int)p.vocab, c.width = (int)p.width;
   c.states_ld = (int)std::max(round_up(p.width, line), line), c.dz_ld = (int)round_up(p.vocab, line);
-  c.aligned = p.width && p.width % line == 0 && p.weight_ld * size % 16 == 0 && p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
-  c.logits_tile = c.aligned ? tile_for(p.tokens) : 0, c.tile_n = c.logits_tile == 4 ? 256 : 128;
-  c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
-  const int64_t row_bytes = gradients ? c.dz_ld * size : (int64_t)c.tiles * 8 * 10;
+  const int64_t row_bytes = gradients ? c.dz_ld * size : (p.vocab + 127) / 128 * 8 * 10;
   const int64_t most = std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows);
   const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
   c.rows = (int)std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
+  plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line, bf16, false);
+  if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line, bf16, true);
+  if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line, bf16, true);
+  c.tile_n = plans.logits.kind == kLargeTile ? 256 : 128;
+  c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
+  const bool whole = p.width && p.width % line == 0 && p.weight_ld * size % 16 == 0 && p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
   size_t at = 0;
   const auto take = [&](int64_t bytes) {
     char* const begin = workspace + at;
@@ -310,14 +330,17 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c) {
   c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
   c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * size) : nullptr;
   c.dweight_sum = bf16 && p.dweight_out && c.rows < p.tokens ? reinterpret_cast<float*>(take(p.vocab * p.width * 4)) : nullptr;
+  c.head = whole ? nullptr : take(p.vocab * c.states_ld * size);
+  c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max(plans.dh.workspace, plans.dweight.workspace)));
   return at;
 }
 
 int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_bytes, hipStream_t s) {
   const bool bf16 = p.dtype == TSENOR_BF16;
-  const size_t need = lay_out(p, nullptr, c);
+  Plans plans = {};
+  const size_t need = lay_out(p, nullptr, c, plans);
   if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need) return TSENOR_ERR_WORKSPACE;
-  lay_out(p, static_cast<char*>(workspace), c);
+  lay_out(p, static_cast<char*>(workspace), c, plans);
   if (p.vocab == 0 || p.tokens == 0 || c.k == 0) {
     launch_zero(p.loss_out, p.tokens, false, s);
     if (p.lse_out) launch_zero(p.lse_out, p.tokens, false, s);
@@ -327,15 +350,20 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
   }
   if (c.teacher) counts_kernel<<<(unsigned)((c.tokens + 3) / 4), kThreads, 0, s>>>(c);
   order_kernel<<<1, kOrderThreads, 0, s>>>(c);
+  if (c.head) {
+    bf16 ? head_kernel<true><<<(unsigned)c.vocab, kThreads, 0, s>>>(c.weight, c.weight_ld, c.width, c.head, c.states_ld)
+         : head_kernel<false><<<(unsigned)c.vocab, kThreads, 0, s>>>(c.weight, c.weight_ld, c.width, c.head, c.states_ld);
+    c.weight = c.head, c.weight_ld = c.states_ld;
+  }
   for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
     LossCall piece = c;
     piece.rows = std::min(c.rows, c.tokens - c.first), piece.last = c.first + piece.rows == c.tokens;
     const unsigned padded = (unsigned)round_up(piece.rows, bf16 ? 64 : 32);
     bf16 ? gather_kernel<true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false><<<padded, kThreads, 0, s>>>(piece);
-    (c.aligned ? launch_logits : launch_any_logits)(piece, bf16, s);
+    launch_logits(piece, plans.logits, bf16, s);
     bf16 ? rows_kernel<true><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece) : rows_kernel<false><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece);
-    if (c.dh && c.width) (c.aligned ? launch_dh : launch_any_dh)(piece, bf16, s);
-    if (c.dweight && c.width) (c.aligned ? launch_dweight : launch_any_dweight)(piece, bf16, s);
+    if (c.dh && c.width) launch_dh(piece, plans.dh, bf16, s);
+    if (c.dweight && c.width) launch_dweight(piece, plans.dweight, bf16, s);
   }
   return status_of_launches();
 }
@@ -355,7 +383,8 @@ template <class Problem>
 size_t workspace_of(const Problem* p) {
   if (check(p) != TSENOR_OK) return 0;
   LossCall c = call_of(*p);
-  return lay_out(p->head, nullptr, c);
+  Plans plans = {};
+  return lay_out(p->head, nullptr, c, plans);
 }
 template <class Problem>
 int run(const Problem* p, void* workspace, size_t workspace_bytes, tsenor_stream_t stream) {

@@ -10,6 +10,8 @@
 // How many tokens count is known on the GPU only.  Grids are made for all of them, and workgroups without work end at once.
 #pragma once
 #include "layer.hpp"
+#include "loss_plan.hpp"
+#include "tile_loads.hpp"
 #include "tsenor_loss.h"
 
 namespace tsenor_dev {
@@ -35,9 +37,11 @@ struct LossCall {
   float2* sums;            // of each row and tile: an exponent of 2, the sum of 2^(z scale - exponent)
   void* dz;                // of the piece, dz_ld to a row, zeros behind the vocabulary
   float* dweight_sum;      // the head's gradient of the pieces so far (bf16 and more than one piece)
+  floatx4* parts;          // of tiles whose sum `splits` workgroups share
+  void* head;              // the head with rows of whole lines, where it has others
+  int splits;
   int states_ld, dz_ld;
-  int logits_tile, tile_n, tiles;  // kind of the tiles of the logits, words of one, tiles of a row
-  bool aligned;            // the head's rows are whole lines of 128 bytes that begin at multiples of 16
+  int tile_n, tiles;       // words of a tile of logits, tiles of a row
   // of the piece
   int first, rows;         // of `order`
   bool last;
@@ -50,15 +54,8 @@ __device__ __forceinline__ int rows_of(const LossCall& c) { return min(max(*c.co
 // that one, and steps of 2^-39 of it below.
 constexpr float kExpBits = 15.0f;
 
-// 64 rows of an operand to a unit of a tile: 4 (256 x 256), 2 (128 x 128) or 1 (64 x 128); 0: any rows, 128 x 128
-inline int tile_for(int64_t m) { return m > 128 ? 4 : m > 64 ? 2 : 1; }
-
-// the products with the tile kernels (heads that are `aligned`), and for any others
-void launch_logits(const LossCall& c, bool bf16, hipStream_t s);
-void launch_dh(const LossCall& c, bool bf16, hipStream_t s);
-void launch_dweight(const LossCall& c, bool bf16, hipStream_t s);
-void launch_any_logits(const LossCall& c, bool bf16, hipStream_t s);
-void launch_any_dh(const LossCall& c, bool bf16, hipStream_t s);
-void launch_any_dweight(const LossCall& c, bool bf16, hipStream_t s);
+void launch_logits(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
+void launch_dh(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
+void launch_dweight(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
 
 }  // namespace tsenor_dev

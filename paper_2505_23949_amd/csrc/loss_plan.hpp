@@ -1,0 +1,37 @@
+// Which tiles the products of the losses are made in, and how many workgroups share the sum of a tile: host code that needs no GPU.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "layer_plan.hpp"
+
+namespace tsenor_dev {
+
+struct ProductPlan {
+  Kind kind;  // kSmallTile (64 rows of a x 128 of b), kTile (128 x 128), kLargeTile (256 x 256)
+  int tiles_m, tiles_n, splits;
+  double us;  // estimated
+  size_t workspace;
+};
+
+// m rows of a, n of b, `blocks` of 128 bytes of the sum; `shared`: whether workgroups may share the sum of a tile
+inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool bf16, bool shared) {
+  ProductPlan best = {};
+  for (const Cost& c : {Cost{kSmallTile, 64, 128, bf16 ? 0.45 : 0.95, 3.0, kCus, false}, Cost{kTile, 128, 128, bf16 ? 0.60 : 1.85, 4.0, kCus, false},
+                        Cost{kLargeTile, 256, 256, bf16 ? 1.65 : 7.2, 8.0, kCus, false}}) {
+    const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n, tiles = tiles_m * tiles_n;
+    for (int64_t splits = 1; splits <= (shared ? std::min<int64_t>(32, std::max<int64_t>(blocks / 4, 1)) : 1); ++splits) {
+      if (splits > 1 && (splits - 1) * tiles >= kCus) break;
+      const int64_t rounds = (tiles * splits + kCus - 1) / kCus;
+      double us = (double)rounds * ((double)((blocks + splits - 1) / splits) * c.step + c.around);
+      const double parts = splits > 1 ? (double)(tiles * splits) * c.rows_m * c.rows_n * 4.0 : 0.0;
+      if (splits > 1) us += 3.0 + 2.0 * parts / 5.0e6;
+      if (best.us == 0.0 || us < best.us) best = {c.kind, (int)tiles_m, (int)tiles_n, (int)splits, us, (size_t)parts};
+    }
+  }
+  return best;
+}
+
+}  // namespace tsenor_dev

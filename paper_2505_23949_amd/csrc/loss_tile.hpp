@@ -7,7 +7,6 @@
 #include <algorithm>
 
 #include "loss.hpp"
-#include "tile_loads.hpp"
 
 namespace tsenor_dev {
 
@@ -135,6 +134,17 @@ __device__ __forceinline__ floatx16 multiply(const intx8& b, const intx8& a, flo
   }
 }
 
+// columns col .. col + 3 of a row of n
+__device__ __forceinline__ void store4(float* to, const floatx4& v, int col, int n) {
+  if (col + 4 <= n) {
+    __builtin_memcpy(to, &v, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < n) to[e] = v[e];
+  }
+}
+
 // What a lane holds of tile t of b and j of a: element 4 g + e is row 8 g + 4 q + e of the tile of b.  Columns 32 t + 16 p .. of a wave go
 // out (p: pair of g), 8 of them from each lane (bf16: the halves of the wave exchange fours first) or twice four (fp32).
 template <bool BF16, int USE>
@@ -144,15 +154,20 @@ __device__ __forceinline__ void write_gradient(const LossCall& c, int row, int64
   float* const sums = USE == kHead && BF16 ? c.dweight_sum : static_cast<float*>(c.dweight);
   if (USE == kHead && (c.first > 0 || !c.last)) {  // sums of several pieces, in fp32
     const auto add = [&](floatx4& v, int col) {
-      if (row < 0 || col >= n) return;
+      if (row < 0) return;
       float* const to = sums + at + col;
       if (c.first > 0) {
         float old[4];
-        __builtin_memcpy(old, to, 16);
+        if (col + 4 <= n) {
+          __builtin_memcpy(old, to, 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) old[e] = col + e < n ? to[e] : 0.0f;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += old[e];
       }
-      if (!BF16 || !c.last) __builtin_memcpy(to, &v, 16);
+      if (!BF16 || !c.last) store4(to, v, col, n);
     };
     add(lo, col + 4 * q);
     add(hi, col + 8 + 4 * q);
@@ -167,17 +182,26 @@ __device__ __forceinline__ void write_gradient(const LossCall& c, int row, int64
       w[k] = r[0], w[2 + k] = r[1];
     }
     col += 8 * q;
-    if (row >= 0 && col < n) __builtin_memcpy(static_cast<uint16_t*>(out) + at + col, w, 16);
-  } else {
-    if (row >= 0 && col + 4 * q < n) __builtin_memcpy(static_cast<float*>(out) + at + col + 4 * q, &lo, 16);
-    if (row >= 0 && col + 8 + 4 * q < n) __builtin_memcpy(static_cast<float*>(out) + at + col + 8 + 4 * q, &hi, 16);
+    uint16_t* const to = static_cast<uint16_t*>(out) + at + col;
+    if (row < 0) return;
+    if (col + 8 <= n) {
+      __builtin_memcpy(to, w, 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < n) to[e] = (uint16_t)(w[e / 2] >> (e % 2 * 16));
+    }
+  } else if (row >= 0) {
+    store4(static_cast<float*>(out) + at + col + 4 * q, lo, col + 4 * q, n);
+    store4(static_cast<float*>(out) + at + col + 8 + 4 * q, hi, col + 8 + 4 * q, n);
   }
 }
 
 template <int TN, int TM, int BUFFERS>
 constexpr int kGroupsPerCu = BUFFERS * TileShape<TN, TM>::kBuffer <= 80 * 1024 ? 2 : 1;
 
-template <bool BF16, int USE, int TN, int TM, int BUFFERS>
+// SPLIT: c.splits workgroups share the sum of a tile, and each leaves its part in c.parts.
+template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
 __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
   using Shape = TileShape<TN, TM>;
   constexpr int kSize = BF16 ? 2 : 4, kLine = 128 / kSize;
@@ -188,12 +212,15 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   const int piece = __builtin_amdgcn_readfirstlane(rows_of(c));
   const int m = USE == kHead ? c.vocab : piece, n = USE == kLogits ? c.vocab : c.width;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB;
-  if ((int)blockIdx.x >= tiles_m * tiles_n) return;
-  const int blocks = USE == kLogits ? c.states_ld / kLine : USE == kStates ? c.dz_ld / kLine : (piece + kLine - 1) / kLine;
-  if (USE == kHead && blocks == 0 && c.first > 0 && !c.last) return;
+  const int tiles = tiles_m * tiles_n, split = SPLIT ? (int)blockIdx.x / max(tiles, 1) : 0;
+  if (SPLIT ? split >= c.splits : (int)blockIdx.x >= tiles) return;
+  const int all_blocks = USE == kLogits ? c.states_ld / kLine : USE == kStates ? c.dz_ld / kLine : (piece + kLine - 1) / kLine;
+  if (USE == kHead && all_blocks == 0 && c.first > 0 && !c.last) return;
   int tile_m, tile_n;
-  tile_of((int)blockIdx.x, tiles_m, tiles_n, tile_m, tile_n);
-  const int m0 = tile_m * Shape::kRowsA, n0 = tile_n * Shape::kRowsB, last = blocks - 1;
+  tile_of((int)blockIdx.x - split * tiles, tiles_m, tiles_n, tile_m, tile_n);
+  const int first = SPLIT ? (int)((int64_t)all_blocks * split / c.splits) : 0;
+  const int last = (SPLIT ? (int)((int64_t)all_blocks * (split + 1) / c.splits) : all_blocks) - 1;
+  const int m0 = tile_m * Shape::kRowsA, n0 = tile_n * Shape::kRowsB;
 
   floatx16 sum[TN][TM];
 #pragma unroll
@@ -208,9 +235,9 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
     if constexpr (USE == kLogits)
       return LoaderAlong<TN, true>(c.weight, c.weight_ld * kSize, n0, n, lane, wave, lds_at);
     else if constexpr (USE == kStates)
-      return LoaderAcross<TN, kSize>(c.weight, c.weight_ld * kSize, n0, c.width * kSize, c.vocab, lane, wave, lds_at);
+      return LoaderAcross<TN, kSize>(c.weight, c.weight_ld * kSize, n0, c.states_ld * kSize, c.vocab, lane, wave, lds_at);
     else
-      return LoaderAcross<TN, kSize>(c.states, c.states_ld * kSize, n0, c.states_ld * kSize, blocks * kLine, lane, wave, lds_at);
+      return LoaderAcross<TN, kSize>(c.states, c.states_ld * kSize, n0, c.states_ld * kSize, all_blocks * kLine, lane, wave, lds_at);
   }();
   const uint32_t lds_a = lds_at + Shape::kRowsB * 128;
   const auto of_a = [&] {
@@ -235,11 +262,11 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   // (A block past the last is the last one again, which nothing uses.)
   constexpr int kEarly = BUFFERS > 2 ? Shape::kPieces / 2 : Shape::kPieces;  // loads of a block in the second half
   intx8 b[TN][2], a[TM][2];                                                   // tile, half of the columns
-  if (blocks > 0) {
+  if (first <= last) {
 #pragma unroll
     for (int k = 0; k < BUFFERS; ++k)
 #pragma unroll
-      for (int at = 0; at < (k == BUFFERS - 1 ? kEarly : Shape::kPieces); ++at) load(k * Shape::kBuffer, at, min(k, last));
+      for (int at = 0; at < (k == BUFFERS - 1 ? kEarly : Shape::kPieces); ++at) load(k * Shape::kBuffer, at, min(first + k, last));
     meet<(BUFFERS - 2) * Shape::kPieces + kEarly>();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -260,7 +287,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
 #define LATE(k) if constexpr (k >= kEarly) { load(old_buffer, k, ahead_of_old); TSENOR_IN_ORDER(); }
   constexpr int kPending = (BUFFERS - 2) * Shape::kPieces;  // loads of the blocks after the next
   int buffer = 0, next_buffer = Shape::kBuffer, old_buffer = (BUFFERS - 1) * Shape::kBuffer;
-  for (int block = 0; block <= last; ++block) {
+  for (int block = first; block <= last; ++block) {
     const int ahead = min(block + BUFFERS, last), ahead_of_old = min(block + BUFFERS - 1, last);
     TSENOR_IN_ORDER();
     if constexpr (TN == 4 && TM == 4) {
@@ -366,6 +393,15 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
       if (q == 0 && wave_n == 0 && m0 + row < m)
         c.sums[(int64_t)(m0 + row) * c.tiles + tile_n] = make_float2(largest[j], part[row] + part[Shape::kRowsA + row]);
     }
+  } else if constexpr (SPLIT) {
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          c.parts[((int64_t)blockIdx.x * (TM * TN * 4) + (j * TN + t) * 4 + g) * 256 + threadIdx.x] =
+              floatx4{sum[t][j][4 * g], sum[t][j][4 * g + 1], sum[t][j][4 * g + 2], sum[t][j][4 * g + 3]};
   } else {
     const float scale = c.largest_weight[1];
 #pragma unroll
@@ -385,15 +421,57 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   }
 }
 
-// the kernel with the tiles that suit the rows of a
+// adds the parts of a tile in their order: a workgroup for each tile and TN TM-th of it
+template <bool BF16, int USE, int TN, int TM>
+__global__ __launch_bounds__(256) void join_kernel(LossCall c) {
+  using Shape = TileShape<TN, TM>;
+  const int piece = rows_of(c), m = USE == kHead ? c.vocab : piece;
+  const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (c.width + Shape::kRowsB - 1) / Shape::kRowsB, tiles = tiles_m * tiles_n;
+  const int tile = (int)blockIdx.x / (TN * TM), j = (int)blockIdx.x / TN % TM, t = (int)blockIdx.x % TN;
+  if (tile >= tiles || (USE == kHead && piece == 0 && c.first > 0 && !c.last)) return;
+  int tile_m, tile_n;
+  tile_of(tile, tiles_m, tiles_n, tile_m, tile_n);
+  const floatx4* part = c.parts + ((int64_t)tile * (TM * TN * 4) + (j * TN + t) * 4) * 256 + threadIdx.x;
+  const int64_t step = (int64_t)tiles * (TM * TN * 4) * 256;
+  floatx4 v[4];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) v[g] = part[g * 256];
+#pragma unroll 4
+  for (int k = 1; k < c.splits; ++k)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) v[g] += part[k * step + g * 256];
+  const float scale = c.largest_weight[1];
+  const int wave = (int)threadIdx.x / kWave, row = tile_m * Shape::kRowsA + (wave / 2 * TM + j) * 32 + (int)threadIdx.x % 32;
+  const int64_t at = (int64_t)(row >= m ? 0 : USE == kStates ? c.order[c.first + row] : row) * c.width;
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    floatx4 lo, hi;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lo[e] = v[2 * p][e] * scale, hi[e] = v[2 * p + 1][e] * scale;
+    write_gradient<BF16, USE>(c, row < m ? row : -1, at, tile_n * Shape::kRowsB + (wave % 2 * TN + t) * 32 + 16 * p, lo, hi);
+  }
+}
+
+// the kernel with the tiles of a plan
+template <bool BF16, int USE, int TN, int TM, int BUFFERS>
+void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
+  const unsigned tiles = (unsigned)(plan.tiles_m * plan.tiles_n);
+  if constexpr (USE != kLogits)
+    if (plan.splits > 1) {
+      LossCall shared = c;
+      shared.splits = plan.splits;
+      tile_kernel<BF16, USE, TN, TM, BUFFERS, true><<<tiles * (unsigned)plan.splits, 256, 0, s>>>(shared);
+      join_kernel<BF16, USE, TN, TM><<<tiles * TN * TM, 256, 0, s>>>(shared);
+      return;
+    }
+  tile_kernel<BF16, USE, TN, TM, BUFFERS, false><<<tiles, 256, 0, s>>>(c);
+}
 template <bool BF16, int USE>
-void launch_tiles(const LossCall& c, hipStream_t s) {
-  const int64_t m = USE == kHead ? c.vocab : c.rows, n = USE == kLogits ? c.vocab : c.width;
-  const auto groups = [&](int tn, int tm) { return (unsigned)((m + 64 * tm - 1) / (64 * tm) * ((n + 64 * tn - 1) / (64 * tn))); };
-  switch (USE == kLogits ? c.logits_tile : tile_for(m)) {
-    case 4: tile_kernel<BF16, USE, 4, 4, 2><<<groups(4, 4), 256, 0, s>>>(c); break;
-    case 2: tile_kernel<BF16, USE, 2, 2, 4><<<groups(2, 2), 256, 0, s>>>(c); break;
-    default: tile_kernel<BF16, USE, 2, 1, 6><<<groups(2, 1), 256, 0, s>>>(c); break;
+void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
+  switch (plan.kind) {
+    case kLargeTile: launch_tiles<BF16, USE, 4, 4, 2>(c, plan, s); break;
+    case kTile: launch_tiles<BF16, USE, 2, 2, 4>(c, plan, s); break;
+    default: launch_tiles<BF16, USE, 2, 1, 6>(c, plan, s); break;
   }
 }
 
