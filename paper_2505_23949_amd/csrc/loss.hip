@@ -26,6 +26,32 @@ __device__ __forceinline__ float teacher_of(const LossCall& c, int64_t token, in
   return u * c.inverse_temperature;
 }
 
+// what is left of x (infinities and NaN have nothing left; the largest numbers round up to infinity, which they are then)
+__device__ __forceinline__ float remainder_of(float x, uint32_t rounded) {
+  return (rounded & kInfinityBits) == kInfinityBits ? 0.0f : x - __uint_as_float(rounded);
+}
+// 8 elements of a row of an operand as the products read it: bf16, or three planes whose sum they are
+template <bool BF16>
+__device__ __forceinline__ void store_planes(void* row, int ld, int c, const float (&x)[8]) {
+  if constexpr (BF16) {
+    store_row8<true>(row, c, ld, x);
+  } else {
+    float rest[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) rest[k] = x[k];
+#pragma unroll
+    for (int plane = 0; plane < 3; ++plane) {
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[k] = pack_bf16(rest[2 * k], rest[2 * k + 1]);
+        rest[2 * k] = remainder_of(rest[2 * k], w[k] << 16), rest[2 * k + 1] = remainder_of(rest[2 * k + 1], w[k] & 0xFFFF0000u);
+      }
+      __builtin_memcpy(static_cast<uint16_t*>(row) + plane * ld + c, w, 16);
+    }
+  }
+}
+
 // which tokens have an entry that takes part: a wave to a token
 __global__ __launch_bounds__(kThreads) void counts_kernel(LossCall c) {
   const int token = (int)blockIdx.x * (kThreads / kWave) + (int)threadIdx.x / kWave, lane = (int)threadIdx.x % kWave;
@@ -93,17 +119,17 @@ template <bool BF16>
 __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
   constexpr int kSize = BF16 ? 2 : 4;
   const int row = (int)blockIdx.x, rows = rows_of(c);
-  char* const state = static_cast<char*>(c.states) + (int64_t)row * c.states_ld * kSize;
+  uint16_t* const state = static_cast<uint16_t*>(c.states) + (int64_t)row * c.states_ld * (BF16 ? 1 : 3);
   float x[8] = {};
   if (row < rows) {
     const char* const h = static_cast<const char*>(c.h) + (int64_t)c.order[c.first + row] * c.h_ld * kSize;
     for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) {
       load_row8<BF16>(h, k, c.width, x);
-      store_row8<BF16>(state, k, c.states_ld, x);
+      store_planes<BF16>(state, c.states_ld, k, x);
     }
     return;
   }
-  for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) store_row8<BF16>(state, k, c.states_ld, x);
+  for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) store_planes<BF16>(state, c.states_ld, k, x);
   if (row >= c.rows) return;
   const int token = c.order[c.first + row];
   if (threadIdx.x == 0) {
@@ -117,14 +143,13 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
 
 // the head with rows of whole lines: a workgroup to a row
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void head_kernel(const void* weight, int64_t ld, int width, void* head, int head_ld) {
-  constexpr int kSize = BF16 ? 2 : 4;
-  const char* const from = static_cast<const char*>(weight) + (int64_t)blockIdx.x * ld * kSize;
-  char* const to = static_cast<char*>(head) + (int64_t)blockIdx.x * head_ld * kSize;
-  for (int k = (int)threadIdx.x * 8; k < head_ld; k += kThreads * 8) {
+__global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* head) {
+  const char* const from = static_cast<const char*>(c.weight) + (int64_t)blockIdx.x * c.weight_ld * (BF16 ? 2 : 4);
+  uint16_t* const to = head + (int64_t)blockIdx.x * c.head_ld;
+  for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) {
     float x[8];
-    load_row8<BF16>(from, k, width, x);
-    store_row8<BF16>(to, k, head_ld, x);
+    load_row8<BF16>(from, k, c.width, x);
+    store_planes<BF16>(to, c.states_ld, k, x);
   }
 }
 
@@ -158,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
     const bool valid = id >= 0 && id < c.vocab;
     float s = 0.0f;
     if (valid) {
-      const char* const h = static_cast<const char*>(c.states) + (int64_t)row * c.states_ld * kSize;
+      const char* const h = static_cast<const char*>(c.h) + (int64_t)token * c.h_ld * kSize;
       const char* const w = static_cast<const char*>(c.weight) + id * c.weight_ld * kSize;
       for (int k = lane * 8; k < c.width; k += kWave * 8) {
         float x[8], y[8];
@@ -213,29 +238,32 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
     dentry[i] = weight * (__builtin_amdgcn_exp2f(logits[i]) / total - p);
   }
   const float share = weight / total;
-  char* const dz = static_cast<char*>(c.dz) + (int64_t)row * c.dz_ld * kSize;
+  uint16_t* const dz = static_cast<uint16_t*>(c.dz) + (int64_t)row * c.dz_ld * (BF16 ? 1 : 3);
+  const char* const exps = static_cast<const char*>(c.exps) + (int64_t)row * c.dz_ld * kSize;
   for (int k = (int)threadIdx.x * 8; k < c.dz_ld; k += kThreads * 8) {
     const float scale = share * __builtin_amdgcn_exp2f(sums[k / c.tile_n].x - largest);
     float x[8];
     if constexpr (BF16) {
       _Float16 y[8];
-      __builtin_memcpy(y, dz + k * 2, 16);
+      __builtin_memcpy(y, exps + k * 2, 16);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = (float)y[e];
     } else {
-      __builtin_memcpy(x, dz + k * 4, 32);
+      __builtin_memcpy(x, exps + k * 4, 32);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = k + e < c.vocab ? x[e] * scale : 0.0f;
-    store_row8<BF16>(dz, k, c.dz_ld, x);
+    store_planes<BF16>(dz, c.dz_ld, k, x);
   }
   __syncthreads();
   for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
     if (words[i] < 0) continue;
-    if constexpr (BF16)
-      reinterpret_cast<uint16_t*>(dz)[words[i]] = (uint16_t)pack_bf16(dentry[i], 0.0f);
-    else
-      reinterpret_cast<float*>(dz)[words[i]] = dentry[i];
+    float rest = dentry[i];
+    for (int plane = 0; plane < (BF16 ? 1 : 3); ++plane) {
+      const uint32_t w = pack_bf16(rest, 0.0f);
+      dz[plane * c.dz_ld + words[i]] = (uint16_t)w;
+      rest = remainder_of(rest, w << 16);
+    }
   }
 }
 
@@ -301,21 +329,21 @@ struct Plans {
 // describes a call to the kernels; the workspace begins at `workspace` (which may be NULL to ask for its size alone)
 size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans) {
   const bool bf16 = p.dtype == TSENOR_BF16, gradients = p.dh_out || p.dweight_out;
-  const int64_t size = bf16 ? 2 : 4, line = 128 / size;
+  const int64_t size = bf16 ? 2 : 4, planes = bf16 ? 1 : 3, line = 64;
   c.h = p.h, c.weight = p.weight, c.h_ld = p.h_ld, c.weight_ld = p.weight_ld;
   c.dloss = p.dloss, c.loss = p.loss_out, c.lse = p.lse_out, c.dh = p.dh_out, c.dweight = p.dweight_out;
   c.tokens = (int)p.tokens, c.vocab = (int)p.vocab, c.width = (int)p.width;
   c.states_ld = (int)std::max(round_up(p.width, line), line), c.dz_ld = (int)round_up(p.vocab, line);
-  const int64_t row_bytes = gradients ? c.dz_ld * size : (p.vocab + 127) / 128 * 8 * 10;
+  const int64_t row_bytes = gradients ? c.dz_ld * (bf16 ? 2 : 10) : (p.vocab + 127) / 128 * 8 * 10;
   const int64_t most = std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows);
   const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
   c.rows = (int)std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
-  plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line, bf16, false);
-  if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line, bf16, true);
-  if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line, bf16, true);
+  plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line * (bf16 ? 1 : kPairs), false);
+  if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line * (bf16 ? 1 : kPairs), true);
+  if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), true);
   c.tile_n = plans.logits.kind == kLargeTile ? 256 : 128;
   c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
-  const bool whole = p.width && p.width % line == 0 && p.weight_ld * size % 16 == 0 && p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
+  const bool whole = bf16 && p.width && p.width % line == 0 && p.weight_ld * size % 16 == 0 && p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
   size_t at = 0;
   const auto take = [&](int64_t bytes) {
     char* const begin = workspace + at;
@@ -326,11 +354,13 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.largest_weight = reinterpret_cast<float*>(c.count + 1);
   c.order = reinterpret_cast<int*>(take(p.tokens * 4));
   c.counts = reinterpret_cast<uint8_t*>(c.teacher ? take(p.tokens) : nullptr);
-  c.states = take((int64_t)round_up(c.rows, line) * c.states_ld * size);
+  c.states = take((int64_t)round_up(c.rows, line) * c.states_ld * planes * 2);
   c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
-  c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * size) : nullptr;
+  c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * planes * 2) : nullptr;
+  c.exps = gradients && !bf16 ? take((int64_t)c.rows * c.dz_ld * 4) : c.dz;
   c.dweight_sum = bf16 && p.dweight_out && c.rows < p.tokens ? reinterpret_cast<float*>(take(p.vocab * p.width * 4)) : nullptr;
-  c.head = whole ? nullptr : take(p.vocab * c.states_ld * size);
+  c.head = whole ? p.weight : take(p.vocab * c.states_ld * planes * 2);
+  c.head_ld = whole ? p.weight_ld : c.states_ld * planes;
   c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max(plans.dh.workspace, plans.dweight.workspace)));
   return at;
 }
@@ -350,15 +380,14 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
   }
   if (c.teacher) counts_kernel<<<(unsigned)((c.tokens + 3) / 4), kThreads, 0, s>>>(c);
   order_kernel<<<1, kOrderThreads, 0, s>>>(c);
-  if (c.head) {
-    bf16 ? head_kernel<true><<<(unsigned)c.vocab, kThreads, 0, s>>>(c.weight, c.weight_ld, c.width, c.head, c.states_ld)
-         : head_kernel<false><<<(unsigned)c.vocab, kThreads, 0, s>>>(c.weight, c.weight_ld, c.width, c.head, c.states_ld);
-    c.weight = c.head, c.weight_ld = c.states_ld;
+  if (c.head != c.weight) {
+    uint16_t* const head = static_cast<uint16_t*>(const_cast<void*>(c.head));
+    bf16 ? head_kernel<true><<<(unsigned)c.vocab, kThreads, 0, s>>>(c, head) : head_kernel<false><<<(unsigned)c.vocab, kThreads, 0, s>>>(c, head);
   }
   for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
     LossCall piece = c;
     piece.rows = std::min(c.rows, c.tokens - c.first), piece.last = c.first + piece.rows == c.tokens;
-    const unsigned padded = (unsigned)round_up(piece.rows, bf16 ? 64 : 32);
+    const unsigned padded = (unsigned)round_up(piece.rows, 64);
     bf16 ? gather_kernel<true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false><<<padded, kThreads, 0, s>>>(piece);
     launch_logits(piece, plans.logits, bf16, s);
     bf16 ? rows_kernel<true><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece) : rows_kernel<false><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece);

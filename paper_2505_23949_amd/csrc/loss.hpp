@@ -33,13 +33,16 @@ struct LossCall {
   float* largest_weight;   // largest |dloss| of them (of the finite ones), and that over the temperature
   int* order;              // tokens that count, in order; the last ones left out
   uint8_t* counts;         // of a token, where that takes more than a look at its target
-  void* states;            // hidden states of the piece, states_ld to a row, zeros behind the width and the last row
+  // Rows of the operands of the products are whole lines of 128 bytes: one plane in bf16, or three for single precision (see loss_tile.hpp)
+  void* states;            // hidden states of the piece, states_ld to a row and plane, zeros behind the width and the last row
+  const void* head;        // the head (its own memory, where its rows are such lines), head_ld to a row
   float2* sums;            // of each row and tile: an exponent of 2, the sum of 2^(z scale - exponent)
-  void* dz;                // of the piece, dz_ld to a row, zeros behind the vocabulary
+  void* exps;              // exponentials of the piece, dz_ld to a row: fp16 in the memory of dz (bf16), or fp32
+  void* dz;                // of the piece, dz_ld to a row and plane, zeros behind the vocabulary
   float* dweight_sum;      // the head's gradient of the pieces so far (bf16 and more than one piece)
   floatx4* parts;          // of tiles whose sum `splits` workgroups share
-  void* head;              // the head with rows of whole lines, where it has others
   int splits;
+  int64_t head_ld;
   int states_ld, dz_ld;
   int tile_n, tiles;       // words of a tile of logits, tiles of a row
   // of the piece
@@ -53,6 +56,8 @@ __device__ __forceinline__ int rows_of(const LossCall& c) { return min(max(*c.co
 // An exponential is 2^15 for the largest of its row and tile: kept in fp16 (bf16 matrices) they then have 11 bits down to 2^-29 of
 // that one, and steps of 2^-39 of it below.
 constexpr float kExpBits = 15.0f;
+
+constexpr int kPairs = 6;  // of planes, that a product in single precision takes
 
 void launch_logits(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
 void launch_dh(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);

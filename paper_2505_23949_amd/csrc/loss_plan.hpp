@@ -16,11 +16,11 @@ struct ProductPlan {
   size_t workspace;
 };
 
-// m rows of a, n of b, `blocks` of 128 bytes of the sum; `shared`: whether workgroups may share the sum of a tile
-inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool bf16, bool shared) {
+// m rows of a, n of b, `blocks` of 64 columns of the sum; `shared`: whether workgroups may share the sum of a tile
+inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool shared) {
   ProductPlan best = {};
-  for (const Cost& c : {Cost{kSmallTile, 64, 128, bf16 ? 0.45 : 0.95, 3.0, kCus, false}, Cost{kTile, 128, 128, bf16 ? 0.60 : 1.85, 4.0, kCus, false},
-                        Cost{kLargeTile, 256, 256, bf16 ? 1.65 : 7.2, 8.0, kCus, false}}) {
+  for (const Cost& c : {Cost{kSmallTile, 64, 128, 0.45, 3.0, kCus, false}, Cost{kTile, 128, 128, 0.60, 4.0, kCus, false},
+                        Cost{kLargeTile, 256, 256, 1.65, 8.0, kCus, false}}) {
     const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n, tiles = tiles_m * tiles_n;
     for (int64_t splits = 1; splits <= (shared ? std::min<int64_t>(32, std::max<int64_t>(blocks / 4, 1)) : 1); ++splits) {
       if (splits > 1 && (splits - 1) * tiles >= kCus) break;

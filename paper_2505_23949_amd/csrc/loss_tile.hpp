@@ -12,22 +12,26 @@ namespace tsenor_dev {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef float floatx8 __attribute__((ext_vector_type(8)));
 
 enum Use { kLogits, kStates, kHead };
 
 // A workgroup of four waves, two by two, takes 64 TN rows of b (columns of the result) and 64 TM rows of a; a wave 32 TN x 32 TM results
 // in accumulators, of the 32 x 32 matrix instructions whose first operand is b: a lane holds four neighbouring columns of a row.
-// What 128 bytes of a row hold (64 columns of the sum in bf16, 32 in fp32) is a block; blocks come into a ring of BUFFERS in LDS by
-// loads that go there directly.
+// 64 columns of the sum, 128 bytes of a row, are a block; blocks come into a ring of BUFFERS in LDS by loads that go there directly.
 //   Along: 128 bytes of LDS to a row; piece c of 16 bytes of row r stands at place c ^ (r / 2 % 8), so that the lanes that LDS serves
 //   at a time take all banks.
-//   Across: a row of LDS holds one column of the sum for all rows of the operand.  In bf16, reads that transpose 4 x 16 values on the way
-//   give a lane four columns of the sum for its row; the 64-byte chunks of LDS rows k are exchanged by k % 4 (chunk c stands at
-//   c ^ (k % 4)), so that the four rows of such a read take different banks.  In fp32 a lane reads single values.
-//   The order of the columns in the sum is free as long as both operands agree on it: a lane of half q of the wave holds, of half h of a
-//   block, the 16 h' + 8 q .. (see `fetch`).
+//   Across: a row of LDS holds one column of the sum for all rows of the operand, and reads that transpose 4 x 16 values on the way give a
+//   lane four columns of the sum for its row; the 64-byte chunks of LDS rows k are exchanged by k % 4 (chunk c stands at c ^ (k % 4)),
+//   so that the four rows of such a read take different banks.
+//   The order of the columns in the sum is free as long as both operands agree on it: half q of a wave holds, of half h of a block, its
+//   columns 32 h + 16 q to 32 h + 16 q + 15.
+//
+// Single precision: x = x1 + x2 + x3 exactly, with x1 the nearest bf16 value to x, x2 to x - x1 and x3 the rest, and of the nine products of
+// two such sums six are made, x1 y1, x1 y2, x2 y1, x2 y2, x1 y3 and x3 y1; the others are below 2^-25 of x y.  bf16 products run 16 times as
+// fast as those of fp32, so six of them take 0.4 of one in fp32.  Rows of the operands then hold three planes one behind the other, and a
+// block of the sum is one of the six pairs of planes of 64 columns.
 template <int TN, int TM>
 struct TileShape {
   static constexpr int kRowsB = 64 * TN, kRowsA = 64 * TM;
@@ -35,68 +39,80 @@ struct TileShape {
   static constexpr int kPieces = 2 * TN + 2 * TM;          // loads that a wave makes for a block
 };
 
-// Loads a wave's share of 64 T rows of an operand.
+// Which planes of a and b block `block` of the sum takes, and which 64 columns of them.
+template <bool BF16>
+struct Place {
+  int plane_a, plane_b, at;
+  __device__ __forceinline__ Place(int block) {
+    if constexpr (BF16) {
+      plane_a = plane_b = 0, at = block;
+    } else {
+      const int pair = block % kPairs;
+      plane_a = 0x850 >> 2 * pair & 3, plane_b = 0x244 >> 2 * pair & 3, at = block / kPairs;  // 0 0 1 1 0 2 and 0 1 0 1 2 0
+    }
+  }
+};
+
+// Loads a wave's share of 64 T rows of an operand; `plane`: bytes from plane to plane of a row.
 // INTERLEAVED: row 32 t + r of each 32 T rows of LDS is row T r + t of memory, so that a lane gets T times as many neighbouring columns.
 template <int T, bool INTERLEAVED>
 struct LoaderAlong {
   intx4 from;
   uint32_t to;
-  int lane[2 * T];
-  __device__ __forceinline__ LoaderAlong(const void* p, int64_t ld_bytes, int first, int rows, int lane_id, int wave, uint32_t lds) {
+  int plane_bytes, lane[2 * T];
+  __device__ __forceinline__ LoaderAlong(const void* p, int64_t ld_bytes, int plane_bytes_, int first, int rows, int lane_id, int wave, uint32_t lds) {
     from = resource_of(static_cast<const char*>(p) + first * ld_bytes, min(64 * T, rows - first) * ld_bytes);
     to = lds + wave * 16 * T * 128;
+    plane_bytes = plane_bytes_;
 #pragma unroll
     for (int j = 0; j < 2 * T; ++j) {
       const int at = wave * 16 * T + 8 * j + lane_id / 8;
       const int row = INTERLEAVED ? at / (32 * T) * (32 * T) + at % 32 * T + at % (32 * T) / 32 : at;
-      lane[j] = min(row, rows - 1 - first) * (int)ld_bytes + (lane_id % 8 ^ at / 2 % 8) * 16;
+      lane[j] = (int)((uint32_t)min(row, rows - 1 - first) * (uint32_t)ld_bytes + (lane_id % 8 ^ at / 2 % 8) * 16);  // (32 bits, unsigned)
     }
   }
-  __device__ __forceinline__ void load(int buffer, int j, int block) const { load_to_lds(to + buffer + j * 1024, lane[j], from, block * 128); }
+  __device__ __forceinline__ void load(int buffer, int j, int plane, int at) const {
+    load_to_lds(to + buffer + j * 1024, lane[j], from, plane * plane_bytes + at * 128);
+  }
 };
 
-// `count` columns of the sum, `row_bytes` bytes of operand in each.  What lies past either end is read as something inside: past the
+// `count` columns of the sum, `plane_bytes` bytes of operand in each.  What lies past either end is read as something inside: past the
 // last column the other operand is zero, and past the last row nothing is written.
-template <int T, int SIZE>
+template <int T>
 struct LoaderAcross {
-  static constexpr int kRowBytes = 64 * T * SIZE, kAtOnce = 1024 / kRowBytes, kLine = 128 / SIZE;
-  static_assert(kRowBytes <= 1024);
+  static constexpr int kRowBytes = 128 * T, kAtOnce = 1024 / kRowBytes;
   const char* base;
-  int64_t ld_bytes, past;  // offset of the last 16 bytes
+  int64_t ld_bytes, past;  // past: offset of the last 16 bytes of a plane
   uint32_t to;
-  int lane, step;
-  __device__ __forceinline__ LoaderAcross(const void* p, int64_t ld_bytes_, int first, int row_bytes, int count, int lane_id, int wave, uint32_t lds) {
-    base = static_cast<const char*>(p), ld_bytes = ld_bytes_, past = (count - 1) * ld_bytes + row_bytes - 16;
+  int plane_bytes, lane, step;
+  __device__ __forceinline__ LoaderAcross(const void* p, int64_t ld_bytes_, int plane_bytes_, int first, int count, int lane_id, int wave, uint32_t lds) {
+    base = static_cast<const char*>(p), ld_bytes = ld_bytes_, plane_bytes = plane_bytes_, past = (count - 1) * ld_bytes + plane_bytes - 16;
     to = lds + wave * 1024;
-    const int k = wave * kAtOnce + lane_id * 16 / kRowBytes, at = lane_id * 16 % kRowBytes;
-    const int swap = SIZE == 4 ? 0 : kRowBytes >= 256 ? k % 4 : k / 2 % 2;
-    lane = k * (int)ld_bytes + min(first * SIZE + (at ^ swap * 64), row_bytes - 16);
+    const int k = wave * kAtOnce + lane_id * 16 / kRowBytes, at = lane_id * 16 % kRowBytes, swap = kRowBytes >= 256 ? k % 4 : k / 2 % 2;
+    lane = k * (int)ld_bytes + min(first * 2 + (at ^ swap * 64), plane_bytes - 16);
     step = 4 * kAtOnce * (int)ld_bytes;
   }
-  __device__ __forceinline__ void load(int buffer, int j, int block) const {
-    const int64_t begin = block * (kLine * ld_bytes);
+  __device__ __forceinline__ void load(int buffer, int j, int plane, int at) const {
+    const int64_t begin = at * (64 * ld_bytes);
     const int limit = (int)min(past - begin, (int64_t)INT32_MAX - 16), offset = min(j * step, limit);
-    load_to_lds(to + buffer + j * 4096, min(lane, limit - offset), resource_of(base + begin, (int64_t)limit + 16), offset);
+    load_to_lds(to + buffer + j * 4096, min(lane, limit - offset), resource_of(base + begin + plane * plane_bytes, (int64_t)limit + 16), offset);
   }
 };
 
 // Reads one of a wave's T tiles of 32 rows: half h of the sum's columns of a block.
-template <int T, bool ALONG, int SIZE>
+template <int T, bool ALONG>
 struct Reader {
-  static constexpr int kRowBytes = 64 * T * SIZE;
+  static constexpr int kRowBytes = 128 * T;
   int place[ALONG ? 2 : T];
   __device__ __forceinline__ Reader(int lane, int wave) {  // wave: which half of the 64 T rows
     const int r = lane % 32, q = lane / 32;
     if constexpr (ALONG) {
       place[0] = wave * 32 * T * 128 + r * 128 + ((2 * q) ^ (r / 2 % 8)) * 16;
       place[1] = wave * 32 * T * 128 + r * 128 + ((2 * q + 1) ^ (r / 2 % 8)) * 16;
-    } else if constexpr (SIZE == 2) {
+    } else {
       const int i = lane % 16, k = 16 * q + i / 4, swap = kRowBytes >= 256 ? k % 4 : k / 2 % 2;
 #pragma unroll
       for (int t = 0; t < T; ++t) place[t] = k * kRowBytes + ((wave * T + t) ^ swap) * 64 + lane / 16 % 2 * 32 + i % 4 * 8;
-    } else {
-#pragma unroll
-      for (int t = 0; t < T; ++t) place[t] = 8 * q * kRowBytes + (wave * 32 * T + 32 * t + r) * 4;
     }
   }
   __device__ __forceinline__ intx8 fetch(const uint8_t* rows, int t, int h) const {
@@ -104,34 +120,21 @@ struct Reader {
       const intx4 lo = *reinterpret_cast<const intx4*>(rows + t * 4096 + (place[0] ^ h * 64));
       const intx4 hi = *reinterpret_cast<const intx4*>(rows + t * 4096 + (place[1] ^ h * 64));
       return intx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    } else if constexpr (SIZE == 2) {
+    } else {
       typedef __attribute__((address_space(3))) shortx4* Lds;
-      typedef int intx2 __attribute__((ext_vector_type(2)));
       intx2 v[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         v[u] = __builtin_bit_cast(intx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(rows + place[t] + (32 * h + 4 * u) * kRowBytes)));
       return intx8{v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
-    } else {
-      intx8 v;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const int*>(rows + place[t] + (16 * h + u) * kRowBytes);
-      return v;
     }
   }
 };
 
-template <bool BF16>
 __device__ __forceinline__ floatx16 multiply(const intx8& b, const intx8& a, floatx16 sum) {
-  if constexpr (BF16) {
-    const intx4 b0 = {b[0], b[1], b[2], b[3]}, b1 = {b[4], b[5], b[6], b[7]}, a0 = {a[0], a[1], a[2], a[3]}, a1 = {a[4], a[5], a[6], a[7]};
-    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b0), __builtin_bit_cast(bf16x8, a0), sum, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b1), __builtin_bit_cast(bf16x8, a1), sum, 0, 0, 0);
-  } else {
-#pragma unroll
-    for (int u = 0; u < 8; ++u) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(b[u]), __int_as_float(a[u]), sum, 0, 0, 0);
-    return sum;
-  }
+  const intx4 b0 = {b[0], b[1], b[2], b[3]}, b1 = {b[4], b[5], b[6], b[7]}, a0 = {a[0], a[1], a[2], a[3]}, a1 = {a[4], a[5], a[6], a[7]};
+  sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b0), __builtin_bit_cast(bf16x8, a0), sum, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b1), __builtin_bit_cast(bf16x8, a1), sum, 0, 0, 0);
 }
 
 // columns col .. col + 3 of a row of n
@@ -204,7 +207,7 @@ constexpr int kGroupsPerCu = BUFFERS * TileShape<TN, TM>::kBuffer <= 80 * 1024 ?
 template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
 __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
   using Shape = TileShape<TN, TM>;
-  constexpr int kSize = BF16 ? 2 : 4, kLine = 128 / kSize;
+  constexpr int kPlanes = BF16 ? 1 : 3;
   constexpr bool kAlongB = USE == kLogits, kAlongA = USE != kHead;
   __shared__ __align__(1024) uint8_t lds[BUFFERS * Shape::kBuffer];
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -212,9 +215,10 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   const int piece = __builtin_amdgcn_readfirstlane(rows_of(c));
   const int m = USE == kHead ? c.vocab : piece, n = USE == kLogits ? c.vocab : c.width;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB;
-  const int tiles = tiles_m * tiles_n, split = SPLIT ? (int)blockIdx.x / max(tiles, 1) : 0;
-  if (SPLIT ? split >= c.splits : (int)blockIdx.x >= tiles) return;
-  const int all_blocks = USE == kLogits ? c.states_ld / kLine : USE == kStates ? c.dz_ld / kLine : (piece + kLine - 1) / kLine;
+  const int tiles = tiles_m * tiles_n;
+  if ((int)blockIdx.x >= tiles * (SPLIT ? c.splits : 1)) return;  // (of a piece without tokens that count, all of them)
+  const int split = SPLIT ? (int)blockIdx.x / tiles : 0;
+  const int all_blocks = (USE == kLogits ? c.states_ld / 64 : USE == kStates ? c.dz_ld / 64 : (piece + 63) / 64) * (BF16 ? 1 : kPairs);
   if (USE == kHead && all_blocks == 0 && c.first > 0 && !c.last) return;
   int tile_m, tile_n;
   tile_of((int)blockIdx.x - split * tiles, tiles_m, tiles_n, tile_m, tile_n);
@@ -231,31 +235,33 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
       for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.0f;
 
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+  const int states = c.states_ld * 2, dz = c.dz_ld * 2;  // bytes of a row of a plane (of the head: as of the states)
   const auto of_b = [&] {
     if constexpr (USE == kLogits)
-      return LoaderAlong<TN, true>(c.weight, c.weight_ld * kSize, n0, n, lane, wave, lds_at);
+      return LoaderAlong<TN, true>(c.head, c.head_ld * 2, states, n0, n, lane, wave, lds_at);
     else if constexpr (USE == kStates)
-      return LoaderAcross<TN, kSize>(c.weight, c.weight_ld * kSize, n0, c.states_ld * kSize, c.vocab, lane, wave, lds_at);
+      return LoaderAcross<TN>(c.head, c.head_ld * 2, states, n0, c.vocab, lane, wave, lds_at);
     else
-      return LoaderAcross<TN, kSize>(c.states, c.states_ld * kSize, n0, c.states_ld * kSize, all_blocks * kLine, lane, wave, lds_at);
+      return LoaderAcross<TN>(c.states, (int64_t)states * kPlanes, states, n0, (piece + 63) / 64 * 64, lane, wave, lds_at);
   }();
   const uint32_t lds_a = lds_at + Shape::kRowsB * 128;
   const auto of_a = [&] {
     if constexpr (USE == kLogits)
-      return LoaderAlong<TM, false>(c.states, c.states_ld * kSize, m0, m, lane, wave, lds_a);
+      return LoaderAlong<TM, false>(c.states, (int64_t)states * kPlanes, states, m0, m, lane, wave, lds_a);
     else if constexpr (USE == kStates)
-      return LoaderAlong<TM, false>(c.dz, (int64_t)c.dz_ld * kSize, m0, m, lane, wave, lds_a);
+      return LoaderAlong<TM, false>(c.dz, (int64_t)dz * kPlanes, dz, m0, m, lane, wave, lds_a);
     else
-      return LoaderAcross<TM, kSize>(c.dz, (int64_t)c.dz_ld * kSize, m0, c.dz_ld * kSize, piece, lane, wave, lds_a);
+      return LoaderAcross<TM>(c.dz, (int64_t)dz * kPlanes, dz, m0, piece, lane, wave, lds_a);
   }();
   const auto load = [&](int buffer, int k, int block) {
+    const Place<BF16> place(block);
     if (k < 2 * TN)
-      of_b.load(buffer, k, block);
+      of_b.load(buffer, k, place.plane_b, place.at);
     else
-      of_a.load(buffer, k - 2 * TN, block);
+      of_a.load(buffer, k - 2 * TN, place.plane_a, place.at);
   };
-  const Reader<TN, kAlongB, kSize> read_b(lane, wave_n);
-  const Reader<TM, kAlongA, kSize> read_a(lane, wave_m);
+  const Reader<TN, kAlongB> read_b(lane, wave_n);
+  const Reader<TM, kAlongA> read_a(lane, wave_m);
   const uint8_t *const rows_b = lds, *const rows_a = lds + Shape::kRowsB * 128;
 
   // With more than two buffers the loads of a block are spread over the second half of a step and the first of the next.
@@ -278,7 +284,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
 // The instructions of a step stand in the order in which they are issued: reads of LDS, loads and multiplications are spread evenly.
 // (The statement behind each multiplication does nothing but keep it from being moved past the next.)
 #define MULTIPLY(i, j, h)                               \
-  sum[i][j] = multiply<BF16>(b[i][h], a[j][h], sum[i][j]); \
+  sum[i][j] = multiply(b[i][h], a[j][h], sum[i][j]); \
   asm volatile("" : "+a"(sum[i][j]));                   \
   TSENOR_IN_ORDER();
 #define FETCH_B(buffer, t, h) b[t][h] = read_b.fetch(rows_b + buffer, t, h); TSENOR_IN_ORDER();
@@ -371,15 +377,15 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
             v += x[e * TN + t];
           }
         const int col = col0 + 8 * TN * g;
-        if (c.dz && m0 + row < m && col < c.dz_ld) {
+        if (c.exps && m0 + row < m && col < c.dz_ld) {
           if constexpr (BF16) {
             uint32_t w[2 * TN];
 #pragma unroll
             for (int k = 0; k < 2 * TN; ++k)
               w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{x[2 * k], x[2 * k + 1]}, halfx2));
-            __builtin_memcpy(__builtin_assume_aligned(static_cast<uint16_t*>(c.dz) + at + col, 16), w, 8 * TN);
+            __builtin_memcpy(__builtin_assume_aligned(static_cast<uint16_t*>(c.exps) + at + col, 16), w, 8 * TN);
           } else {
-            __builtin_memcpy(__builtin_assume_aligned(static_cast<float*>(c.dz) + at + col, 16), x, 16 * TN);
+            __builtin_memcpy(__builtin_assume_aligned(static_cast<float*>(c.exps) + at + col, 16), x, 16 * TN);
           }
         }
       }
