@@ -158,11 +158,26 @@ template <bool BF16>
 __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
   constexpr int kSize = BF16 ? 2 : 4;
   constexpr int kWaves = kThreads / kWave;
-  __shared__ float part[kWaves], logits[kMaxEntries], q[kMaxEntries], dentry[kMaxEntries];
+  __shared__ float part[kWaves], dots[kMaxEntries], logits[kMaxEntries], q[kMaxEntries], dentry[kMaxEntries];
   __shared__ int words[kMaxEntries];
   const int row = (int)blockIdx.x, lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
   if (row >= rows_of(c)) return;
-  const int token = c.order[c.first + row];
+  const int token = c.count ? c.order[c.first + row] : c.first + row;
+  if (!c.count) {
+    bool any = false;
+    if (c.teacher) {
+      for (int i = (int)threadIdx.x; i < c.k; i += kThreads) any |= teacher_of(c, token, i) != -__builtin_inff();
+    } else {
+      any = c.ids[token] >= 0 && c.ids[token] < c.vocab;
+    }
+    if (!__syncthreads_or(any)) {
+      if (threadIdx.x == 0) {
+        c.loss[token] = 0.0f;
+        if (c.lse) c.lse[token] = 0.0f;
+      }
+      return;
+    }
+  }
   const float2* const sums = c.sums + (int64_t)row * c.tiles;
 
   float largest = -__builtin_inff();
@@ -177,15 +192,17 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
   total = wave_sum(total);
   if (lane == 0) part[wave] = total;
 
-  // entries: a wave to each in turn
-  for (int i = wave; i < c.k; i += kWaves) {
+  // entries: a wave to each in turn, the only one of a token for all four
+  const int waves = c.k == 1 ? kWaves : 1;
+  for (int i = c.k == 1 ? 0 : wave; i < c.k; i += kWaves) {
     const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
     const bool valid = id >= 0 && id < c.vocab;
     float s = 0.0f;
     if (valid) {
       const char* const h = static_cast<const char*>(c.h) + (int64_t)token * c.h_ld * kSize;
       const char* const w = static_cast<const char*>(c.weight) + id * c.weight_ld * kSize;
-      for (int k = lane * 8; k < c.width; k += kWave * 8) {
+#pragma unroll 2
+      for (int k = (wave % waves * kWave + lane) * 8; k < c.width; k += waves * kWave * 8) {
         float x[8], y[8];
         load_row8<BF16>(h, k, c.width, x);
         load_row8<BF16>(w, k, c.width, y);
@@ -194,14 +211,20 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
       }
     }
     s = wave_sum(s);
-    if (lane == 0) logits[i] = fmaf(s, c.scale, -largest), words[i] = valid ? (int)id : -1;
+    if (lane == 0) {
+      dots[waves == 1 ? i : wave] = s;
+      words[i] = valid ? (int)id : -1;
+    }
   }
+  __syncthreads();
+  for (int i = (int)threadIdx.x; i < c.k; i += kThreads)
+    logits[i] = fmaf(waves == 1 ? dots[i] : dots[0] + dots[1] + dots[2] + dots[3], c.scale, -largest);
   __syncthreads();
   // from here on exponents of 2, counted from `largest`; lse is what they are all divided by
   total = part[0] + part[1] + part[2] + part[3];
   const float lse = log2f(total);
 
-  const float unit = c.largest_weight[0], weight = c.dloss ? (unit > 0.0f ? c.dloss[token] / unit : c.dloss[token]) : 1.0f;
+  const float unit = c.dz ? c.largest_weight[0] : 1.0f, weight = c.dloss ? (unit > 0.0f ? c.dloss[token] / unit : c.dloss[token]) : 1.0f;
   if (wave == 0) {
     float loss;
     if (!c.teacher) {
@@ -334,14 +357,14 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.dloss = p.dloss, c.loss = p.loss_out, c.lse = p.lse_out, c.dh = p.dh_out, c.dweight = p.dweight_out;
   c.tokens = (int)p.tokens, c.vocab = (int)p.vocab, c.width = (int)p.width;
   c.states_ld = (int)std::max(round_up(p.width, line), line), c.dz_ld = (int)round_up(p.vocab, line);
-  const int64_t row_bytes = gradients ? c.dz_ld * (bf16 ? 2 : 10) : (p.vocab + 127) / 128 * 8 * 10;
+  const int64_t row_bytes = gradients ? c.dz_ld * (bf16 ? 2 : 10) : (p.vocab + 63) / 64 * 8 * 10;
   const int64_t most = std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows);
   const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
   c.rows = (int)std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
   plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line * (bf16 ? 1 : kPairs), false);
   if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line * (bf16 ? 1 : kPairs), true);
   if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), true);
-  c.tile_n = plans.logits.kind == kLargeTile ? 256 : 128;
+  c.tile_n = plans.logits.kind == kLargeTile ? 128 : 64;
   c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
   const bool whole = bf16 && p.width && p.width % line == 0 && p.weight_ld * size % 16 == 0 && p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
   size_t at = 0;
@@ -350,10 +373,17 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
     at += (size_t)round_up(bytes, 256);
     return begin;
   };
+  // A tile has 64 rows at the least: up to there, rows of tokens that are left out cost nothing, and the states are read where they are.
+  if (!gradients && whole && p.tokens <= 64 && p.h_ld * size % 16 == 0 && p.h_ld <= kMaxTileLd && aligned_to(p.h, 16)) {
+    c.states = const_cast<void*>(p.h), c.states_row = p.h_ld, c.head = p.weight, c.head_ld = p.weight_ld;
+    c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
+    return at;
+  }
   c.count = reinterpret_cast<int*>(take(12));
   c.largest_weight = reinterpret_cast<float*>(c.count + 1);
   c.order = reinterpret_cast<int*>(take(p.tokens * 4));
   c.counts = reinterpret_cast<uint8_t*>(c.teacher ? take(p.tokens) : nullptr);
+  c.states_row = c.states_ld * planes;
   c.states = take((int64_t)round_up(c.rows, line) * c.states_ld * planes * 2);
   c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
   c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * planes * 2) : nullptr;
@@ -376,6 +406,14 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     if (p.lse_out) launch_zero(p.lse_out, p.tokens, false, s);
     if (p.dh_out) launch_zero(p.dh_out, p.tokens * p.width, bf16, s);
     if (p.dweight_out) launch_zero(p.dweight_out, p.vocab * p.width, bf16, s);
+    return status_of_launches();
+  }
+  if (!c.count) {
+    for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
+      c.rows = std::min(c.rows, c.tokens - c.first);
+      launch_logits(c, plans.logits, bf16, s);
+      bf16 ? rows_kernel<true><<<(unsigned)c.rows, kThreads, 0, s>>>(c) : rows_kernel<false><<<(unsigned)c.rows, kThreads, 0, s>>>(c);
+    }
     return status_of_launches();
   }
   if (c.teacher) counts_kernel<<<(unsigned)((c.tokens + 3) / 4), kThreads, 0, s>>>(c);

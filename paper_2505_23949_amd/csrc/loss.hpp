@@ -29,7 +29,7 @@ struct LossCall {
   void *dh, *dweight;
   int tokens, vocab, width;
   // workspace
-  int* count;              // tokens that count
+  int* count;              // tokens that count; NULL: the rows are the tokens in their order, those left out among them
   float* largest_weight;   // largest |dloss| of them (of the finite ones), and that over the temperature
   int* order;              // tokens that count, in order; the last ones left out
   uint8_t* counts;         // of a token, where that takes more than a look at its target
@@ -42,16 +42,16 @@ struct LossCall {
   float* dweight_sum;      // the head's gradient of the pieces so far (bf16 and more than one piece)
   floatx4* parts;          // of tiles whose sum `splits` workgroups share
   int splits;
-  int64_t head_ld;
+  int64_t head_ld, states_row;  // states_row: elements from row to row of the states
   int states_ld, dz_ld;
-  int tile_n, tiles;       // words of a tile of logits, tiles of a row
+  int tile_n, tiles;       // words of a wave's part of a tile of logits, such parts of a row
   // of the piece
   int first, rows;         // of `order`
   bool last;
 };
 
 // rows of the piece that there are
-__device__ __forceinline__ int rows_of(const LossCall& c) { return min(max(*c.count - c.first, 0), c.rows); }
+__device__ __forceinline__ int rows_of(const LossCall& c) { return c.count ? min(max(*c.count - c.first, 0), c.rows) : c.rows; }
 
 // An exponential is 2^15 for the largest of its row and tile: kept in fp16 (bf16 matrices) they then have 11 bits down to 2^-29 of
 // that one, and steps of 2^-39 of it below.

@@ -10,7 +10,7 @@
 namespace tsenor_dev {
 
 struct ProductPlan {
-  Kind kind;  // kSmallTile (64 rows of a x 128 of b), kTile (128 x 128), kLargeTile (256 x 256)
+  Kind kind;  // kSmallTile (64 rows of a x 128 of b), kTile and kTilePairs (128 x 128), kWideTile (256 x 128), kLargeTile (256 x 256)
   int tiles_m, tiles_n, splits;
   double us;  // estimated
   size_t workspace;
@@ -18,15 +18,20 @@ struct ProductPlan {
 
 // m rows of a, n of b, `blocks` of 64 columns of the sum; `shared`: whether workgroups may share the sum of a tile
 inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool shared) {
-  ProductPlan best = {};
-  for (const Cost& c : {Cost{kSmallTile, 64, 128, 0.45, 3.0, kCus, false}, Cost{kTile, 128, 128, 0.60, 4.0, kCus, false},
-                        Cost{kLargeTile, 256, 256, 1.65, 8.0, kCus, false}}) {
+  ProductPlan best = {kSmallTile, 0, 0, 1, 0.0, 0};
+  if (m == 0 || n == 0) return best;
+  for (const Cost& c : {Cost{kSmallTile, 64, 128, 0.42, 3.0, kCus, false}, Cost{kTile, 128, 128, 0.585, 4.0, kCus, false},
+                        Cost{kTilePairs, 128, 128, 1.085, 4.5, 2 * kCus, true}, Cost{kWideTile, 256, 128, 0.86, 6.0, kCus, false},
+                        Cost{kLargeTile, 256, 256, 1.556, 9.0, kCus, false}}) {
     const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n, tiles = tiles_m * tiles_n;
     for (int64_t splits = 1; splits <= (shared ? std::min<int64_t>(32, std::max<int64_t>(blocks / 4, 1)) : 1); ++splits) {
-      if (splits > 1 && (splits - 1) * tiles >= kCus) break;
-      const int64_t rounds = (tiles * splits + kCus - 1) / kCus;
-      double us = (double)rounds * ((double)((blocks + splits - 1) / splits) * c.step + c.around);
-      const double parts = splits > 1 ? (double)(tiles * splits) * c.rows_m * c.rows_n * 4.0 : 0.0;
+      if (splits > 1 && (splits - 1) * tiles >= c.at_once) break;
+      const double steps = (double)((blocks + splits - 1) / splits) * c.step;
+      const int64_t groups = tiles * splits, rounds = groups / c.at_once, rest = groups % c.at_once;
+      // (the last round: fewer workgroups have more of the memory and of the power each; of two on a CU, one alone takes 0.7 of the time)
+      const double fill = c.fluid ? (rest <= kCus ? 0.7 : 1.0) : 0.75 + 0.25 * (double)rest / c.at_once;
+      double us = (double)rounds * (steps + c.around) + (rest ? steps * fill + c.around : 0.0);
+      const double parts = splits > 1 ? (double)groups * c.rows_m * c.rows_n * 4.0 : 0.0;
       if (splits > 1) us += 3.0 + 2.0 * parts / 5.0e6;
       if (best.us == 0.0 || us < best.us) best = {c.kind, (int)tiles_m, (int)tiles_n, (int)splits, us, (size_t)parts};
     }

@@ -247,7 +247,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   const uint32_t lds_a = lds_at + Shape::kRowsB * 128;
   const auto of_a = [&] {
     if constexpr (USE == kLogits)
-      return LoaderAlong<TM, false>(c.states, (int64_t)states * kPlanes, states, m0, m, lane, wave, lds_a);
+      return LoaderAlong<TM, false>(c.states, c.states_row * 2, states, m0, m, lane, wave, lds_a);
     else if constexpr (USE == kStates)
       return LoaderAlong<TM, false>(c.dz, (int64_t)dz * kPlanes, dz, m0, m, lane, wave, lds_a);
     else
@@ -278,6 +278,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
     for (int h = 0; h < 2; ++h) {
       b[0][h] = read_b.fetch(rows_b, 0, h), a[0][h] = read_a.fetch(rows_a, 0, h);
       if constexpr (TN == 4) b[1][h] = read_b.fetch(rows_b, 1, h);
+      if constexpr (TN == 2 && TM == 4) a[1][h] = read_a.fetch(rows_a, 1, h);
     }
   }
 
@@ -311,6 +312,14 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
       MULTIPLY(2, 0, 1) FETCH_B(next_buffer, 0, 1) LOAD(10) MULTIPLY(3, 0, 1) FETCH_B(next_buffer, 1, 1) LOAD(11)
       MULTIPLY(2, 1, 0) FETCH_A(next_buffer, 0, 0) LOAD(12) MULTIPLY(3, 1, 0) FETCH_A(next_buffer, 0, 1) LOAD(13)
       MULTIPLY(2, 1, 1) LOAD(14) MULTIPLY(3, 1, 1) LOAD(15)
+    } else if constexpr (TN == 2 && TM == 4) {
+      MULTIPLY(0, 0, 0) FETCH_B(buffer, 1, 0) MULTIPLY(0, 1, 0) FETCH_B(buffer, 1, 1) LATE(6) MULTIPLY(0, 0, 1) FETCH_A(buffer, 2, 0) LATE(7)
+      MULTIPLY(0, 1, 1) FETCH_A(buffer, 2, 1) LATE(8) MULTIPLY(1, 0, 0) FETCH_A(buffer, 3, 0) LATE(9) MULTIPLY(1, 1, 0) FETCH_A(buffer, 3, 1) LATE(10)
+      MULTIPLY(1, 0, 1) LATE(11) MULTIPLY(1, 1, 1)
+      meet<kPending>();
+      MULTIPLY(0, 2, 0) LOAD(0) FETCH_A(next_buffer, 0, 0) MULTIPLY(0, 3, 0) LOAD(1) MULTIPLY(0, 2, 1) LOAD(2) FETCH_A(next_buffer, 0, 1)
+      MULTIPLY(0, 3, 1) LOAD(3) MULTIPLY(1, 2, 0) LOAD(4) FETCH_B(next_buffer, 0, 0)
+      MULTIPLY(1, 3, 0) LOAD(5) FETCH_B(next_buffer, 0, 1) MULTIPLY(1, 2, 1) FETCH_A(next_buffer, 1, 0) MULTIPLY(1, 3, 1) FETCH_A(next_buffer, 1, 1)
     } else if constexpr (TN == 2 && TM == 2) {
       MULTIPLY(0, 0, 0) FETCH_A(buffer, 1, 0) FETCH_A(buffer, 1, 1) LATE(4) MULTIPLY(0, 0, 1) FETCH_B(buffer, 1, 0) FETCH_B(buffer, 1, 1) LATE(5)
       MULTIPLY(0, 1, 0) LATE(6) LATE(7) MULTIPLY(0, 1, 1)
@@ -335,36 +344,29 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   meet<0>();  // (no load into LDS outlives the workgroup)
 
   if constexpr (USE == kLogits) {
-    // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b
-    float* const part = reinterpret_cast<float*>(lds);  // [2][kRowsA]
-    const int col0 = n0 + wave_n * 32 * TN + 4 * TN * q;
-    const bool whole = n0 + Shape::kRowsB <= n;
-    float largest[TM];
+    // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b.  The sums of a row are
+    // of those 32 TN columns: no wave waits for another.
+    const int wave_col = n0 + wave_n * 32 * TN, col0 = wave_col + 4 * TN * q;
+    if (wave_col + 32 * TN > n) {
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
+    }
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
-      float v = -__builtin_inff();
+      const int row = m0 + (wave_m * TM + j) * 32 + r;
+      const int64_t at = (int64_t)row * c.dz_ld;
+      float largest = -__builtin_inff();
 #pragma unroll
       for (int t = 0; t < TN; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (!whole && col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
-          v = fmaxf(v, sum[t][j][e]);
-        }
-      v = fmaxf(v, lane_xor<32>(v));
-      if (q == 0) part[wave_n * Shape::kRowsA + (wave_m * TM + j) * 32 + r] = v;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int row = (wave_m * TM + j) * 32 + r;
-      largest[j] = fmaxf(part[row], part[Shape::kRowsA + row]) * c.scale - kExpBits;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int row = (wave_m * TM + j) * 32 + r;
-      const float base = largest[j] == -__builtin_inff() ? 0.0f : largest[j];
-      const int64_t at = (int64_t)(m0 + row) * c.dz_ld;
+        for (int e = 0; e < 16; ++e) largest = fmaxf(largest, sum[t][j][e]);
+      largest = fmaxf(largest, lane_xor<32>(largest)) * c.scale - kExpBits;
+      const float base = largest == -__builtin_inff() ? 0.0f : largest;
       float v = 0.0f;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
             v += x[e * TN + t];
           }
         const int col = col0 + 8 * TN * g;
-        if (c.exps && m0 + row < m && col < c.dz_ld) {
+        if (c.exps && row < m && col < c.dz_ld) {
           if constexpr (BF16) {
             uint32_t w[2 * TN];
 #pragma unroll
@@ -390,14 +392,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
         }
       }
       v += lane_xor<32>(v);
-      if (q == 0) part[wave_n * Shape::kRowsA + row] = v;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int row = (wave_m * TM + j) * 32 + r;
-      if (q == 0 && wave_n == 0 && m0 + row < m)
-        c.sums[(int64_t)(m0 + row) * c.tiles + tile_n] = make_float2(largest[j], part[row] + part[Shape::kRowsA + row]);
+      if (q == 0 && row < m && wave_col < n) c.sums[(int64_t)row * c.tiles + wave_col / (32 * TN)] = make_float2(largest, v);
     }
   } else if constexpr (SPLIT) {
 #pragma unroll
@@ -476,7 +471,9 @@ template <bool BF16, int USE>
 void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
   switch (plan.kind) {
     case kLargeTile: launch_tiles<BF16, USE, 4, 4, 2>(c, plan, s); break;
+    case kWideTile: launch_tiles<BF16, USE, 2, 4, 3>(c, plan, s); break;
     case kTile: launch_tiles<BF16, USE, 2, 2, 4>(c, plan, s); break;
+    case kTilePairs: launch_tiles<BF16, USE, 2, 2, 2>(c, plan, s); break;
     default: launch_tiles<BF16, USE, 2, 1, 6>(c, plan, s); break;
   }
 }
