@@ -141,6 +141,39 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
       store_row8<BF16>(static_cast<char*>(c.dh) + (int64_t)token * c.width * kSize, k, c.width, x);
 }
 
+// the entries of a row by word, and where those of each part of a tile begin: a workgroup to a row
+__global__ __launch_bounds__(kThreads) void sort_kernel(LossCall c) {
+  static_assert(kThreads == kMaxEntries);
+  __shared__ uint32_t keys[kMaxEntries], sorted[kMaxEntries];
+  const int row = (int)blockIdx.x, i = (int)threadIdx.x;
+  if (row >= rows_of(c)) return;
+  const int token = c.order[c.first + row];
+  if (i < c.k) {
+    const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
+    keys[i] = id < 0 || id >= c.vocab ? UINT32_MAX - 255 + i : (uint32_t)id << 8 | i;
+  }
+  __syncthreads();
+  if (i < c.k) {
+    int rank = 0;
+    for (int j = 0; j < c.k; ++j) rank += keys[j] < keys[i];
+    sorted[rank] = keys[i];
+    c.sorted[(int64_t)row * c.k + rank] = keys[i];
+  }
+  __syncthreads();
+  for (int t = i; t <= c.tiles; t += kThreads) {
+    const uint32_t first = (uint32_t)min(t * c.tile_n, c.vocab) << 8;
+    int lo = 0, hi = c.k;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (sorted[mid] < first)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    c.begins[(int64_t)row * (c.tiles + 1) + t] = (uint16_t)lo;
+  }
+}
+
 // the head with rows of whole lines: a workgroup to a row
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* head) {
@@ -193,32 +226,41 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
   if (lane == 0) part[wave] = total;
 
   // entries: a wave to each in turn, the only one of a token for all four
-  const int waves = c.k == 1 ? kWaves : 1;
-  for (int i = c.k == 1 ? 0 : wave; i < c.k; i += kWaves) {
-    const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
-    const bool valid = id >= 0 && id < c.vocab;
-    float s = 0.0f;
-    if (valid) {
-      const char* const h = static_cast<const char*>(c.h) + (int64_t)token * c.h_ld * kSize;
-      const char* const w = static_cast<const char*>(c.weight) + id * c.weight_ld * kSize;
+  if (c.dots) {
+    for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
+      const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
+      const bool valid = id >= 0 && id < c.vocab;
+      words[i] = valid ? (int)id : -1;
+      logits[i] = valid ? fmaf(c.dots[(int64_t)row * c.k + i], c.scale, -largest) : 0.0f;
+    }
+  } else {
+    const int waves = c.k == 1 ? kWaves : 1;
+    for (int i = c.k == 1 ? 0 : wave; i < c.k; i += kWaves) {
+      const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
+      const bool valid = id >= 0 && id < c.vocab;
+      float s = 0.0f;
+      if (valid) {
+        const char* const h = static_cast<const char*>(c.h) + (int64_t)token * c.h_ld * kSize;
+        const char* const w = static_cast<const char*>(c.weight) + id * c.weight_ld * kSize;
 #pragma unroll 2
-      for (int k = (wave % waves * kWave + lane) * 8; k < c.width; k += waves * kWave * 8) {
-        float x[8], y[8];
-        load_row8<BF16>(h, k, c.width, x);
-        load_row8<BF16>(w, k, c.width, y);
+        for (int k = (wave % waves * kWave + lane) * 8; k < c.width; k += waves * kWave * 8) {
+          float x[8], y[8];
+          load_row8<BF16>(h, k, c.width, x);
+          load_row8<BF16>(w, k, c.width, y);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
+          for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
+        }
+      }
+      s = wave_sum(s);
+      if (lane == 0) {
+        dots[waves == 1 ? i : wave] = s;
+        words[i] = valid ? (int)id : -1;
       }
     }
-    s = wave_sum(s);
-    if (lane == 0) {
-      dots[waves == 1 ? i : wave] = s;
-      words[i] = valid ? (int)id : -1;
-    }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < c.k; i += kThreads)
+      logits[i] = fmaf(waves == 1 ? dots[i] : dots[0] + dots[1] + dots[2] + dots[3], c.scale, -largest);
   }
-  __syncthreads();
-  for (int i = (int)threadIdx.x; i < c.k; i += kThreads)
-    logits[i] = fmaf(waves == 1 ? dots[i] : dots[0] + dots[1] + dots[2] + dots[3], c.scale, -largest);
   __syncthreads();
   // from here on exponents of 2, counted from `largest`; lse is what they are all divided by
   total = part[0] + part[1] + part[2] + part[3];
@@ -386,6 +428,12 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.states_row = c.states_ld * planes;
   c.states = take((int64_t)round_up(c.rows, line) * c.states_ld * planes * 2);
   c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
+  // Entries: the rows kernel reads their rows of the head at 4.3 TB/s; picked from the tiles they cost 2.5 us a round of tiles and a launch
+  if (c.teacher && (double)c.rows * c.k * (double)p.width * (double)size / 4.3e6 > 6.0 + 2.5 * (plans.logits.tiles_m * (double)plans.logits.tiles_n / kCus)) {
+    c.dots = reinterpret_cast<float*>(take((int64_t)c.rows * c.k * 4));
+    c.sorted = reinterpret_cast<uint32_t*>(take((int64_t)c.rows * c.k * 4));
+    c.begins = reinterpret_cast<uint16_t*>(take((int64_t)c.rows * (c.tiles + 1) * 2));
+  }
   c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * planes * 2) : nullptr;
   c.exps = gradients && !bf16 ? take((int64_t)c.rows * c.dz_ld * 4) : c.dz;
   c.dweight_sum = bf16 && p.dweight_out && c.rows < p.tokens ? reinterpret_cast<float*>(take(p.vocab * p.width * 4)) : nullptr;
@@ -427,6 +475,7 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     piece.rows = std::min(c.rows, c.tokens - c.first), piece.last = c.first + piece.rows == c.tokens;
     const unsigned padded = (unsigned)round_up(piece.rows, 64);
     bf16 ? gather_kernel<true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false><<<padded, kThreads, 0, s>>>(piece);
+    if (c.dots) sort_kernel<<<(unsigned)piece.rows, kThreads, 0, s>>>(piece);
     launch_logits(piece, plans.logits, bf16, s);
     bf16 ? rows_kernel<true><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece) : rows_kernel<false><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece);
     if (c.dh && c.width) launch_dh(piece, plans.dh, bf16, s);

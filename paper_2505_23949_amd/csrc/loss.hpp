@@ -37,6 +37,10 @@ struct LossCall {
   void* states;            // hidden states of the piece, states_ld to a row and plane, zeros behind the width and the last row
   const void* head;        // the head (its own memory, where its rows are such lines), head_ld to a row
   float2* sums;            // of each row and tile: an exponent of 2, the sum of 2^(z scale - exponent)
+  // the logits of the entries, where the tiles that they are in leave them (NULL: the rows kernel makes them)
+  float* dots;             // of each row and entry
+  uint32_t* sorted;        // of each row: its k entries by word, word << 8 | entry, those that take no part behind
+  uint16_t* begins;        // of each row and part of a tile, and once more: how many entries stand before it
   void* exps;              // exponentials of the piece, dz_ld to a row: fp16 in the memory of dz (bf16), or fp32
   void* dz;                // of the piece, dz_ld to a row and plane, zeros behind the vocabulary
   float* dweight_sum;      // the head's gradient of the pieces so far (bf16 and more than one piece)

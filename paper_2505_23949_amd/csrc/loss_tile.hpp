@@ -347,19 +347,50 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
     // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b.  The sums of a row are
     // of those 32 TN columns: no wave waits for another.
     const int wave_col = n0 + wave_n * 32 * TN, col0 = wave_col + 4 * TN * q;
-    if (wave_col + 32 * TN > n) {
+    // Entries: a wave puts 32 rows into LDS, where their entries' columns can be picked.  (distill 4096 x 128256 x 4096 with 128 entries:
+    // the rows kernel would read 4 GB of the head again for them, 1 ms)
+    uint32_t entries[TM];
+    if (c.dots) {
 #pragma unroll
-      for (int j = 0; j < TM; ++j)
-#pragma unroll
-        for (int t = 0; t < TN; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
+      for (int j = 0; j < TM; ++j) {
+        const int row = m0 + (wave_m * TM + j) * 32 + r;
+        entries[j] = 0;
+        if (row < m && wave_col < n) __builtin_memcpy(&entries[j], c.begins + (int64_t)row * (c.tiles + 1) + wave_col / (32 * TN), 4);
+      }
     }
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
       const int row = m0 + (wave_m * TM + j) * 32 + r;
       const int64_t at = (int64_t)row * c.dz_ld;
+      TSENOR_IN_ORDER();
+#pragma unroll
+      for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int k = j; k < TM; ++k) asm volatile("" : "+a"(sum[t][k]));  // (accumulators stay what they are until their turn)
+      if (wave_col + 32 * TN > n) {
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
+      }
+      if (c.dots && __any((entries[j] & 0xFFFFu) != entries[j] >> 16)) {
+        constexpr int kStride = 32 * TN + 4;
+        float* const staged = reinterpret_cast<float*>(lds) + (wave * 32 + r) * kStride;
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; e += 4 / TN) {
+            floatx4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = sum[k % TN][j][4 * g + e + k / TN];
+            *reinterpret_cast<floatx4*>(staged + TN * (8 * g + 4 * q + e)) = v;
+          }
+        for (int i = (int)(entries[j] & 0xFFFFu) + q; i < (int)(entries[j] >> 16); i += 2) {
+          const uint32_t key = c.sorted[(int64_t)row * c.k + i];
+          c.dots[(int64_t)row * c.k + (key & 255)] = staged[(int)(key >> 8) - wave_col];
+        }
+      }
       float largest = -__builtin_inff();
 #pragma unroll
       for (int t = 0; t < TN; ++t)

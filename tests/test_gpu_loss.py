@@ -153,6 +153,18 @@ def test_distill(loss, tokens, vocab, width, dtype):
         Case(tokens, vocab, width, dtype, k=k, temperature=temperature).reference().run(loss).check()
 
 
+@pytest.mark.parametrize("tokens,vocab,width,dtype,k,left_out", [(512, 2000, 1024, "bf16", 64, 0.0), (700, 1031, 960, "bf16", 130, 0.2),
+                                                                 (300, 1500, 1000, "f32", 100, 0.1), (2100, 4099, 512, "bf16", 256, 0.0)])
+def test_entries_picked_from_the_tiles(loss, tokens, vocab, width, dtype, k, left_out):
+    """So many entries that their rows of the head are not read again."""
+    case = Case(tokens, vocab, width, dtype, k=k, left_out=left_out, temperature=1.5)
+    case.ids[0, :8] = torch.tensor([vocab - 1, 0, vocab - 1, 127, 128, 63, 64, 0]) % vocab  # ends, the same word twice
+    case.ids[1, 5:] = -1
+    case.ids[2, ::2] = vocab + 3
+    case.ids[3, :] = 77
+    case.reference().run(loss).check()
+
+
 @pytest.mark.parametrize("k", [255, 256])
 def test_most_entries(loss, k):
     Case(33, 600, 64, "bf16", k=k, temperature=3.0).reference().run(loss).check()
