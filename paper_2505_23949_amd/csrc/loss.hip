@@ -114,40 +114,95 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(LossCall c) {
   }
 }
 
-// a workgroup to a row of the piece's states, and to one more for each that its last tile has
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
-  constexpr int kSize = BF16 ? 2 : 4;
-  const int row = (int)blockIdx.x, rows = rows_of(c);
-  uint16_t* const state = static_cast<uint16_t*>(c.states) + (int64_t)row * c.states_ld * (BF16 ? 1 : 3);
-  float x[8] = {};
-  if (row < rows) {
-    const char* const h = static_cast<const char*>(c.h) + (int64_t)c.order[c.first + row] * c.h_ld * kSize;
-    for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) {
-      load_row8<BF16>(h, k, c.width, x);
-      store_planes<BF16>(state, c.states_ld, k, x);
+// The token that a row is of, by a workgroup on its own: the row-th of those that count, or, behind them, of those that do not.  A thread
+// looks at 8 tokens.  `count` becomes how many count, `weight` the largest finite |dloss| of the thread's.
+constexpr int kAloneTokens = kThreads * 8;
+__device__ __forceinline__ int token_alone(const LossCall& c, int row, int& count, float& weight) {
+  __shared__ int before[kThreads / kWave], found;
+  const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave, begin = (int)threadIdx.x * 8;
+  unsigned bits = 0;
+  weight = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int t = begin + e;
+    if (t < c.tokens && (c.teacher ? c.counts[t] != 0 : c.ids[t] >= 0 && c.ids[t] < c.vocab)) {
+      bits |= 1u << e;
+      const float w = c.dloss && row == 0 ? fabsf(c.dloss[t]) : 1.0f;
+      if (w < __builtin_inff()) weight = fmaxf(weight, w);
     }
-    return;
   }
-  for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) store_planes<BF16>(state, c.states_ld, k, x);
-  if (row >= c.rows) return;
-  const int token = c.order[c.first + row];
-  if (threadIdx.x == 0) {
-    c.loss[token] = 0.0f;
-    if (c.lse) c.lse[token] = 0.0f;
+  int upto = __popc(bits);
+#pragma unroll
+  for (int step = 1; step < kWave; step *= 2) {
+    const int v = __shfl_up(upto, step);
+    if (lane >= step) upto += v;
   }
-  if (c.dh)
-    for (int k = (int)threadIdx.x * 8; k < c.width; k += kThreads * 8)
-      store_row8<BF16>(static_cast<char*>(c.dh) + (int64_t)token * c.width * kSize, k, c.width, x);
+  if (lane == kWave - 1) before[wave] = upto;
+  __syncthreads();
+  int at = upto - __popc(bits);
+  count = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / kWave; ++w) {
+    if (w < wave) at += before[w];
+    count += before[w];
+  }
+  const bool counts = row < count;
+  int rank = counts ? at : begin - at;  // of the thread's first token of the kind
+  for (int e = 0; e < 8 && begin + e < c.tokens; ++e)
+    if ((bits >> e & 1) == counts && rank++ == (counts ? row : row - count)) found = begin + e;
+  __syncthreads();
+  return found;
 }
 
-// the entries of a row by word, and where those of each part of a tile begin: a workgroup to a row
-__global__ __launch_bounds__(kThreads) void sort_kernel(LossCall c) {
+// A workgroup to a row of the piece's states, and to one more for each that its last tile has.  ALONE: nothing has put the tokens in order
+// before (up to kAloneTokens of them, in one piece: a launch less, 5 us).
+template <bool BF16, bool ALONE>
+__global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
+  constexpr int kSize = BF16 ? 2 : 4;
+  const int row = (int)blockIdx.x;
+  int rows, token = 0;
+  if constexpr (ALONE) {
+    float weight;
+    if (row < c.tokens || row == 0) token = token_alone(c, row, rows, weight);
+    else rows = 0;
+    if (row < c.tokens && threadIdx.x == 0) c.order[row] = token;
+    if (row == 0) {
+      __shared__ float weights[kThreads / kWave];
+      weight = wave_max(weight);
+      if (threadIdx.x % kWave == 0) weights[threadIdx.x / kWave] = weight;
+      __syncthreads();
+      weight = fmaxf(fmaxf(weights[0], weights[1]), fmaxf(weights[2], weights[3]));
+      if (threadIdx.x == 0) *c.count = rows, c.largest_weight[0] = weight, c.largest_weight[1] = weight * c.inverse_temperature;
+    }
+  } else {
+    rows = rows_of(c);
+    if (row < c.rows) token = c.order[c.first + row];
+  }
+  uint16_t* const state = static_cast<uint16_t*>(c.states) + (int64_t)row * c.states_ld * (BF16 ? 1 : 3);
+  float x[8] = {};
+  if (row >= rows) {
+    for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) store_planes<BF16>(state, c.states_ld, k, x);
+    if (row >= c.rows) return;
+    if (threadIdx.x == 0) {
+      c.loss[token] = 0.0f;
+      if (c.lse) c.lse[token] = 0.0f;
+    }
+    if (c.dh)
+      for (int k = (int)threadIdx.x * 8; k < c.width; k += kThreads * 8)
+        store_row8<BF16>(static_cast<char*>(c.dh) + (int64_t)token * c.width * kSize, k, c.width, x);
+    return;
+  }
+  const char* const h = static_cast<const char*>(c.h) + (int64_t)token * c.h_ld * kSize;
+  for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) {
+    load_row8<BF16>(h, k, c.width, x);
+    store_planes<BF16>(state, c.states_ld, k, x);
+  }
+  if (!c.dots) return;
+
+  // its entries by word, and where those of each part of a tile begin
   static_assert(kThreads == kMaxEntries);
   __shared__ uint32_t keys[kMaxEntries], sorted[kMaxEntries];
-  const int row = (int)blockIdx.x, i = (int)threadIdx.x;
-  if (row >= rows_of(c)) return;
-  const int token = c.order[c.first + row];
+  const int i = (int)threadIdx.x;
   if (i < c.k) {
     const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
     keys[i] = id < 0 || id >= c.vocab ? UINT32_MAX - 255 + i : (uint32_t)id << 8 | i;
@@ -186,11 +241,12 @@ __global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* he
   }
 }
 
-// A workgroup to a token: lse, the logits of its entries, loss; exponentials into dz.
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
+// A workgroup to a token: lse, the logits of its entries, loss; exponentials into dz.  Of 1024 threads where there are few tokens (126 x
+// 116032 x 128 36 -> 15 us), of 256 where they fill the GPU.
+template <bool BF16, int THREADS>
+__global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   constexpr int kSize = BF16 ? 2 : 4;
-  constexpr int kWaves = kThreads / kWave;
+  constexpr int kThreads = THREADS, kWaves = kThreads / kWave;
   __shared__ float part[kWaves], dots[kMaxEntries], logits[kMaxEntries], q[kMaxEntries], dentry[kMaxEntries];
   __shared__ int words[kMaxEntries];
   const int row = (int)blockIdx.x, lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
@@ -218,14 +274,15 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
   largest = wave_max(largest);
   if (lane == 0) part[wave] = largest;
   __syncthreads();
-  largest = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) largest = fmaxf(largest, part[w]);
   __syncthreads();
   float total = 0.0f;
   for (int t = (int)threadIdx.x; t < c.tiles; t += kThreads) total += sums[t].y * __builtin_amdgcn_exp2f(sums[t].x - largest);
   total = wave_sum(total);
   if (lane == 0) part[wave] = total;
 
-  // entries: a wave to each in turn, the only one of a token for all four
+  // entries: a wave to each in turn, the only one of a token for all of them
   if (c.dots) {
     for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
       const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
@@ -258,12 +315,17 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
       }
     }
     __syncthreads();
-    for (int i = (int)threadIdx.x; i < c.k; i += kThreads)
-      logits[i] = fmaf(waves == 1 ? dots[i] : dots[0] + dots[1] + dots[2] + dots[3], c.scale, -largest);
+    for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
+      float s = dots[i];
+      for (int w = 1; w < waves; ++w) s += dots[w];
+      logits[i] = fmaf(s, c.scale, -largest);
+    }
   }
   __syncthreads();
   // from here on exponents of 2, counted from `largest`; lse is what they are all divided by
-  total = part[0] + part[1] + part[2] + part[3];
+  total = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) total += part[w];
   const float lse = log2f(total);
 
   const float unit = c.dz ? c.largest_weight[0] : 1.0f, weight = c.dloss ? (unit > 0.0f ? c.dloss[token] / unit : c.dloss[token]) : 1.0f;
@@ -330,6 +392,14 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LossCall c) {
       rest = remainder_of(rest, w << 16);
     }
   }
+}
+
+void launch_rows(const LossCall& c, bool bf16, hipStream_t s) {
+  const unsigned rows = (unsigned)c.rows;
+  if (rows <= 2 * kCus)
+    bf16 ? rows_kernel<true, 1024><<<rows, 1024, 0, s>>>(c) : rows_kernel<false, 1024><<<rows, 1024, 0, s>>>(c);
+  else
+    bf16 ? rows_kernel<true, kThreads><<<rows, kThreads, 0, s>>>(c) : rows_kernel<false, kThreads><<<rows, kThreads, 0, s>>>(c);
 }
 
 // no token counts, or there is none: zeros
@@ -408,7 +478,9 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), true);
   c.tile_n = plans.logits.kind == kLargeTile ? 128 : 64;
   c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
-  const bool whole = bf16 && p.width && p.width % line == 0 && p.weight_ld * size % 16 == 0 && p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
+  // (a row's last line goes on into the next row, but not into what lies between the rows of a wider matrix)
+  const bool whole = bf16 && p.width && (p.width % line == 0 || (p.width % 8 == 0 && p.weight_ld == p.width)) && p.weight_ld % 8 == 0 &&
+                     p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
   size_t at = 0;
   const auto take = [&](int64_t bytes) {
     char* const begin = workspace + at;
@@ -416,8 +488,8 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
     return begin;
   };
   // A tile has 64 rows at the least: up to there, rows of tokens that are left out cost nothing, and the states are read where they are.
-  if (!gradients && whole && p.tokens <= 64 && p.h_ld * size % 16 == 0 && p.h_ld <= kMaxTileLd && aligned_to(p.h, 16)) {
-    c.states = const_cast<void*>(p.h), c.states_row = p.h_ld, c.head = p.weight, c.head_ld = p.weight_ld;
+  if (!gradients && whole && p.width % line == 0 && p.tokens <= 64 && p.h_ld * size % 16 == 0 && p.h_ld <= kMaxTileLd && aligned_to(p.h, 16)) {
+    c.states = const_cast<void*>(p.h), c.states_row = p.h_ld, c.head = p.weight, c.head_ld = p.weight_ld, c.head_bytes = (int)p.width * 2;
     c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
     return at;
   }
@@ -428,8 +500,10 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.states_row = c.states_ld * planes;
   c.states = take((int64_t)round_up(c.rows, line) * c.states_ld * planes * 2);
   c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
-  // Entries: the rows kernel reads their rows of the head at 4.3 TB/s; picked from the tiles they cost 2.5 us a round of tiles and a launch
-  if (c.teacher && (double)c.rows * c.k * (double)p.width * (double)size / 4.3e6 > 6.0 + 2.5 * (plans.logits.tiles_m * (double)plans.logits.tiles_n / kCus)) {
+  // Entries: the rows kernel reads their rows of the head at 4.3 TB/s, 16 (4) at a time of a token in 3 us; picked from the tiles they cost
+  // 2.5 us a round of tiles, and their order 3
+  const double read = std::max((double)c.rows * c.k * (double)p.width * (double)size / 4.3e6, 3.0 * (double)(c.k / (c.rows <= 2 * kCus ? 16 : 4)));
+  if (c.teacher && read > 5.0 + 2.5 * (plans.logits.tiles_m * (double)plans.logits.tiles_n / kCus)) {
     c.dots = reinterpret_cast<float*>(take((int64_t)c.rows * c.k * 4));
     c.sorted = reinterpret_cast<uint32_t*>(take((int64_t)c.rows * c.k * 4));
     c.begins = reinterpret_cast<uint16_t*>(take((int64_t)c.rows * (c.tiles + 1) * 2));
@@ -439,6 +513,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.dweight_sum = bf16 && p.dweight_out && c.rows < p.tokens ? reinterpret_cast<float*>(take(p.vocab * p.width * 4)) : nullptr;
   c.head = whole ? p.weight : take(p.vocab * c.states_ld * planes * 2);
   c.head_ld = whole ? p.weight_ld : c.states_ld * planes;
+  c.head_bytes = whole ? (int)p.width * 2 : c.states_ld * 2;
   c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max(plans.dh.workspace, plans.dweight.workspace)));
   return at;
 }
@@ -460,12 +535,13 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
       c.rows = std::min(c.rows, c.tokens - c.first);
       launch_logits(c, plans.logits, bf16, s);
-      bf16 ? rows_kernel<true><<<(unsigned)c.rows, kThreads, 0, s>>>(c) : rows_kernel<false><<<(unsigned)c.rows, kThreads, 0, s>>>(c);
+      launch_rows(c, bf16, s);
     }
     return status_of_launches();
   }
   if (c.teacher) counts_kernel<<<(unsigned)((c.tokens + 3) / 4), kThreads, 0, s>>>(c);
-  order_kernel<<<1, kOrderThreads, 0, s>>>(c);
+  const bool alone = c.tokens <= std::min(c.rows, kAloneTokens);
+  if (!alone) order_kernel<<<1, kOrderThreads, 0, s>>>(c);
   if (c.head != c.weight) {
     uint16_t* const head = static_cast<uint16_t*>(const_cast<void*>(c.head));
     bf16 ? head_kernel<true><<<(unsigned)c.vocab, kThreads, 0, s>>>(c, head) : head_kernel<false><<<(unsigned)c.vocab, kThreads, 0, s>>>(c, head);
@@ -474,10 +550,12 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     LossCall piece = c;
     piece.rows = std::min(c.rows, c.tokens - c.first), piece.last = c.first + piece.rows == c.tokens;
     const unsigned padded = (unsigned)round_up(piece.rows, 64);
-    bf16 ? gather_kernel<true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false><<<padded, kThreads, 0, s>>>(piece);
-    if (c.dots) sort_kernel<<<(unsigned)piece.rows, kThreads, 0, s>>>(piece);
+    if (alone)
+      bf16 ? gather_kernel<true, true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false, true><<<padded, kThreads, 0, s>>>(piece);
+    else
+      bf16 ? gather_kernel<true, false><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false, false><<<padded, kThreads, 0, s>>>(piece);
     launch_logits(piece, plans.logits, bf16, s);
-    bf16 ? rows_kernel<true><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece) : rows_kernel<false><<<(unsigned)piece.rows, kThreads, 0, s>>>(piece);
+    launch_rows(piece, bf16, s);
     if (c.dh && c.width) launch_dh(piece, plans.dh, bf16, s);
     if (c.dweight && c.width) launch_dweight(piece, plans.dweight, bf16, s);
   }

@@ -35,7 +35,7 @@ struct LossCall {
   uint8_t* counts;         // of a token, where that takes more than a look at its target
   // Rows of the operands of the products are whole lines of 128 bytes: one plane in bf16, or three for single precision (see loss_tile.hpp)
   void* states;            // hidden states of the piece, states_ld to a row and plane, zeros behind the width and the last row
-  const void* head;        // the head (its own memory, where its rows are such lines), head_ld to a row
+  const void* head;        // the head (its own memory, where its rows begin at multiples of 16 bytes and end there), head_ld to a row
   float2* sums;            // of each row and tile: an exponent of 2, the sum of 2^(z scale - exponent)
   // the logits of the entries, where the tiles that they are in leave them (NULL: the rows kernel makes them)
   float* dots;             // of each row and entry
@@ -47,7 +47,7 @@ struct LossCall {
   floatx4* parts;          // of tiles whose sum `splits` workgroups share
   int splits;
   int64_t head_ld, states_row;  // states_row: elements from row to row of the states
-  int states_ld, dz_ld;
+  int states_ld, dz_ld, head_bytes;  // head_bytes: of a row of a plane of the head
   int tile_n, tiles;       // words of a wave's part of a tile of logits, such parts of a row
   // of the piece
   int first, rows;         // of `order`

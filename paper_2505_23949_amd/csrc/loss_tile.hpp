@@ -1,5 +1,6 @@
 // The tile kernel of the losses' products, C[row][col] = sum_k a(row, k) b(col, k), in its three uses:
 //   kLogits   a: states   (along the sum)    b: head (along)        z = h W^T, its rows' sums and exponentials
+//   kLogitsInPlace                              the same, of a head whose rows end inside a line of 128 bytes
 //   kStates   a: dz       (along)            b: head (across)       dh = dz W
 //   kHead     a: dz       (across)           b: states (across)     dW = dz^T h
 // "Along": a row of the operand lies along the sum in memory.  "Across": the sum goes from row to row of memory.
@@ -15,7 +16,8 @@ typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-enum Use { kLogits, kStates, kHead };
+enum Use { kLogits, kLogitsInPlace, kStates, kHead };
+constexpr bool makes_logits(int use) { return use == kLogits || use == kLogitsInPlace; }
 
 // A workgroup of four waves, two by two, takes 64 TN rows of b (columns of the result) and 64 TM rows of a; a wave 32 TN x 32 TM results
 // in accumulators, of the 32 x 32 matrix instructions whose first operand is b: a lane holds four neighbouring columns of a row.
@@ -53,30 +55,38 @@ struct Place {
   }
 };
 
-// Loads a wave's share of 64 T rows of an operand; `plane`: bytes from plane to plane of a row.
+// Loads a wave's share of 64 T rows of an operand; `plane_bytes`: from plane to plane of a row.
+// PART: rows end inside a line: what follows them is read for its rest, and behind the last row something inside (the other operand has
+// zeros there).  A kernel of its own, because the choice costs each load a branch: 10 % of the product.
 // INTERLEAVED: row 32 t + r of each 32 T rows of LDS is row T r + t of memory, so that a lane gets T times as many neighbouring columns.
-template <int T, bool INTERLEAVED>
+template <int T, bool INTERLEAVED, bool PART>
 struct LoaderAlong {
   intx4 from;
-  uint32_t to;
-  int plane_bytes, lane[2 * T];
-  __device__ __forceinline__ LoaderAlong(const void* p, int64_t ld_bytes, int plane_bytes_, int first, int rows, int lane_id, int wave, uint32_t lds) {
-    from = resource_of(static_cast<const char*>(p) + first * ld_bytes, min(64 * T, rows - first) * ld_bytes);
+  uint32_t to, past;  // past: offset of the last 16 bytes
+  int plane_bytes, whole, lane[2 * T];
+  __device__ __forceinline__ LoaderAlong(const void* p, int64_t ld_bytes, int plane_bytes_, int row_bytes, int first, int rows, int lane_id, int wave,
+                                         uint32_t lds) {
+    const int count = min(64 * T, rows - first);
+    past = (uint32_t)(count - 1) * (uint32_t)ld_bytes + row_bytes - 16;
+    from = resource_of(static_cast<const char*>(p) + first * ld_bytes, (int64_t)past + 16);
     to = lds + wave * 16 * T * 128;
-    plane_bytes = plane_bytes_;
+    plane_bytes = plane_bytes_, whole = row_bytes / 128;
 #pragma unroll
     for (int j = 0; j < 2 * T; ++j) {
       const int at = wave * 16 * T + 8 * j + lane_id / 8;
       const int row = INTERLEAVED ? at / (32 * T) * (32 * T) + at % 32 * T + at % (32 * T) / 32 : at;
-      lane[j] = (int)((uint32_t)min(row, rows - 1 - first) * (uint32_t)ld_bytes + (lane_id % 8 ^ at / 2 % 8) * 16);  // (32 bits, unsigned)
+      lane[j] = (int)((uint32_t)min(row, count - 1) * (uint32_t)ld_bytes + (lane_id % 8 ^ at / 2 % 8) * 16);  // (32 bits, unsigned)
     }
   }
   __device__ __forceinline__ void load(int buffer, int j, int plane, int at) const {
-    load_to_lds(to + buffer + j * 1024, lane[j], from, plane * plane_bytes + at * 128);
+    if (!PART || at < whole)
+      load_to_lds(to + buffer + j * 1024, lane[j], from, plane * plane_bytes + at * 128);
+    else
+      load_to_lds(to + buffer + j * 1024, (int)min((uint32_t)lane[j] + at * 128, past), from, 0);  // (rows of one plane)
   }
 };
 
-// `count` columns of the sum, `plane_bytes` bytes of operand in each.  What lies past either end is read as something inside: past the
+// `count` columns of the sum, `row_bytes` bytes of operand in each plane.  What lies past either end is read as something inside: past the
 // last column the other operand is zero, and past the last row nothing is written.
 template <int T>
 struct LoaderAcross {
@@ -85,11 +95,11 @@ struct LoaderAcross {
   int64_t ld_bytes, past;  // past: offset of the last 16 bytes of a plane
   uint32_t to;
   int plane_bytes, lane, step;
-  __device__ __forceinline__ LoaderAcross(const void* p, int64_t ld_bytes_, int plane_bytes_, int first, int count, int lane_id, int wave, uint32_t lds) {
-    base = static_cast<const char*>(p), ld_bytes = ld_bytes_, plane_bytes = plane_bytes_, past = (count - 1) * ld_bytes + plane_bytes - 16;
+  __device__ __forceinline__ LoaderAcross(const void* p, int64_t ld_bytes_, int row_bytes, int first, int count, int lane_id, int wave, uint32_t lds) {
+    base = static_cast<const char*>(p), ld_bytes = ld_bytes_, plane_bytes = row_bytes, past = (count - 1) * ld_bytes + row_bytes - 16;
     to = lds + wave * 1024;
     const int k = wave * kAtOnce + lane_id * 16 / kRowBytes, at = lane_id * 16 % kRowBytes, swap = kRowBytes >= 256 ? k % 4 : k / 2 % 2;
-    lane = k * (int)ld_bytes + min(first * 2 + (at ^ swap * 64), plane_bytes - 16);
+    lane = k * (int)ld_bytes + min(first * 2 + (at ^ swap * 64), row_bytes - 16);
     step = 4 * kAtOnce * (int)ld_bytes;
   }
   __device__ __forceinline__ void load(int buffer, int j, int plane, int at) const {
@@ -208,17 +218,17 @@ template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
 __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
   using Shape = TileShape<TN, TM>;
   constexpr int kPlanes = BF16 ? 1 : 3;
-  constexpr bool kAlongB = USE == kLogits, kAlongA = USE != kHead;
+  constexpr bool kAlongB = makes_logits(USE), kAlongA = USE != kHead;
   __shared__ __align__(1024) uint8_t lds[BUFFERS * Shape::kBuffer];
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
   const int piece = __builtin_amdgcn_readfirstlane(rows_of(c));
-  const int m = USE == kHead ? c.vocab : piece, n = USE == kLogits ? c.vocab : c.width;
+  const int m = USE == kHead ? c.vocab : piece, n = makes_logits(USE) ? c.vocab : c.width;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB;
   const int tiles = tiles_m * tiles_n;
   if ((int)blockIdx.x >= tiles * (SPLIT ? c.splits : 1)) return;  // (of a piece without tokens that count, all of them)
   const int split = SPLIT ? (int)blockIdx.x / tiles : 0;
-  const int all_blocks = (USE == kLogits ? c.states_ld / 64 : USE == kStates ? c.dz_ld / 64 : (piece + 63) / 64) * (BF16 ? 1 : kPairs);
+  const int all_blocks = (makes_logits(USE) ? c.states_ld / 64 : USE == kStates ? c.dz_ld / 64 : (piece + 63) / 64) * (BF16 ? 1 : kPairs);
   if (USE == kHead && all_blocks == 0 && c.first > 0 && !c.last) return;
   int tile_m, tile_n;
   tile_of((int)blockIdx.x - split * tiles, tiles_m, tiles_n, tile_m, tile_n);
@@ -237,19 +247,19 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
   const int states = c.states_ld * 2, dz = c.dz_ld * 2;  // bytes of a row of a plane (of the head: as of the states)
   const auto of_b = [&] {
-    if constexpr (USE == kLogits)
-      return LoaderAlong<TN, true>(c.head, c.head_ld * 2, states, n0, n, lane, wave, lds_at);
+    if constexpr (makes_logits(USE))
+      return LoaderAlong<TN, true, USE == kLogitsInPlace>(c.head, c.head_ld * 2, states, c.head_bytes * kPlanes, n0, n, lane, wave, lds_at);
     else if constexpr (USE == kStates)
-      return LoaderAcross<TN>(c.head, c.head_ld * 2, states, n0, c.vocab, lane, wave, lds_at);
+      return LoaderAcross<TN>(c.head, c.head_ld * 2, c.head_bytes, n0, c.vocab, lane, wave, lds_at);
     else
       return LoaderAcross<TN>(c.states, (int64_t)states * kPlanes, states, n0, (piece + 63) / 64 * 64, lane, wave, lds_at);
   }();
   const uint32_t lds_a = lds_at + Shape::kRowsB * 128;
   const auto of_a = [&] {
-    if constexpr (USE == kLogits)
-      return LoaderAlong<TM, false>(c.states, c.states_row * 2, states, m0, m, lane, wave, lds_a);
+    if constexpr (makes_logits(USE))
+      return LoaderAlong<TM, false, false>(c.states, c.states_row * 2, states, states * kPlanes, m0, m, lane, wave, lds_a);
     else if constexpr (USE == kStates)
-      return LoaderAlong<TM, false>(c.dz, (int64_t)dz * kPlanes, dz, m0, m, lane, wave, lds_a);
+      return LoaderAlong<TM, false, false>(c.dz, (int64_t)dz * kPlanes, dz, dz * kPlanes, m0, m, lane, wave, lds_a);
     else
       return LoaderAcross<TM>(c.dz, (int64_t)dz * kPlanes, dz, m0, piece, lane, wave, lds_a);
   }();
@@ -343,7 +353,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
 #undef LATE
   meet<0>();  // (no load into LDS outlives the workgroup)
 
-  if constexpr (USE == kLogits) {
+  if constexpr (makes_logits(USE)) {
     // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b.  The sums of a row are
     // of those 32 TN columns: no wave waits for another.
     const int wave_col = n0 + wave_n * 32 * TN, col0 = wave_col + 4 * TN * q;
@@ -453,34 +463,61 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   }
 }
 
-// adds the parts of a tile in their order: a workgroup for each tile and TN TM-th of it
+// adds the parts of a tile in their order: a workgroup for each tile and 4 TN TM-th of it
 template <bool BF16, int USE, int TN, int TM>
 __global__ __launch_bounds__(256) void join_kernel(LossCall c) {
   using Shape = TileShape<TN, TM>;
   const int piece = rows_of(c), m = USE == kHead ? c.vocab : piece;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (c.width + Shape::kRowsB - 1) / Shape::kRowsB, tiles = tiles_m * tiles_n;
-  const int tile = (int)blockIdx.x / (TN * TM), j = (int)blockIdx.x / TN % TM, t = (int)blockIdx.x % TN;
+  const int tile = (int)blockIdx.x / (TN * TM * 4), at_j = (int)blockIdx.x / (4 * TN) % TM, t = (int)blockIdx.x / 4 % TN, g = (int)blockIdx.x % 4;
   if (tile >= tiles || (USE == kHead && piece == 0 && c.first > 0 && !c.last)) return;
   int tile_m, tile_n;
   tile_of(tile, tiles_m, tiles_n, tile_m, tile_n);
-  const floatx4* part = c.parts + ((int64_t)tile * (TM * TN * 4) + (j * TN + t) * 4) * 256 + threadIdx.x;
+  const floatx4* part = c.parts + ((int64_t)tile * (TM * TN * 4) + (at_j * TN + t) * 4 + g) * 256 + threadIdx.x;
   const int64_t step = (int64_t)tiles * (TM * TN * 4) * 256;
-  floatx4 v[4];
+  floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  int k = 0;
+  for (; k + 8 <= c.splits; k += 8) {
+    floatx4 x[8];
 #pragma unroll
-  for (int g = 0; g < 4; ++g) v[g] = part[g * 256];
-#pragma unroll 4
-  for (int k = 1; k < c.splits; ++k)
+    for (int u = 0; u < 8; ++u) x[u] = part[(k + u) * step];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) v[g] += part[k * step + g * 256];
+    for (int u = 0; u < 8; ++u) v += x[u];
+  }
+  for (; k < c.splits; ++k) v += part[k * step];
+  const int wave = (int)threadIdx.x / kWave, row = tile_m * Shape::kRowsA + (wave / 2 * TM + at_j) * 32 + (int)threadIdx.x % 32;
+  if (row >= m) return;
+  const int col = tile_n * Shape::kRowsB + (wave % 2 * TN + t) * 32 + 8 * g + 4 * ((int)threadIdx.x / 32 % 2), n = c.width;
+  const int64_t at = (int64_t)(USE == kStates ? c.order[c.first + row] : row) * n + col;
   const float scale = c.largest_weight[1];
-  const int wave = (int)threadIdx.x / kWave, row = tile_m * Shape::kRowsA + (wave / 2 * TM + j) * 32 + (int)threadIdx.x % 32;
-  const int64_t at = (int64_t)(row >= m ? 0 : USE == kStates ? c.order[c.first + row] : row) * c.width;
+  float x[4];
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    floatx4 lo, hi;
+  for (int e = 0; e < 4; ++e) x[e] = v[e] * scale;
+  if constexpr (USE == kHead) {
+    float* const sums = (BF16 ? c.dweight_sum : static_cast<float*>(c.dweight)) + at;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) lo[e] = v[2 * p][e] * scale, hi[e] = v[2 * p + 1][e] * scale;
-    write_gradient<BF16, USE>(c, row < m ? row : -1, at, tile_n * Shape::kRowsB + (wave % 2 * TN + t) * 32 + 16 * p, lo, hi);
+    for (int e = 0; e < 4; ++e)
+      if (c.first > 0 && col + e < n) x[e] += sums[e];
+    if (BF16 && !c.last) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < n) sums[e] = x[e];
+      return;
+    }
+  }
+  void* const out = USE == kStates ? c.dh : c.dweight;
+  if constexpr (BF16) {
+    const uint32_t w[2] = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    uint16_t* const to = static_cast<uint16_t*>(out) + at;
+    if (col + 4 <= n) {
+      __builtin_memcpy(to, w, 8);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < n) to[e] = (uint16_t)(w[e / 2] >> (e % 2 * 16));
+    }
+  } else {
+    store4(static_cast<float*>(out) + at, floatx4{x[0], x[1], x[2], x[3]}, col, n);
   }
 }
 
@@ -488,12 +525,12 @@ __global__ __launch_bounds__(256) void join_kernel(LossCall c) {
 template <bool BF16, int USE, int TN, int TM, int BUFFERS>
 void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
   const unsigned tiles = (unsigned)(plan.tiles_m * plan.tiles_n);
-  if constexpr (USE != kLogits)
+  if constexpr (!makes_logits(USE))
     if (plan.splits > 1) {
       LossCall shared = c;
       shared.splits = plan.splits;
       tile_kernel<BF16, USE, TN, TM, BUFFERS, true><<<tiles * (unsigned)plan.splits, 256, 0, s>>>(shared);
-      join_kernel<BF16, USE, TN, TM><<<tiles * TN * TM, 256, 0, s>>>(shared);
+      join_kernel<BF16, USE, TN, TM><<<tiles * TN * TM * 4, 256, 0, s>>>(shared);
       return;
     }
   tile_kernel<BF16, USE, TN, TM, BUFFERS, false><<<tiles, 256, 0, s>>>(c);

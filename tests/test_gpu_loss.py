@@ -137,7 +137,8 @@ class Case:
 # ---- values ---------------------------------------------------------------------------------------------------------------
 
 SIZES = [(1, 1, 1), (1, 5, 7), (2, 64, 64), (3, 129, 100), (16, 1000, 72), (17, 257, 256), (64, 128, 128), (65, 300, 513), (130, 1029, 96),
-         (257, 515, 320), (300, 2048, 64), (9, 4099, 129)]
+         (257, 515, 320), (300, 2048, 64), (9, 4099, 129),
+         (70, 700, 328), (2, 534, 1096), (2049, 300, 40)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -174,7 +175,8 @@ def test_most_entries(loss, k):
 @pytest.mark.parametrize("k", [0, 6])
 @pytest.mark.parametrize("ld,offset", [(8, 0), (8, 8), (3, 1), (64, 16), (5, 5)])
 def test_strides(loss, dtype, k, ld, offset):
-    Case(37, 260, 128, dtype, k=k).reference().run(loss, ld=ld, offset=offset).check()
+    for width in (128, 72):
+        Case(37, 260, width, dtype, k=k).reference().run(loss, ld=ld, offset=offset).check()
 
 
 @pytest.mark.parametrize("k", [0, 4])
