@@ -368,7 +368,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   uint16_t* const dz = static_cast<uint16_t*>(c.dz) + (int64_t)row * c.dz_ld * (BF16 ? 1 : 3);
   const char* const exps = static_cast<const char*>(c.exps) + (int64_t)row * c.dz_ld * kSize;
   for (int k = (int)threadIdx.x * 8; k < c.dz_ld; k += kThreads * 8) {
-    const float scale = share * __builtin_amdgcn_exp2f(sums[k / c.tile_n].x - largest);
+    const float scale = share * __builtin_amdgcn_exp2f(sums[min(k / c.tile_n, c.tiles - 1)].x - largest);
     float x[8];
     if constexpr (BF16) {
       _Float16 y[8];
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
 
 void launch_rows(const LossCall& c, bool bf16, hipStream_t s) {
   const unsigned rows = (unsigned)c.rows;
-  if (rows <= 2 * kCus)
+  if (rows <= 2 * kCus && (c.k > 4 || c.tiles > 1024))
     bf16 ? rows_kernel<true, 1024><<<rows, 1024, 0, s>>>(c) : rows_kernel<false, 1024><<<rows, 1024, 0, s>>>(c);
   else
     bf16 ? rows_kernel<true, kThreads><<<rows, kThreads, 0, s>>>(c) : rows_kernel<false, kThreads><<<rows, kThreads, 0, s>>>(c);
@@ -459,6 +459,7 @@ inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; 
 
 struct Plans {
   ProductPlan logits, dh, dweight;
+  bool few;  // logits by the kernel for few tokens
 };
 
 // describes a call to the kernels; the workspace begins at `workspace` (which may be NULL to ask for its size alone)
@@ -476,11 +477,14 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line * (bf16 ? 1 : kPairs), false);
   if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line * (bf16 ? 1 : kPairs), true);
   if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), true);
-  c.tile_n = plans.logits.kind == kLargeTile ? 128 : 64;
-  c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
   // (a row's last line goes on into the next row, but not into what lies between the rows of a wider matrix)
   const bool whole = bf16 && p.width && (p.width % line == 0 || (p.width % 8 == 0 && p.weight_ld == p.width)) && p.weight_ld % 8 == 0 &&
                      p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
+  // up to 16 tokens: straight from memory, where tiles would need a copy of the head that nothing else needs, or are few (us of the call:
+  // 3 x 1216 x 2326 27.4, 10.4 so, 4 x 1650 x 6912 with dh 58.3, 39.6; but 1 x 32000 x 2048 29.0, 33.6)
+  plans.few = p.tokens <= kFewTokens && (p.vocab < 64 * kCus || (!whole && !p.dh_out));
+  c.tile_n = plans.few ? kFewWords : plans.logits.kind == kLargeTile ? 128 : 64;
+  c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
   size_t at = 0;
   const auto take = [&](int64_t bytes) {
     char* const begin = workspace + at;
@@ -488,10 +492,14 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
     return begin;
   };
   // A tile has 64 rows at the least: up to there, rows of tokens that are left out cost nothing, and the states are read where they are.
+  if (!gradients && plans.few) {
+    c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
+    return std::max<size_t>(at, 256);
+  }
   if (!gradients && whole && p.width % line == 0 && p.tokens <= 64 && p.h_ld * size % 16 == 0 && p.h_ld <= kMaxTileLd && aligned_to(p.h, 16)) {
     c.states = const_cast<void*>(p.h), c.states_row = p.h_ld, c.head = p.weight, c.head_ld = p.weight_ld, c.head_bytes = (int)p.width * 2;
     c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
-    return at;
+    return std::max<size_t>(at, 256);
   }
   c.count = reinterpret_cast<int*>(take(12));
   c.largest_weight = reinterpret_cast<float*>(c.count + 1);
@@ -503,7 +511,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   // Entries: the rows kernel reads their rows of the head at 4.3 TB/s, 16 (4) at a time of a token in 3 us; picked from the tiles they cost
   // 2.5 us a round of tiles, and their order 3
   const double read = std::max((double)c.rows * c.k * (double)p.width * (double)size / 4.3e6, 3.0 * (double)(c.k / (c.rows <= 2 * kCus ? 16 : 4)));
-  if (c.teacher && read > 5.0 + 2.5 * (plans.logits.tiles_m * (double)plans.logits.tiles_n / kCus)) {
+  if (c.teacher && !plans.few && read > 5.0 + 2.5 * (plans.logits.tiles_m * (double)plans.logits.tiles_n / kCus)) {
     c.dots = reinterpret_cast<float*>(take((int64_t)c.rows * c.k * 4));
     c.sorted = reinterpret_cast<uint32_t*>(take((int64_t)c.rows * c.k * 4));
     c.begins = reinterpret_cast<uint16_t*>(take((int64_t)c.rows * (c.tiles + 1) * 2));
@@ -511,11 +519,11 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * planes * 2) : nullptr;
   c.exps = gradients && !bf16 ? take((int64_t)c.rows * c.dz_ld * 4) : c.dz;
   c.dweight_sum = bf16 && p.dweight_out && c.rows < p.tokens ? reinterpret_cast<float*>(take(p.vocab * p.width * 4)) : nullptr;
-  c.head = whole ? p.weight : take(p.vocab * c.states_ld * planes * 2);
+  c.head = whole || (plans.few && !p.dh_out) ? p.weight : take(p.vocab * c.states_ld * planes * 2);
   c.head_ld = whole ? p.weight_ld : c.states_ld * planes;
   c.head_bytes = whole ? (int)p.width * 2 : c.states_ld * 2;
   c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max(plans.dh.workspace, plans.dweight.workspace)));
-  return at;
+  return std::max<size_t>(at, 256);
 }
 
 int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_bytes, hipStream_t s) {
@@ -534,7 +542,7 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
   if (!c.count) {
     for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
       c.rows = std::min(c.rows, c.tokens - c.first);
-      launch_logits(c, plans.logits, bf16, s);
+      plans.few ? launch_few_logits(c, bf16, s) : launch_logits(c, plans.logits, bf16, s);
       launch_rows(c, bf16, s);
     }
     return status_of_launches();
@@ -554,7 +562,7 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
       bf16 ? gather_kernel<true, true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false, true><<<padded, kThreads, 0, s>>>(piece);
     else
       bf16 ? gather_kernel<true, false><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false, false><<<padded, kThreads, 0, s>>>(piece);
-    launch_logits(piece, plans.logits, bf16, s);
+    plans.few ? launch_few_logits(piece, bf16, s) : launch_logits(piece, plans.logits, bf16, s);
     launch_rows(piece, bf16, s);
     if (c.dh && c.width) launch_dh(piece, plans.dh, bf16, s);
     if (c.dweight && c.width) launch_dweight(piece, plans.dweight, bf16, s);
