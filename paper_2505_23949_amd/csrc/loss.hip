@@ -116,7 +116,8 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(LossCall c) {
 
 // The token that a row is of, by a workgroup on its own: the row-th of those that count, or, behind them, of those that do not.  A thread
 // looks at 8 tokens.  `count` becomes how many count, `weight` the largest finite |dloss| of the thread's.
-constexpr int kAloneTokens = kThreads * 8;
+constexpr int kAloneTokens = 1024;
+static_assert(kAloneTokens <= kThreads * 8);
 __device__ __forceinline__ int token_alone(const LossCall& c, int row, int& count, float& weight) {
   __shared__ int before[kThreads / kWave], found;
   const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave, begin = (int)threadIdx.x * 8;
@@ -241,64 +242,67 @@ __global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* he
   }
 }
 
-// A workgroup to a token: lse, the logits of its entries, loss; exponentials into dz.  Of 1024 threads where there are few tokens (126 x
-// 116032 x 128 36 -> 15 us), of 256 where they fill the GPU.
+// A workgroup to a token: lse, the logits of its entries, loss; exponentials into dz.  1024 threads where there are few tokens (126 x 116032 x
+// 128: 36 -> 23 us), a wave where a token has little to do, so that more of them wait at a time (7744 x 512, one entry: 32 -> 14 us).
+// Exponents here are of 2 and counted from `largest`.
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
-  constexpr int kSize = BF16 ? 2 : 4;
-  constexpr int kThreads = THREADS, kWaves = kThreads / kWave;
-  __shared__ float part[kWaves], dots[kMaxEntries], logits[kMaxEntries], q[kMaxEntries], dentry[kMaxEntries];
+  constexpr int kSize = BF16 ? 2 : 4, kWaves = THREADS / kWave, kMine = 2;
+  __shared__ float part[2][kWaves], dots[kMaxEntries], teacher[kMaxEntries], q[kMaxEntries], dentry[kMaxEntries];
   __shared__ int words[kMaxEntries];
   const int row = (int)blockIdx.x, lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
   if (row >= rows_of(c)) return;
   const int token = c.count ? c.order[c.first + row] : c.first + row;
-  if (!c.count) {
-    bool any = false;
-    if (c.teacher) {
-      for (int i = (int)threadIdx.x; i < c.k; i += kThreads) any |= teacher_of(c, token, i) != -__builtin_inff();
-    } else {
-      any = c.ids[token] >= 0 && c.ids[token] < c.vocab;
-    }
-    if (!__syncthreads_or(any)) {
-      if (threadIdx.x == 0) {
-        c.loss[token] = 0.0f;
-        if (c.lse) c.lse[token] = 0.0f;
-      }
-      return;
-    }
-  }
   const float2* const sums = c.sums + (int64_t)row * c.tiles;
 
+  // what has to be read, asked for at once
+  float2 mine[kMine];
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) {
+    const int t = u * THREADS + (int)threadIdx.x;
+    mine[u] = t < c.tiles ? sums[t] : make_float2(-__builtin_inff(), 0.0f);
+  }
+  float top = -__builtin_inff();
+  bool any = false;
+  for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
+    const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
+    const bool valid = id >= 0 && id < c.vocab;
+    const float u = c.teacher ? teacher_of(c, token, i) : valid ? 0.0f : -__builtin_inff();
+    words[i] = valid ? (int)id : -1, teacher[i] = u;
+    if (c.dots) dots[i] = valid ? c.dots[(int64_t)row * c.k + i] : 0.0f;
+    top = fmaxf(top, u), any |= u != -__builtin_inff();  // (NaN takes part)
+  }
+  if (!c.count && !__syncthreads_or(any)) {  // nothing has left it out before
+    if (threadIdx.x == 0) {
+      c.loss[token] = 0.0f;
+      if (c.lse) c.lse[token] = 0.0f;
+    }
+    return;
+  }
   float largest = -__builtin_inff();
-  for (int t = (int)threadIdx.x; t < c.tiles; t += kThreads) largest = fmaxf(largest, sums[t].x);
-  largest = wave_max(largest);
-  if (lane == 0) part[wave] = largest;
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) largest = fmaxf(largest, mine[u].x);
+  for (int t = kMine * THREADS + (int)threadIdx.x; t < c.tiles; t += THREADS) largest = fmaxf(largest, sums[t].x);
+  largest = wave_max(largest), top = wave_max(top);
+  if (lane == 0) part[0][wave] = largest, part[1][wave] = top;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) largest = fmaxf(largest, part[w]);
-  __syncthreads();
-  float total = 0.0f;
-  for (int t = (int)threadIdx.x; t < c.tiles; t += kThreads) total += sums[t].y * __builtin_amdgcn_exp2f(sums[t].x - largest);
-  total = wave_sum(total);
-  if (lane == 0) part[wave] = total;
+  for (int w = 0; w < kWaves; ++w) largest = fmaxf(largest, part[0][w]), top = fmaxf(top, part[1][w]);
 
-  // entries: a wave to each in turn, the only one of a token for all of them
-  if (c.dots) {
-    for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
-      const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
-      const bool valid = id >= 0 && id < c.vocab;
-      words[i] = valid ? (int)id : -1;
-      logits[i] = valid ? fmaf(c.dots[(int64_t)row * c.k + i], c.scale, -largest) : 0.0f;
-    }
-  } else {
-    const int waves = c.k == 1 ? kWaves : 1;
+  float total = 0.0f, all = 0.0f;
+#pragma unroll
+  for (int u = 0; u < kMine; ++u)
+    if (u * THREADS + (int)threadIdx.x < c.tiles) total += mine[u].y * __builtin_amdgcn_exp2f(mine[u].x - largest);
+  for (int t = kMine * THREADS + (int)threadIdx.x; t < c.tiles; t += THREADS) total += sums[t].y * __builtin_amdgcn_exp2f(sums[t].x - largest);
+  for (int i = (int)threadIdx.x; i < c.k; i += THREADS) all += expf(teacher[i] - top);
+  const int waves = c.k == 1 ? kWaves : 1;  // of an entry: all of them for the only one of a token
+  if (!c.dots) {
     for (int i = c.k == 1 ? 0 : wave; i < c.k; i += kWaves) {
-      const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
-      const bool valid = id >= 0 && id < c.vocab;
+      const int word = words[i];
       float s = 0.0f;
-      if (valid) {
+      if (word >= 0) {
         const char* const h = static_cast<const char*>(c.h) + (int64_t)token * c.h_ld * kSize;
-        const char* const w = static_cast<const char*>(c.weight) + id * c.weight_ld * kSize;
+        const char* const w = static_cast<const char*>(c.weight) + word * c.weight_ld * kSize;
 #pragma unroll 2
         for (int k = (wave % waves * kWave + lane) * 8; k < c.width; k += waves * kWave * 8) {
           float x[8], y[8];
@@ -309,65 +313,52 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
         }
       }
       s = wave_sum(s);
-      if (lane == 0) {
-        dots[waves == 1 ? i : wave] = s;
-        words[i] = valid ? (int)id : -1;
-      }
-    }
-    __syncthreads();
-    for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
-      float s = dots[i];
-      for (int w = 1; w < waves; ++w) s += dots[w];
-      logits[i] = fmaf(s, c.scale, -largest);
+      if (lane == 0) dots[waves == 1 ? i : wave] = s;
     }
   }
+  total = wave_sum(total), all = wave_sum(all);
   __syncthreads();
-  // from here on exponents of 2, counted from `largest`; lse is what they are all divided by
-  total = 0.0f;
+  if (lane == 0) part[0][wave] = total, part[1][wave] = all;
+  __syncthreads();
+  total = all = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) total += part[w];
-  const float lse = log2f(total);
+  for (int w = 0; w < kWaves; ++w) total += part[0][w], all += part[1][w];
 
+  const float lse = log2f(total), log_all = logf(all);
   const float unit = c.dz ? c.largest_weight[0] : 1.0f, weight = c.dloss ? (unit > 0.0f ? c.dloss[token] / unit : c.dloss[token]) : 1.0f;
-  if (wave == 0) {
-    float loss;
-    if (!c.teacher) {
-      loss = (lse - logits[0]) * kLn2;
-      if (lane == 0) q[0] = 1.0f;
-    } else {
-      float top = -__builtin_inff();
-      for (int i = lane; i < c.k; i += kWave) top = fmaxf(top, teacher_of(c, token, i));
-      top = wave_max(top);
-      float all = 0.0f;
-      for (int i = lane; i < c.k; i += kWave) all += expf(teacher_of(c, token, i) - top);
-      all = wave_sum(all);
-      const float log_all = logf(all);
-      loss = 0.0f;
-      for (int i = lane; i < c.k; i += kWave) {
-        const float u = teacher_of(c, token, i) - top, p = expf(u) / all;
-        q[i] = p;
-        if (p != 0.0f) loss = fmaf(p, u - log_all + (lse - logits[i]) * kLn2, loss);
-      }
-      loss = wave_sum(loss);
-    }
-    if (lane == 0) {
-      c.loss[token] = loss;
-      if (c.lse) c.lse[token] = (largest + lse) * kLn2;
-    }
+  float loss = 0.0f;
+  for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
+    float s = dots[i];
+    for (int w = 1; w < waves; ++w) s += dots[w];
+    s = fmaf(s, c.scale, -largest);
+    const float u = teacher[i] - top, p = c.teacher ? expf(u) / all : 1.0f;
+    q[i] = p, dentry[i] = __builtin_amdgcn_exp2f(s) / total;
+    if (!c.teacher)
+      loss = (lse - s) * kLn2;
+    else if (p != 0.0f)
+      loss = fmaf(p, u - log_all + (lse - s) * kLn2, loss);
+  }
+  loss = wave_sum(loss);
+  __syncthreads();
+  if (lane == 0) part[0][wave] = loss;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kWaves; ++w) loss += part[0][w];
+    c.loss[token] = loss;
+    if (c.lse) c.lse[token] = (largest + lse) * kLn2;
   }
   if (!c.dz) return;
-  __syncthreads();
   // (the same word twice: both write what belongs to both)
-  for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
+  for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
     float p = 0.0f;
     for (int j = 0; j < c.k; ++j)
       if (words[j] == words[i]) p += q[j];
-    dentry[i] = weight * (__builtin_amdgcn_exp2f(logits[i]) / total - p);
+    dentry[i] = weight * (dentry[i] - p);
   }
   const float share = weight / total;
   uint16_t* const dz = static_cast<uint16_t*>(c.dz) + (int64_t)row * c.dz_ld * (BF16 ? 1 : 3);
   const char* const exps = static_cast<const char*>(c.exps) + (int64_t)row * c.dz_ld * kSize;
-  for (int k = (int)threadIdx.x * 8; k < c.dz_ld; k += kThreads * 8) {
+  for (int k = (int)threadIdx.x * 8; k < c.dz_ld; k += THREADS * 8) {
     const float scale = share * __builtin_amdgcn_exp2f(sums[min(k / c.tile_n, c.tiles - 1)].x - largest);
     float x[8];
     if constexpr (BF16) {
@@ -383,7 +374,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
     store_planes<BF16>(dz, c.dz_ld, k, x);
   }
   __syncthreads();
-  for (int i = (int)threadIdx.x; i < c.k; i += kThreads) {
+  for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
     if (words[i] < 0) continue;
     float rest = dentry[i];
     for (int plane = 0; plane < (BF16 ? 1 : 3); ++plane) {
@@ -394,13 +385,17 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   }
 }
 
-void launch_rows(const LossCall& c, bool bf16, hipStream_t s) {
+template <bool BF16>
+void launch_rows(const LossCall& c, hipStream_t s) {
   const unsigned rows = (unsigned)c.rows;
   if (rows <= 2 * kCus && (c.k > 4 || c.tiles > 1024))
-    bf16 ? rows_kernel<true, 1024><<<rows, 1024, 0, s>>>(c) : rows_kernel<false, 1024><<<rows, 1024, 0, s>>>(c);
+    rows_kernel<BF16, 1024><<<rows, 1024, 0, s>>>(c);
+  else if (rows > 4 * kCus && c.vocab <= 2048 && c.k <= kWave && (c.k == 1 || c.dots))
+    rows_kernel<BF16, kWave><<<rows, kWave, 0, s>>>(c);
   else
-    bf16 ? rows_kernel<true, kThreads><<<rows, kThreads, 0, s>>>(c) : rows_kernel<false, kThreads><<<rows, kThreads, 0, s>>>(c);
+    rows_kernel<BF16, kThreads><<<rows, kThreads, 0, s>>>(c);
 }
+void launch_rows(const LossCall& c, bool bf16, hipStream_t s) { bf16 ? launch_rows<true>(c, s) : launch_rows<false>(c, s); }
 
 // no token counts, or there is none: zeros
 template <bool BF16>
@@ -474,9 +469,9 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   const int64_t most = std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows);
   const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
   c.rows = (int)std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
-  plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line * (bf16 ? 1 : kPairs), false);
-  if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line * (bf16 ? 1 : kPairs), true);
-  if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), true);
+  plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line * (bf16 ? 1 : kPairs), true);
+  if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line * (bf16 ? 1 : kPairs), false);
+  if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), false);
   // (a row's last line goes on into the next row, but not into what lies between the rows of a wider matrix)
   const bool whole = bf16 && p.width && (p.width % line == 0 || (p.width % 8 == 0 && p.weight_ld == p.width)) && p.weight_ld % 8 == 0 &&
                      p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
@@ -499,6 +494,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   if (!gradients && whole && p.width % line == 0 && p.tokens <= 64 && p.h_ld * size % 16 == 0 && p.h_ld <= kMaxTileLd && aligned_to(p.h, 16)) {
     c.states = const_cast<void*>(p.h), c.states_row = p.h_ld, c.head = p.weight, c.head_ld = p.weight_ld, c.head_bytes = (int)p.width * 2;
     c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
+    c.parts = reinterpret_cast<floatx4*>(take((int64_t)plans.logits.workspace));
     return std::max<size_t>(at, 256);
   }
   c.count = reinterpret_cast<int*>(take(12));
@@ -522,7 +518,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.head = whole || (plans.few && !p.dh_out) ? p.weight : take(p.vocab * c.states_ld * planes * 2);
   c.head_ld = whole ? p.weight_ld : c.states_ld * planes;
   c.head_bytes = whole ? (int)p.width * 2 : c.states_ld * 2;
-  c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max(plans.dh.workspace, plans.dweight.workspace)));
+  c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max({plans.logits.workspace, plans.dh.workspace, plans.dweight.workspace})));
   return std::max<size_t>(at, 256);
 }
 

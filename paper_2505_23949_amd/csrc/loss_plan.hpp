@@ -16,15 +16,16 @@ struct ProductPlan {
   size_t workspace;
 };
 
-// m rows of a, n of b, `blocks` of 64 columns of the sum; `shared`: whether workgroups may share the sum of a tile
-inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool shared) {
+// m rows of a, n of b, `blocks` of 64 columns of the sum; `logits`: they need whole sums, so that parts are joined by one workgroup to a tile
+inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool logits) {
   ProductPlan best = {kSmallTile, 0, 0, 1, 0.0, 0};
   if (m == 0 || n == 0) return best;
   for (const Cost& c : {Cost{kSmallTile, 64, 128, 0.42, 3.0, kCus, false}, Cost{kTile, 128, 128, 0.585, 4.0, kCus, false},
                         Cost{kTilePairs, 128, 128, 1.085, 4.5, 2 * kCus, true}, Cost{kWideTile, 256, 128, 0.86, 6.0, kCus, false},
                         Cost{kLargeTile, 256, 256, 1.556, 9.0, kCus, false}}) {
     const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n, tiles = tiles_m * tiles_n;
-    for (int64_t splits = 1; splits <= (shared ? std::min<int64_t>(128, std::max<int64_t>(blocks / 4, 1)) : 1); ++splits) {
+    const int64_t most = logits ? (c.rows_m * c.rows_n <= 128 * 128 ? 16 : 1) : 128;
+    for (int64_t splits = 1; splits <= std::min<int64_t>(most, std::max<int64_t>(blocks / 4, 1)); ++splits) {
       if (splits > 1 && (splits - 1) * tiles >= c.at_once) break;
       const double steps = (double)((blocks + splits - 1) / splits) * c.step;
       const int64_t groups = tiles * splits, rounds = groups / c.at_once, rest = groups % c.at_once;
@@ -32,7 +33,7 @@ inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool share
       const double fill = c.fluid ? (rest <= kCus ? 0.7 : 1.0) : 0.75 + 0.25 * (double)rest / c.at_once;
       double us = (double)rounds * (steps + c.around) + (rest ? steps * fill + c.around : 0.0);
       const double parts = splits > 1 ? (double)groups * c.rows_m * c.rows_n * 4.0 : 0.0;
-      if (splits > 1) us += 4.0 + 2.0 * parts / 5.0e6 + 0.1 * (double)splits;
+      if (splits > 1) us += 4.0 + 2.0 * parts / 5.0e6 + (logits ? 0.5 : 0.1) * (double)splits;
       if (best.us == 0.0 || us < best.us) best = {c.kind, (int)tiles_m, (int)tiles_n, (int)splits, us, (size_t)parts};
     }
   }

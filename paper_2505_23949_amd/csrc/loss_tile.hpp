@@ -213,6 +213,94 @@ __device__ __forceinline__ void write_gradient(const LossCall& c, int row, int64
 template <int TN, int TM, int BUFFERS>
 constexpr int kGroupsPerCu = BUFFERS * TileShape<TN, TM>::kBuffer <= 80 * 1024 ? 2 : 1;
 
+// What becomes of a tile of logits.
+template <bool BF16, int TN, int TM>
+__device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)[TN][TM], int m, int n, int m0, int n0, uint8_t* lds) {
+  const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
+  // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b.  The sums of a row are
+  // of those 32 TN columns: no wave waits for another.
+  const int wave_col = n0 + wave_n * 32 * TN, col0 = wave_col + 4 * TN * q;
+  // Entries: a wave puts 32 rows into LDS, where their entries' columns can be picked.  (distill 4096 x 128256 x 4096 with 128 entries:
+  // the rows kernel would read 4 GB of the head again for them, 1 ms)
+  uint32_t entries[TM];
+  if (c.dots) {
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int row = m0 + (wave_m * TM + j) * 32 + r;
+      entries[j] = 0;
+      if (row < m && wave_col < n) __builtin_memcpy(&entries[j], c.begins + (int64_t)row * (c.tiles + 1) + wave_col / (32 * TN), 4);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < TM; ++j) {
+    const int row = m0 + (wave_m * TM + j) * 32 + r;
+    const int64_t at = (int64_t)row * c.dz_ld;
+    TSENOR_IN_ORDER();
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+      for (int k = j; k < TM; ++k) asm volatile("" : "+a"(sum[t][k]));  // (accumulators stay what they are until their turn)
+    if (wave_col + 32 * TN > n) {
+#pragma unroll
+      for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
+    }
+    if (c.dots && __any((entries[j] & 0xFFFFu) != entries[j] >> 16)) {
+      constexpr int kStride = 32 * TN + 4;
+      float* const staged = reinterpret_cast<float*>(lds) + (wave * 32 + r) * kStride;
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; e += 4 / TN) {
+          floatx4 v;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = sum[k % TN][j][4 * g + e + k / TN];
+          *reinterpret_cast<floatx4*>(staged + TN * (8 * g + 4 * q + e)) = v;
+        }
+      for (int i = (int)(entries[j] & 0xFFFFu) + q; i < (int)(entries[j] >> 16); i += 2) {
+        const uint32_t key = c.sorted[(int64_t)row * c.k + i];
+        c.dots[(int64_t)row * c.k + (key & 255)] = staged[(int)(key >> 8) - wave_col];
+      }
+    }
+    float largest = -__builtin_inff();
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) largest = fmaxf(largest, sum[t][j][e]);
+    largest = fmaxf(largest, lane_xor<32>(largest)) * c.scale - kExpBits;
+    const float base = largest == -__builtin_inff() ? 0.0f : largest;
+    float v = 0.0f;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float x[4 * TN];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t = 0; t < TN; ++t) {
+          x[e * TN + t] = __builtin_amdgcn_exp2f(fmaf(sum[t][j][4 * g + e], c.scale, -base));
+          v += x[e * TN + t];
+        }
+      const int col = col0 + 8 * TN * g;
+      if (c.exps && row < m && col < c.dz_ld) {
+        if constexpr (BF16) {
+          uint32_t w[2 * TN];
+#pragma unroll
+          for (int k = 0; k < 2 * TN; ++k)
+            w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{x[2 * k], x[2 * k + 1]}, halfx2));
+          __builtin_memcpy(__builtin_assume_aligned(static_cast<uint16_t*>(c.exps) + at + col, 16), w, 8 * TN);
+        } else {
+          __builtin_memcpy(__builtin_assume_aligned(static_cast<float*>(c.exps) + at + col, 16), x, 16 * TN);
+        }
+      }
+    }
+    v += lane_xor<32>(v);
+    if (q == 0 && row < m && wave_col < n) c.sums[(int64_t)row * c.tiles + wave_col / (32 * TN)] = make_float2(largest, v);
+  }
+}
+
 // SPLIT: c.splits workgroups share the sum of a tile, and each leaves its part in c.parts.
 template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
 __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
@@ -353,88 +441,8 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
 #undef LATE
   meet<0>();  // (no load into LDS outlives the workgroup)
 
-  if constexpr (makes_logits(USE)) {
-    // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b.  The sums of a row are
-    // of those 32 TN columns: no wave waits for another.
-    const int wave_col = n0 + wave_n * 32 * TN, col0 = wave_col + 4 * TN * q;
-    // Entries: a wave puts 32 rows into LDS, where their entries' columns can be picked.  (distill 4096 x 128256 x 4096 with 128 entries:
-    // the rows kernel would read 4 GB of the head again for them, 1 ms)
-    uint32_t entries[TM];
-    if (c.dots) {
-#pragma unroll
-      for (int j = 0; j < TM; ++j) {
-        const int row = m0 + (wave_m * TM + j) * 32 + r;
-        entries[j] = 0;
-        if (row < m && wave_col < n) __builtin_memcpy(&entries[j], c.begins + (int64_t)row * (c.tiles + 1) + wave_col / (32 * TN), 4);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int row = m0 + (wave_m * TM + j) * 32 + r;
-      const int64_t at = (int64_t)row * c.dz_ld;
-      TSENOR_IN_ORDER();
-#pragma unroll
-      for (int t = 0; t < TN; ++t)
-#pragma unroll
-        for (int k = j; k < TM; ++k) asm volatile("" : "+a"(sum[t][k]));  // (accumulators stay what they are until their turn)
-      if (wave_col + 32 * TN > n) {
-#pragma unroll
-        for (int t = 0; t < TN; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
-      }
-      if (c.dots && __any((entries[j] & 0xFFFFu) != entries[j] >> 16)) {
-        constexpr int kStride = 32 * TN + 4;
-        float* const staged = reinterpret_cast<float*>(lds) + (wave * 32 + r) * kStride;
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-          for (int e = 0; e < 4; e += 4 / TN) {
-            floatx4 v;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = sum[k % TN][j][4 * g + e + k / TN];
-            *reinterpret_cast<floatx4*>(staged + TN * (8 * g + 4 * q + e)) = v;
-          }
-        for (int i = (int)(entries[j] & 0xFFFFu) + q; i < (int)(entries[j] >> 16); i += 2) {
-          const uint32_t key = c.sorted[(int64_t)row * c.k + i];
-          c.dots[(int64_t)row * c.k + (key & 255)] = staged[(int)(key >> 8) - wave_col];
-        }
-      }
-      float largest = -__builtin_inff();
-#pragma unroll
-      for (int t = 0; t < TN; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) largest = fmaxf(largest, sum[t][j][e]);
-      largest = fmaxf(largest, lane_xor<32>(largest)) * c.scale - kExpBits;
-      const float base = largest == -__builtin_inff() ? 0.0f : largest;
-      float v = 0.0f;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        float x[4 * TN];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int t = 0; t < TN; ++t) {
-            x[e * TN + t] = __builtin_amdgcn_exp2f(fmaf(sum[t][j][4 * g + e], c.scale, -base));
-            v += x[e * TN + t];
-          }
-        const int col = col0 + 8 * TN * g;
-        if (c.exps && row < m && col < c.dz_ld) {
-          if constexpr (BF16) {
-            uint32_t w[2 * TN];
-#pragma unroll
-            for (int k = 0; k < 2 * TN; ++k)
-              w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{x[2 * k], x[2 * k + 1]}, halfx2));
-            __builtin_memcpy(__builtin_assume_aligned(static_cast<uint16_t*>(c.exps) + at + col, 16), w, 8 * TN);
-          } else {
-            __builtin_memcpy(__builtin_assume_aligned(static_cast<float*>(c.exps) + at + col, 16), x, 16 * TN);
-          }
-        }
-      }
-      v += lane_xor<32>(v);
-      if (q == 0 && row < m && wave_col < n) c.sums[(int64_t)row * c.tiles + wave_col / (32 * TN)] = make_float2(largest, v);
-    }
+  if constexpr (makes_logits(USE) && !SPLIT) {
+    finish_logits<BF16, TN, TM>(c, sum, m, n, m0, n0, lds);
   } else if constexpr (SPLIT) {
 #pragma unroll
     for (int j = 0; j < TM; ++j)
@@ -521,18 +529,49 @@ __global__ __launch_bounds__(256) void join_kernel(LossCall c) {
   }
 }
 
+// the same of logits: a workgroup to a tile, which takes the place of its first
+template <bool BF16, int TN, int TM>
+__global__ __launch_bounds__(256) void join_logits_kernel(LossCall c) {
+  using Shape = TileShape<TN, TM>;
+  __shared__ __align__(16) uint8_t lds[4 * 32 * (32 * TN + 4) * 4];
+  const int m = rows_of(c), n = c.vocab;
+  const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB, tiles = tiles_m * tiles_n;
+  if ((int)blockIdx.x >= tiles) return;
+  int tile_m, tile_n;
+  tile_of((int)blockIdx.x, tiles_m, tiles_n, tile_m, tile_n);
+  const floatx4* const part = c.parts + (int64_t)blockIdx.x * (TM * TN * 4) * 256 + threadIdx.x;
+  const int64_t step = (int64_t)tiles * (TM * TN * 4) * 256;
+  floatx4 v[TM * TN * 4] = {};
+  for (int k = 0; k < c.splits; ++k) {
+#pragma unroll
+    for (int at = 0; at < TM * TN * 4; ++at) v[at] += part[k * step + at * 256];
+  }
+  floatx16 sum[TN][TM];
+#pragma unroll
+  for (int j = 0; j < TM; ++j)
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum[t][j][e] = v[(j * TN + t) * 4 + e / 4][e % 4];
+  finish_logits<BF16, TN, TM>(c, sum, m, n, tile_m * Shape::kRowsA, tile_n * Shape::kRowsB, lds);
+}
+
 // the kernel with the tiles of a plan
 template <bool BF16, int USE, int TN, int TM, int BUFFERS>
 void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
   const unsigned tiles = (unsigned)(plan.tiles_m * plan.tiles_n);
-  if constexpr (!makes_logits(USE))
+  if constexpr (!makes_logits(USE) || TN * TM <= 4) {
     if (plan.splits > 1) {
       LossCall shared = c;
       shared.splits = plan.splits;
       tile_kernel<BF16, USE, TN, TM, BUFFERS, true><<<tiles * (unsigned)plan.splits, 256, 0, s>>>(shared);
-      join_kernel<BF16, USE, TN, TM><<<tiles * TN * TM * 4, 256, 0, s>>>(shared);
+      if constexpr (makes_logits(USE))
+        join_logits_kernel<BF16, TN, TM><<<tiles, 256, 0, s>>>(shared);
+      else
+        join_kernel<BF16, USE, TN, TM><<<tiles * TN * TM * 4, 256, 0, s>>>(shared);
       return;
     }
+  }
   tile_kernel<BF16, USE, TN, TM, BUFFERS, false><<<tiles, 256, 0, s>>>(c);
 }
 template <bool BF16, int USE>

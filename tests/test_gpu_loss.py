@@ -138,7 +138,7 @@ class Case:
 
 SIZES = [(1, 1, 1), (1, 5, 7), (2, 64, 64), (3, 129, 100), (16, 1000, 72), (17, 257, 256), (64, 128, 128), (65, 300, 513), (130, 1029, 96),
          (257, 515, 320), (300, 2048, 64), (9, 4099, 129),
-         (70, 700, 328), (2, 534, 1096), (2049, 300, 40)]
+         (70, 700, 328), (2, 534, 1096), (2049, 300, 40), (71, 200, 1200), (40, 300, 1500), (20, 130, 3008)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
