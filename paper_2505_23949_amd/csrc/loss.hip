@@ -453,7 +453,8 @@ int check(const tsenor_distill_problem* p) {
 inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 struct Plans {
-  ProductPlan logits, dh, dweight;
+  ProductPlan logits, dh;
+  HeadPlan dweight;
   bool few;  // logits by the kernel for few tokens
 };
 
@@ -471,7 +472,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.rows = (int)std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
   plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line * (bf16 ? 1 : kPairs), true);
   if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line * (bf16 ? 1 : kPairs), false);
-  if (p.dweight_out) plans.dweight = product_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), false);
+  if (p.dweight_out) plans.dweight = head_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs));
   // (a row's last line goes on into the next row, but not into what lies between the rows of a wider matrix)
   const bool whole = bf16 && p.width && (p.width % line == 0 || (p.width % 8 == 0 && p.weight_ld == p.width)) && p.weight_ld % 8 == 0 &&
                      p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
@@ -518,7 +519,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.head = whole || (plans.few && !p.dh_out) ? p.weight : take(p.vocab * c.states_ld * planes * 2);
   c.head_ld = whole ? p.weight_ld : c.states_ld * planes;
   c.head_bytes = whole ? (int)p.width * 2 : c.states_ld * 2;
-  c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max({plans.logits.workspace, plans.dh.workspace, plans.dweight.workspace})));
+  c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max({plans.logits.workspace, plans.dh.workspace, plans.dweight.parts[0].workspace, plans.dweight.parts[1].workspace})));
   return std::max<size_t>(at, 256);
 }
 
@@ -561,7 +562,11 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     plans.few ? launch_few_logits(piece, bf16, s) : launch_logits(piece, plans.logits, bf16, s);
     launch_rows(piece, bf16, s);
     if (c.dh && c.width) launch_dh(piece, plans.dh, bf16, s);
-    if (c.dweight && c.width) launch_dweight(piece, plans.dweight, bf16, s);
+    if (c.dweight && c.width)
+      for (int k = 0; k < plans.dweight.count; ++k) {
+        piece.head_first = k ? (int)plans.dweight.rows[0] : 0, piece.head_rows = (int)plans.dweight.rows[k];
+        launch_dweight(piece, plans.dweight.parts[k], bf16, s);
+      }
   }
   return status_of_launches();
 }

@@ -44,14 +44,15 @@ struct LossCall {
   void* exps;              // exponentials of the piece, dz_ld to a row: fp16 in the memory of dz (bf16), or fp32
   void* dz;                // of the piece, dz_ld to a row and plane, zeros behind the vocabulary
   float* dweight_sum;      // the head's gradient of the pieces so far (bf16 and more than one piece)
-  floatx4* parts;          // of tiles whose sum `splits` workgroups share
-  int splits;
+  floatx4* parts;          // of tiles whose sums workgroups share
+  int groups;              // workgroups that share the tiles of a product
   int64_t head_ld, states_row;  // states_row: elements from row to row of the states
   int states_ld, dz_ld, head_bytes;  // head_bytes: of a row of a plane of the head
   int tile_n, tiles;       // words of a wave's part of a tile of logits, such parts of a row
   // of the piece
   int first, rows;         // of `order`
   bool last;
+  int head_first, head_rows;  // words whose gradient a launch makes
 };
 
 // rows of the piece that there are

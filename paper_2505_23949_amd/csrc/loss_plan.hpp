@@ -9,6 +9,7 @@
 
 namespace tsenor_dev {
 
+constexpr int kMaxSplits = 128;
 struct ProductPlan {
   Kind kind;  // kSmallTile (64 rows of a x 128 of b), kTile and kTilePairs (128 x 128), kWideTile (256 x 128), kLargeTile (256 x 256)
   int tiles_m, tiles_n, splits;
@@ -24,7 +25,7 @@ inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool logit
                         Cost{kTilePairs, 128, 128, 1.085, 4.5, 2 * kCus, true}, Cost{kWideTile, 256, 128, 0.86, 6.0, kCus, false},
                         Cost{kLargeTile, 256, 256, 1.556, 9.0, kCus, false}}) {
     const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n, tiles = tiles_m * tiles_n;
-    const int64_t most = logits ? (c.rows_m * c.rows_n <= 128 * 128 ? 16 : 1) : 128;
+    const int64_t most = logits ? (c.rows_m * c.rows_n <= 128 * 128 ? 16 : 1) : kMaxSplits;
     for (int64_t splits = 1; splits <= std::min<int64_t>(most, std::max<int64_t>(blocks / 4, 1)); ++splits) {
       if (splits > 1 && (splits - 1) * tiles >= c.at_once) break;
       const double steps = (double)((blocks + splits - 1) / splits) * c.step;
@@ -36,6 +37,27 @@ inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool logit
       if (splits > 1) us += 4.0 + 2.0 * parts / 5.0e6 + (logits ? 0.5 : 0.1) * (double)splits;
       if (best.us == 0.0 || us < best.us) best = {c.kind, (int)tiles_m, (int)tiles_n, (int)splits, us, (size_t)parts};
     }
+  }
+  return best;
+}
+
+// The head's gradient: what does not fill a round of large or wide tiles can go to a launch of its own (us of the kernels, one launch and two:
+// 50257 x 1024 x 1433 175, XXX).
+struct HeadPlan {
+  int count;
+  int64_t rows[2];
+  ProductPlan parts[2];
+};
+inline HeadPlan head_plan(int64_t m, int64_t n, int64_t blocks) {
+  const ProductPlan whole = product_plan(m, n, blocks, false);
+  HeadPlan best = {1, {m, 0}, {whole, {}}};
+  double least = whole.us;
+  for (int rows_n : {128, 256}) {
+    const int64_t tiles_m = (m + 255) / 256, tiles_n = (n + rows_n - 1) / rows_n, rounds = tiles_m * tiles_n / kCus;
+    const int64_t m1 = tiles_n ? rounds * kCus / tiles_n * 256 : 0;
+    if (m1 <= 0 || m1 >= m) continue;
+    const ProductPlan first = product_plan(m1, n, blocks, false), rest = product_plan(m - m1, n, blocks, false);
+    if (first.us + rest.us + 4.0 < least) best = {2, {m1, m - m1}, {first, rest}}, least = first.us + rest.us + 4.0;
   }
   return best;
 }

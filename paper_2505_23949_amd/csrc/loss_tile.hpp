@@ -210,6 +210,9 @@ __device__ __forceinline__ void write_gradient(const LossCall& c, int row, int64
   }
 }
 
+// How many workgroups share the sum of each of `tiles` tiles: more than planned where tokens that are left out leave fewer of them.
+__device__ __forceinline__ int splits_of(const LossCall& c, int tiles) { return min(c.groups / max(tiles, 1), kMaxSplits); }
+
 template <int TN, int TM, int BUFFERS>
 constexpr int kGroupsPerCu = BUFFERS * TileShape<TN, TM>::kBuffer <= 80 * 1024 ? 2 : 1;
 
@@ -301,7 +304,7 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
   }
 }
 
-// SPLIT: c.splits workgroups share the sum of a tile, and each leaves its part in c.parts.
+// SPLIT: several workgroups share the sum of a tile, and each leaves its part in c.parts.
 template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
 __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
   using Shape = TileShape<TN, TM>;
@@ -311,18 +314,20 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
   const int piece = __builtin_amdgcn_readfirstlane(rows_of(c));
-  const int m = USE == kHead ? c.vocab : piece, n = makes_logits(USE) ? c.vocab : c.width;
+  const int m = USE == kHead ? c.head_rows : piece, n = makes_logits(USE) ? c.vocab : c.width;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB;
   const int tiles = tiles_m * tiles_n;
-  if ((int)blockIdx.x >= tiles * (SPLIT ? c.splits : 1)) return;  // (of a piece without tokens that count, all of them)
+  const int splits = SPLIT ? splits_of(c, tiles) : 1;
+  if ((int)blockIdx.x >= tiles * splits) return;  // (of a piece without tokens that count, all of them)
   const int split = SPLIT ? (int)blockIdx.x / tiles : 0;
   const int all_blocks = (makes_logits(USE) ? c.states_ld / 64 : USE == kStates ? c.dz_ld / 64 : (piece + 63) / 64) * (BF16 ? 1 : kPairs);
   if (USE == kHead && all_blocks == 0 && c.first > 0 && !c.last) return;
   int tile_m, tile_n;
   tile_of((int)blockIdx.x - split * tiles, tiles_m, tiles_n, tile_m, tile_n);
-  const int first = SPLIT ? (int)((int64_t)all_blocks * split / c.splits) : 0;
-  const int last = (SPLIT ? (int)((int64_t)all_blocks * (split + 1) / c.splits) : all_blocks) - 1;
+  const int first = SPLIT ? (int)((int64_t)all_blocks * split / splits) : 0;
+  const int last = (SPLIT ? (int)((int64_t)all_blocks * (split + 1) / splits) : all_blocks) - 1;
   const int m0 = tile_m * Shape::kRowsA, n0 = tile_n * Shape::kRowsB;
+  const int first_row = USE == kHead ? c.head_first : 0;
 
   floatx16 sum[TN][TM];
 #pragma unroll
@@ -349,7 +354,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
     else if constexpr (USE == kStates)
       return LoaderAlong<TM, false, false>(c.dz, (int64_t)dz * kPlanes, dz, dz * kPlanes, m0, m, lane, wave, lds_a);
     else
-      return LoaderAcross<TM>(c.dz, (int64_t)dz * kPlanes, dz, m0, piece, lane, wave, lds_a);
+      return LoaderAcross<TM>(c.dz, (int64_t)dz * kPlanes, dz, first_row + m0, piece, lane, wave, lds_a);
   }();
   const auto load = [&](int buffer, int k, int block) {
     const Place<BF16> place(block);
@@ -457,7 +462,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
       const int row = m0 + (wave_m * TM + j) * 32 + r;
-      const int64_t at = (int64_t)(row >= m ? 0 : USE == kStates ? c.order[c.first + row] : row) * c.width;
+      const int64_t at = (int64_t)(row >= m ? 0 : USE == kStates ? c.order[c.first + row] : first_row + row) * c.width;
 #pragma unroll
       for (int t = 0; t < TN; ++t)
 #pragma unroll
@@ -475,7 +480,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
 template <bool BF16, int USE, int TN, int TM>
 __global__ __launch_bounds__(256) void join_kernel(LossCall c) {
   using Shape = TileShape<TN, TM>;
-  const int piece = rows_of(c), m = USE == kHead ? c.vocab : piece;
+  const int piece = rows_of(c), m = USE == kHead ? c.head_rows : piece;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (c.width + Shape::kRowsB - 1) / Shape::kRowsB, tiles = tiles_m * tiles_n;
   const int tile = (int)blockIdx.x / (TN * TM * 4), at_j = (int)blockIdx.x / (4 * TN) % TM, t = (int)blockIdx.x / 4 % TN, g = (int)blockIdx.x % 4;
   if (tile >= tiles || (USE == kHead && piece == 0 && c.first > 0 && !c.last)) return;
@@ -483,20 +488,21 @@ __global__ __launch_bounds__(256) void join_kernel(LossCall c) {
   tile_of(tile, tiles_m, tiles_n, tile_m, tile_n);
   const floatx4* part = c.parts + ((int64_t)tile * (TM * TN * 4) + (at_j * TN + t) * 4 + g) * 256 + threadIdx.x;
   const int64_t step = (int64_t)tiles * (TM * TN * 4) * 256;
+  const int splits = splits_of(c, tiles);
   floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
   int k = 0;
-  for (; k + 8 <= c.splits; k += 8) {
+  for (; k + 8 <= splits; k += 8) {
     floatx4 x[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) x[u] = part[(k + u) * step];
 #pragma unroll
     for (int u = 0; u < 8; ++u) v += x[u];
   }
-  for (; k < c.splits; ++k) v += part[k * step];
+  for (; k < splits; ++k) v += part[k * step];
   const int wave = (int)threadIdx.x / kWave, row = tile_m * Shape::kRowsA + (wave / 2 * TM + at_j) * 32 + (int)threadIdx.x % 32;
   if (row >= m) return;
   const int col = tile_n * Shape::kRowsB + (wave % 2 * TN + t) * 32 + 8 * g + 4 * ((int)threadIdx.x / 32 % 2), n = c.width;
-  const int64_t at = (int64_t)(USE == kStates ? c.order[c.first + row] : row) * n + col;
+  const int64_t at = (int64_t)(USE == kStates ? c.order[c.first + row] : c.head_first + row) * n + col;
   const float scale = c.largest_weight[1];
   float x[4];
 #pragma unroll
@@ -542,7 +548,8 @@ __global__ __launch_bounds__(256) void join_logits_kernel(LossCall c) {
   const floatx4* const part = c.parts + (int64_t)blockIdx.x * (TM * TN * 4) * 256 + threadIdx.x;
   const int64_t step = (int64_t)tiles * (TM * TN * 4) * 256;
   floatx4 v[TM * TN * 4] = {};
-  for (int k = 0; k < c.splits; ++k) {
+  const int splits = splits_of(c, tiles);
+  for (int k = 0; k < splits; ++k) {
 #pragma unroll
     for (int at = 0; at < TM * TN * 4; ++at) v[at] += part[k * step + at * 256];
   }
@@ -563,7 +570,7 @@ void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
   if constexpr (!makes_logits(USE) || TN * TM <= 4) {
     if (plan.splits > 1) {
       LossCall shared = c;
-      shared.splits = plan.splits;
+      shared.groups = (int)tiles * plan.splits;
       tile_kernel<BF16, USE, TN, TM, BUFFERS, true><<<tiles * (unsigned)plan.splits, 256, 0, s>>>(shared);
       if constexpr (makes_logits(USE))
         join_logits_kernel<BF16, TN, TM><<<tiles, 256, 0, s>>>(shared);
