@@ -69,6 +69,8 @@ struct LoaderAlong {
     const int count = min(64 * T, rows - first);
     past = (uint32_t)(count - 1) * (uint32_t)ld_bytes + row_bytes - 16;
     from = resource_of(static_cast<const char*>(p) + first * ld_bytes, (int64_t)past + 16);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) from[k] = __builtin_amdgcn_readfirstlane(from[k]);  // (the same in all lanes: it has to be in scalar registers)
     to = lds + wave * 16 * T * 128;
     plane_bytes = plane_bytes_, whole = row_bytes / 128;
 #pragma unroll
@@ -158,56 +160,41 @@ __device__ __forceinline__ void store4(float* to, const floatx4& v, int col, int
   }
 }
 
-// What a lane holds of tile t of b and j of a: element 4 g + e is row 8 g + 4 q + e of the tile of b.  Columns 32 t + 16 p .. of a wave go
-// out (p: pair of g), 8 of them from each lane (bf16: the halves of the wave exchange fours first) or twice four (fp32).
-template <bool BF16, int USE>
-__device__ __forceinline__ void write_gradient(const LossCall& c, int row, int64_t at, int col, floatx4 lo, floatx4 hi) {
-  // lo, hi: columns col + 4 q and col + 8 + 4 q of the row whose result begins at element `at`
+// Adds columns col + 4 q .. (lo) and col + 8 + 4 q .. (hi) of a row of dW that begins at element `at` to the sums of the pieces before.
+template <bool BF16>
+__device__ __forceinline__ void add_gradient(const LossCall& c, int row, int64_t at, int col, floatx4 lo, floatx4 hi) {
   const int q = (int)threadIdx.x / 32 % 2, n = c.width;
-  float* const sums = USE == kHead && BF16 ? c.dweight_sum : static_cast<float*>(c.dweight);
-  if (USE == kHead && (c.first > 0 || !c.last)) {  // sums of several pieces, in fp32
-    const auto add = [&](floatx4& v, int col) {
-      if (row < 0) return;
-      float* const to = sums + at + col;
-      if (c.first > 0) {
-        float old[4];
-        if (col + 4 <= n) {
-          __builtin_memcpy(old, to, 16);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) old[e] = col + e < n ? to[e] : 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += old[e];
-      }
-      if (!BF16 || !c.last) store4(to, v, col, n);
-    };
-    add(lo, col + 4 * q);
-    add(hi, col + 8 + 4 * q);
-    if (!BF16 || !c.last) return;
-  }
-  void* const out = USE == kStates ? c.dh : c.dweight;
-  if constexpr (BF16) {
-    uint32_t w[4] = {pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const auto r = __builtin_amdgcn_permlane32_swap(w[k], w[2 + k], false, false);
-      w[k] = r[0], w[2 + k] = r[1];
-    }
-    col += 8 * q;
-    uint16_t* const to = static_cast<uint16_t*>(out) + at + col;
+  float* const sums = BF16 ? c.dweight_sum : static_cast<float*>(c.dweight);
+  const auto add = [&](floatx4& v, int col) {
     if (row < 0) return;
-    if (col + 8 <= n) {
-      __builtin_memcpy(to, w, 16);
-    } else {
+    float* const to = sums + at + col;
+    if (c.first > 0) {
+      float old[4];
+      if (col + 4 <= n) {
+        __builtin_memcpy(old, to, 16);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (col + e < n) to[e] = (uint16_t)(w[e / 2] >> (e % 2 * 16));
+        for (int e = 0; e < 4; ++e) old[e] = col + e < n ? to[e] : 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += old[e];
     }
-  } else if (row >= 0) {
-    store4(static_cast<float*>(out) + at + col + 4 * q, lo, col + 4 * q, n);
-    store4(static_cast<float*>(out) + at + col + 8 + 4 * q, hi, col + 8 + 4 * q, n);
-  }
+    if (!BF16 || !c.last) {
+      store4(to, v, col, n);
+    } else {
+      uint16_t* const out = static_cast<uint16_t*>(c.dweight) + at + col;
+      const uint32_t w[2] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+      if (col + 4 <= n) {
+        __builtin_memcpy(out, w, 8);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e < n) out[e] = (uint16_t)(w[e / 2] >> (e % 2 * 16));
+      }
+    }
+  };
+  add(lo, col + 4 * q);
+  add(hi, col + 8 + 4 * q);
 }
 
 // How many workgroups share the sum of each of `tiles` tiles: more than planned where tokens that are left out leave fewer of them.
@@ -216,11 +203,45 @@ __device__ __forceinline__ int splits_of(const LossCall& c, int tiles) { return 
 template <int TN, int TM, int BUFFERS>
 constexpr int kGroupsPerCu = BUFFERS * TileShape<TN, TM>::kBuffer <= 80 * 1024 ? 2 : 1;
 
+// Gradients leave a wave 32 rows at a time, through LDS, so that a store writes whole lines: the lanes hold a few columns of 32 rows each.
+// (1 x 116621 x 5083 in fp32, whose dW is 2.4 GB: 3584 -> 3397 us.  The exponentials, 32 to 64 bytes of a row to a lane, gain nothing by it.)
+template <int TN, int SIZE>
+struct Staged {
+  static constexpr int kRowBytes = 32 * TN * SIZE, kStride = kRowBytes + 16;
+};
+// row_at(row): where a row's columns go, NULL for none; `valid`: bytes of a row that there are
+template <int TN, int SIZE, class RowAt>
+__device__ __forceinline__ void store_staged(const uint8_t* staged, int valid, RowAt row_at) {
+  using S = Staged<TN, SIZE>;
+  constexpr int kPieces = S::kRowBytes / 16;
+  const int lane = (int)threadIdx.x % kWave, piece = lane % kPieces;
+#pragma unroll
+  for (int i = 0; i < 32 * kPieces / kWave; ++i) {
+    const int row = i * (kWave / kPieces) + lane / kPieces;
+    const intx4 v = *reinterpret_cast<const intx4*>(staged + row * S::kStride + piece * 16);
+    char* const to = row_at(row);
+    if (!to) continue;
+    if (piece * 16 + 16 <= valid) {
+      __builtin_memcpy(to + piece * 16, &v, 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16 / SIZE; ++e)
+        if (piece * 16 + (e + 1) * SIZE <= valid) {
+          if constexpr (SIZE == 2)
+            reinterpret_cast<uint16_t*>(to)[piece * 8 + e] = (uint16_t)(v[e / 2] >> (e % 2 * 16));
+          else
+            reinterpret_cast<int*>(to)[piece * 4 + e] = v[e];
+        }
+    }
+  }
+}
+
 // What becomes of a tile of logits.
 template <bool BF16, int TN, int TM>
 __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)[TN][TM], int m, int n, int m0, int n0, uint8_t* lds) {
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
+  uint8_t* const staged = lds + wave * 32 * Staged<TN, 4>::kStride;  // the wave's own
   // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b.  The sums of a row are
   // of those 32 TN columns: no wave waits for another.
   const int wave_col = n0 + wave_n * 32 * TN, col0 = wave_col + 4 * TN * q;
@@ -252,8 +273,7 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
           if (col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
     }
     if (c.dots && __any((entries[j] & 0xFFFFu) != entries[j] >> 16)) {
-      constexpr int kStride = 32 * TN + 4;
-      float* const staged = reinterpret_cast<float*>(lds) + (wave * 32 + r) * kStride;
+      float* const logits = reinterpret_cast<float*>(staged + r * Staged<TN, 4>::kStride);
 #pragma unroll
       for (int g = 0; g < 4; ++g)
 #pragma unroll
@@ -261,11 +281,11 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
           floatx4 v;
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[k] = sum[k % TN][j][4 * g + e + k / TN];
-          *reinterpret_cast<floatx4*>(staged + TN * (8 * g + 4 * q + e)) = v;
+          *reinterpret_cast<floatx4*>(logits + TN * (8 * g + 4 * q + e)) = v;
         }
       for (int i = (int)(entries[j] & 0xFFFFu) + q; i < (int)(entries[j] >> 16); i += 2) {
         const uint32_t key = c.sorted[(int64_t)row * c.k + i];
-        c.dots[(int64_t)row * c.k + (key & 255)] = staged[(int)(key >> 8) - wave_col];
+        c.dots[(int64_t)row * c.k + (key & 255)] = logits[(int)(key >> 8) - wave_col];
       }
     }
     float largest = -__builtin_inff();
@@ -291,8 +311,7 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
         if constexpr (BF16) {
           uint32_t w[2 * TN];
 #pragma unroll
-          for (int k = 0; k < 2 * TN; ++k)
-            w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{x[2 * k], x[2 * k + 1]}, halfx2));
+          for (int k = 0; k < 2 * TN; ++k) w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{x[2 * k], x[2 * k + 1]}, halfx2));
           __builtin_memcpy(__builtin_assume_aligned(static_cast<uint16_t*>(c.exps) + at + col, 16), w, 8 * TN);
         } else {
           __builtin_memcpy(__builtin_assume_aligned(static_cast<float*>(c.exps) + at + col, 16), x, 16 * TN);
@@ -311,6 +330,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   constexpr int kPlanes = BF16 ? 1 : 3;
   constexpr bool kAlongB = makes_logits(USE), kAlongA = USE != kHead;
   __shared__ __align__(1024) uint8_t lds[BUFFERS * Shape::kBuffer];
+  static_assert(4 * 32 * Staged<TN, 4>::kStride <= sizeof(lds));
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
   const int piece = __builtin_amdgcn_readfirstlane(rows_of(c));
@@ -459,19 +479,53 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
               floatx4{sum[t][j][4 * g], sum[t][j][4 * g + 1], sum[t][j][4 * g + 2], sum[t][j][4 * g + 3]};
   } else {
     const float scale = c.largest_weight[1];
+    constexpr int kSize = BF16 ? 2 : 4;
+    using Rows = Staged<TN, kSize>;
+    uint8_t* const staged = lds + wave * 32 * Rows::kStride;
+    const int wave_col = n0 + wave_n * 32 * TN;
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
       const int row = m0 + (wave_m * TM + j) * 32 + r;
-      const int64_t at = (int64_t)(row >= m ? 0 : USE == kStates ? c.order[c.first + row] : first_row + row) * c.width;
+      TSENOR_IN_ORDER();
 #pragma unroll
       for (int t = 0; t < TN; ++t)
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          floatx4 lo, hi;
+        for (int k = j; k < TM; ++k) asm volatile("" : "+a"(sum[t][k]));  // (accumulators stay what they are until their turn)
+      if (USE == kHead && (c.first > 0 || !c.last)) {  // sums of several pieces
+        const int64_t at = (int64_t)(row >= m ? 0 : first_row + row) * c.width;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) lo[e] = sum[t][j][8 * p + e] * scale, hi[e] = sum[t][j][8 * p + 4 + e] * scale;
-          write_gradient<BF16, USE>(c, row < m ? row : -1, at, n0 + (wave_n * TN + t) * 32 + 16 * p, lo, hi);
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            floatx4 lo, hi;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) lo[e] = sum[t][j][8 * p + e] * scale, hi[e] = sum[t][j][8 * p + 4 + e] * scale;
+            add_gradient<BF16>(c, row < m ? row : -1, at, wave_col + t * 32 + 16 * p, lo, hi);
+          }
+        continue;
+      }
+#pragma unroll
+      for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = sum[t][j][4 * g + e] * scale;
+          uint8_t* const to = staged + r * Rows::kStride + (32 * t + 8 * g + 4 * q) * kSize;
+          if constexpr (BF16) {
+            const uint32_t w[2] = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+            __builtin_memcpy(__builtin_assume_aligned(to, 8), w, 8);
+          } else {
+            __builtin_memcpy(__builtin_assume_aligned(to, 16), x, 16);
+          }
         }
+      // (kStates: lanes 0 to 31 know which token each row is of)
+      const int token = USE == kStates ? c.order[c.first + min(row, m - 1)] : 0;
+      char* const out = static_cast<char*>(USE == kStates ? c.dh : c.dweight) + (int64_t)wave_col * kSize;
+      store_staged<TN, kSize>(staged, (n - wave_col) * kSize, [&](int k) -> char* {
+        const int to = USE == kStates ? __shfl(token, k) : first_row + m0 + (wave_m * TM + j) * 32 + k;
+        return m0 + (wave_m * TM + j) * 32 + k < m ? out + (int64_t)to * n * kSize : nullptr;
+      });
     }
   }
 }
@@ -539,7 +593,7 @@ __global__ __launch_bounds__(256) void join_kernel(LossCall c) {
 template <bool BF16, int TN, int TM>
 __global__ __launch_bounds__(256) void join_logits_kernel(LossCall c) {
   using Shape = TileShape<TN, TM>;
-  __shared__ __align__(16) uint8_t lds[4 * 32 * (32 * TN + 4) * 4];
+  __shared__ __align__(16) uint8_t lds[4 * 32 * Staged<TN, 4>::kStride];
   const int m = rows_of(c), n = c.vocab;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB, tiles = tiles_m * tiles_n;
   if ((int)blockIdx.x >= tiles) return;
