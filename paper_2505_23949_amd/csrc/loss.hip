@@ -198,6 +198,33 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
     load_row8<BF16>(h, k, c.width, x);
     store_planes<BF16>(state, c.states_ld, k, x);
   }
+  // a number that its exponentials can be counted from: the largest logit of up to four of its entries
+  if (c.refs) {
+    __shared__ float most[kThreads / kWave];
+    const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+    float z = -__builtin_inff();
+    for (int i = wave; i < c.k; i += kThreads / kWave) {
+      const int64_t id = c.ids[(int64_t)token * c.ids_ld + i];
+      if (id < 0 || id >= c.vocab) continue;
+      const char* const w = static_cast<const char*>(c.weight) + id * c.weight_ld * kSize;
+      float s = 0.0f;
+      for (int k = lane * 8; k < c.width; k += kWave * 8) {
+        float y[8];
+        load_row8<BF16>(h, k, c.width, x);
+        load_row8<BF16>(w, k, c.width, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
+      }
+      z = wave_sum(s);
+      break;
+    }
+    if (lane == 0) most[wave] = z;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      c.refs[row] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * c.scale;
+      if (row == 0) *c.again = 0;
+    }
+  }
   if (!c.dots) return;
 
   // its entries by word, and where those of each part of a tile begin
@@ -348,17 +375,19 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
     if (c.lse) c.lse[token] = (largest + lse) * kLn2;
   }
   if (!c.dz) return;
+  const bool ready = c.refs && !*c.again;  // the exponentials are dz but for 1 / total and the weight
+  if (c.row_scale && threadIdx.x == 0) c.row_scale[row] = ready ? make_float2(1.0f / total, weight) : make_float2(1.0f, 1.0f);
   // (the same word twice: both write what belongs to both)
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
     float p = 0.0f;
     for (int j = 0; j < c.k; ++j)
       if (words[j] == words[i]) p += q[j];
-    dentry[i] = weight * (dentry[i] - p);
+    dentry[i] = (ready ? total : weight) * (dentry[i] - p);
   }
   const float share = weight / total;
   uint16_t* const dz = static_cast<uint16_t*>(c.dz) + (int64_t)row * c.dz_ld * (BF16 ? 1 : 3);
   const char* const exps = static_cast<const char*>(c.exps) + (int64_t)row * c.dz_ld * kSize;
-  for (int k = (int)threadIdx.x * 8; k < c.dz_ld; k += THREADS * 8) {
+  for (int k = (int)threadIdx.x * 8; k < c.dz_ld && !ready; k += THREADS * 8) {
     const float scale = share * __builtin_amdgcn_exp2f(sums[min(k / c.tile_n, c.tiles - 1)].x - largest);
     float x[8];
     if constexpr (BF16) {
@@ -418,6 +447,7 @@ constexpr int64_t kMaxTokens = (int64_t)1 << 24, kMaxVocab = (int64_t)1 << 21, k
 constexpr int64_t kPieceBytes = (int64_t)1 << 31;  // of dz; a tenth of it for the sums of the tiles of a piece
 constexpr int64_t kMaxTileLd = (int64_t)1 << 21;   // (the tile kernels' offsets within a tile have 31 bits)
 constexpr double kLog2e = 1.4426950408889634;
+constexpr int64_t kWithoutPass = 20000000;          // logits (512 x 32000 x 4096, 16.4 million: 274.5 us with the pass, 279 without)
 constexpr int kPieceRows = 256;                    // pieces are a multiple of this
 
 int check(const tsenor_head& p) {
@@ -512,6 +542,12 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
     c.dots = reinterpret_cast<float*>(take((int64_t)c.rows * c.k * 4));
     c.sorted = reinterpret_cast<uint32_t*>(take((int64_t)c.rows * c.k * 4));
     c.begins = reinterpret_cast<uint16_t*>(take((int64_t)c.rows * (c.tiles + 1) * 2));
+  }
+  // dh alone: without the pass that makes dz of the exponentials, where that costs more (4 bytes a logit at 4.8 TB/s) than what is in its place
+  if (bf16 && p.dh_out && !p.dweight_out && plans.logits.kind == kLargeTile && (int64_t)c.rows * p.vocab >= kWithoutPass) {
+    c.refs = reinterpret_cast<float*>(take((int64_t)c.rows * 4));
+    c.again = reinterpret_cast<int*>(take(4));
+    c.row_scale = reinterpret_cast<float2*>(take((int64_t)c.rows * 8));
   }
   c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * planes * 2) : nullptr;
   c.exps = gradients && !bf16 ? take((int64_t)c.rows * c.dz_ld * 4) : c.dz;

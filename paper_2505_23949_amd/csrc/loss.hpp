@@ -41,6 +41,11 @@ struct LossCall {
   float* dots;             // of each row and entry
   uint32_t* sorted;        // of each row: its k entries by word, word << 8 | entry, those that take no part behind
   uint16_t* begins;        // of each row and part of a tile, and once more: how many entries stand before it
+  // Exponentials counted from one number for a row (bf16, dh alone): they are dz but for a factor of the row, which dh takes at the end, and
+  // its entries.  The number comes from the logits of some of the row's entries before all others are known.
+  float* refs;             // of each row; NULL: counted from the largest logit of each part of a tile
+  int* again;              // not 0: a row has exponentials too far above its number, and all are made again the other way
+  float2* row_scale;       // of each row: what dh is multiplied with, in two factors
   void* exps;              // exponentials of the piece, dz_ld to a row: fp16 in the memory of dz (bf16), or fp32
   void* dz;                // of the piece, dz_ld to a row and plane, zeros behind the vocabulary
   float* dweight_sum;      // the head's gradient of the pieces so far (bf16 and more than one piece)

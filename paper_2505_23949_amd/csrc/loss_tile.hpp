@@ -1,6 +1,7 @@
 // The tile kernel of the losses' products, C[row][col] = sum_k a(row, k) b(col, k), in its three uses:
 //   kLogits   a: states   (along the sum)    b: head (along)        z = h W^T, its rows' sums and exponentials
 //   kLogitsInPlace                              the same, of a head whose rows end inside a line of 128 bytes
+//   kLogitsCounted, kLogitsInPlaceCounted       the same, exponentials counted from c.refs
 //   kStates   a: dz       (along)            b: head (across)       dh = dz W
 //   kHead     a: dz       (across)           b: states (across)     dW = dz^T h
 // "Along": a row of the operand lies along the sum in memory.  "Across": the sum goes from row to row of memory.
@@ -16,8 +17,10 @@ typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-enum Use { kLogits, kLogitsInPlace, kStates, kHead };
-constexpr bool makes_logits(int use) { return use == kLogits || use == kLogitsInPlace; }
+enum Use { kLogits, kLogitsInPlace, kLogitsCounted, kLogitsInPlaceCounted, kStates, kHead };
+constexpr bool makes_logits(int use) { return use < kStates; }
+constexpr bool is_counted(int use) { return use == kLogitsCounted || use == kLogitsInPlaceCounted; }
+constexpr bool is_in_place(int use) { return use == kLogitsInPlace || use == kLogitsInPlaceCounted; }
 
 // A workgroup of four waves, two by two, takes 64 TN rows of b (columns of the result) and 64 TM rows of a; a wave 32 TN x 32 TM results
 // in accumulators, of the 32 x 32 matrix instructions whose first operand is b: a lane holds four neighbouring columns of a row.
@@ -236,8 +239,12 @@ __device__ __forceinline__ void store_staged(const uint8_t* staged, int valid, R
   }
 }
 
+// Exponentials of a row counted from one number: sums up to here are taken (2^21 of them stay far inside single precision, and what they
+// are divided by, times a weight, inside its other end).
+constexpr float kMostOverRef = 0x1p60f;
+
 // What becomes of a tile of logits.
-template <bool BF16, int TN, int TM>
+template <bool BF16, bool COUNTED, int TN, int TM>
 __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)[TN][TM], int m, int n, int m0, int n0, uint8_t* lds) {
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
@@ -294,6 +301,7 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
 #pragma unroll
       for (int e = 0; e < 16; ++e) largest = fmaxf(largest, sum[t][j][e]);
     largest = fmaxf(largest, lane_xor<32>(largest)) * c.scale - kExpBits;
+    if (COUNTED && row < m) largest = c.refs[row];
     const float base = largest == -__builtin_inff() ? 0.0f : largest;
     float v = 0.0f;
 #pragma unroll
@@ -311,7 +319,8 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
         if constexpr (BF16) {
           uint32_t w[2 * TN];
 #pragma unroll
-          for (int k = 0; k < 2 * TN; ++k) w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{x[2 * k], x[2 * k + 1]}, halfx2));
+          for (int k = 0; k < 2 * TN; ++k)
+            w[k] = COUNTED ? pack_bf16(x[2 * k], x[2 * k + 1]) : __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{x[2 * k], x[2 * k + 1]}, halfx2));
           __builtin_memcpy(__builtin_assume_aligned(static_cast<uint16_t*>(c.exps) + at + col, 16), w, 8 * TN);
         } else {
           __builtin_memcpy(__builtin_assume_aligned(static_cast<float*>(c.exps) + at + col, 16), x, 16 * TN);
@@ -319,18 +328,18 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
       }
     }
     v += lane_xor<32>(v);
+    if (COUNTED && row < m && v > kMostOverRef) *c.again = 1;  // (whoever finds one writes the same)
     if (q == 0 && row < m && wave_col < n) c.sums[(int64_t)row * c.tiles + wave_col / (32 * TN)] = make_float2(largest, v);
   }
 }
 
 // SPLIT: several workgroups share the sum of a tile, and each leaves its part in c.parts.
 template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
-__global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
+__device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* lds) {
   using Shape = TileShape<TN, TM>;
   constexpr int kPlanes = BF16 ? 1 : 3;
   constexpr bool kAlongB = makes_logits(USE), kAlongA = USE != kHead;
-  __shared__ __align__(1024) uint8_t lds[BUFFERS * Shape::kBuffer];
-  static_assert(4 * 32 * Staged<TN, 4>::kStride <= sizeof(lds));
+  static_assert(4 * 32 * Staged<TN, 4>::kStride <= BUFFERS * Shape::kBuffer);
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
   const int piece = __builtin_amdgcn_readfirstlane(rows_of(c));
@@ -338,12 +347,12 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB;
   const int tiles = tiles_m * tiles_n;
   const int splits = SPLIT ? splits_of(c, tiles) : 1;
-  if ((int)blockIdx.x >= tiles * splits) return;  // (of a piece without tokens that count, all of them)
-  const int split = SPLIT ? (int)blockIdx.x / tiles : 0;
+  if (id >= tiles * splits) return;  // (of a piece without tokens that count, all of them)
+  const int split = SPLIT ? id / tiles : 0;
   const int all_blocks = (makes_logits(USE) ? c.states_ld / 64 : USE == kStates ? c.dz_ld / 64 : (piece + 63) / 64) * (BF16 ? 1 : kPairs);
   if (USE == kHead && all_blocks == 0 && c.first > 0 && !c.last) return;
   int tile_m, tile_n;
-  tile_of((int)blockIdx.x - split * tiles, tiles_m, tiles_n, tile_m, tile_n);
+  tile_of(id - split * tiles, tiles_m, tiles_n, tile_m, tile_n);
   const int first = SPLIT ? (int)((int64_t)all_blocks * split / splits) : 0;
   const int last = (SPLIT ? (int)((int64_t)all_blocks * (split + 1) / splits) : all_blocks) - 1;
   const int m0 = tile_m * Shape::kRowsA, n0 = tile_n * Shape::kRowsB;
@@ -361,7 +370,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   const int states = c.states_ld * 2, dz = c.dz_ld * 2;  // bytes of a row of a plane (of the head: as of the states)
   const auto of_b = [&] {
     if constexpr (makes_logits(USE))
-      return LoaderAlong<TN, true, USE == kLogitsInPlace>(c.head, c.head_ld * 2, states, c.head_bytes * kPlanes, n0, n, lane, wave, lds_at);
+      return LoaderAlong<TN, true, is_in_place(USE)>(c.head, c.head_ld * 2, states, c.head_bytes * kPlanes, n0, n, lane, wave, lds_at);
     else if constexpr (USE == kStates)
       return LoaderAcross<TN>(c.head, c.head_ld * 2, c.head_bytes, n0, c.vocab, lane, wave, lds_at);
     else
@@ -467,7 +476,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
   meet<0>();  // (no load into LDS outlives the workgroup)
 
   if constexpr (makes_logits(USE) && !SPLIT) {
-    finish_logits<BF16, TN, TM>(c, sum, m, n, m0, n0, lds);
+    finish_logits<BF16, is_counted(USE), TN, TM>(c, sum, m, n, m0, n0, lds);
   } else if constexpr (SPLIT) {
 #pragma unroll
     for (int j = 0; j < TM; ++j)
@@ -475,7 +484,7 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
       for (int t = 0; t < TN; ++t)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          c.parts[((int64_t)blockIdx.x * (TM * TN * 4) + (j * TN + t) * 4 + g) * 256 + threadIdx.x] =
+          c.parts[((int64_t)id * (TM * TN * 4) + (j * TN + t) * 4 + g) * 256 + threadIdx.x] =
               floatx4{sum[t][j][4 * g], sum[t][j][4 * g + 1], sum[t][j][4 * g + 2], sum[t][j][4 * g + 3]};
   } else {
     const float scale = c.largest_weight[1];
@@ -504,13 +513,15 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
           }
         continue;
       }
+      const float2 factors = USE == kStates && c.row_scale ? c.row_scale[min(row, m - 1)] : make_float2(1.0f, 1.0f);
+      const float of_row = factors.y * scale;
 #pragma unroll
       for (int t = 0; t < TN; ++t)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           float x[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = sum[t][j][4 * g + e] * scale;
+          for (int e = 0; e < 4; ++e) x[e] = sum[t][j][4 * g + e] * factors.x * of_row;
           uint8_t* const to = staged + r * Rows::kStride + (32 * t + 8 * g + 4 * q) * kSize;
           if constexpr (BF16) {
             const uint32_t w[2] = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -527,6 +538,23 @@ __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_ker
         return m0 + (wave_m * TM + j) * 32 + k < m ? out + (int64_t)to * n * kSize : nullptr;
       });
     }
+  }
+}
+
+template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
+__global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
+  __shared__ __align__(1024) uint8_t lds[BUFFERS * TileShape<TN, TM>::kBuffer];
+  tile<BF16, USE, TN, TM, BUFFERS, SPLIT>(c, (int)blockIdx.x, lds);
+}
+
+// all of them once more, should that be needed, by as many workgroups as run at a time
+template <int USE>
+__global__ __launch_bounds__(256) void logits_again_kernel(LossCall c, int tiles) {
+  __shared__ __align__(1024) uint8_t lds[2 * TileShape<4, 4>::kBuffer];
+  if (!*c.again) return;
+  for (int id = (int)blockIdx.x; id < tiles; id += (int)gridDim.x) {
+    tile<true, USE, 4, 4, 2, false>(c, id, lds);
+    __syncthreads();
   }
 }
 
@@ -557,10 +585,11 @@ __global__ __launch_bounds__(256) void join_kernel(LossCall c) {
   if (row >= m) return;
   const int col = tile_n * Shape::kRowsB + (wave % 2 * TN + t) * 32 + 8 * g + 4 * ((int)threadIdx.x / 32 % 2), n = c.width;
   const int64_t at = (int64_t)(USE == kStates ? c.order[c.first + row] : c.head_first + row) * n + col;
-  const float scale = c.largest_weight[1];
+  const float2 factors = USE == kStates && c.row_scale ? c.row_scale[row] : make_float2(1.0f, 1.0f);
+  const float of_row = factors.y * c.largest_weight[1];
   float x[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = v[e] * scale;
+  for (int e = 0; e < 4; ++e) x[e] = v[e] * factors.x * of_row;
   if constexpr (USE == kHead) {
     float* const sums = (BF16 ? c.dweight_sum : static_cast<float*>(c.dweight)) + at;
 #pragma unroll
@@ -614,7 +643,7 @@ __global__ __launch_bounds__(256) void join_logits_kernel(LossCall c) {
     for (int t = 0; t < TN; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sum[t][j][e] = v[(j * TN + t) * 4 + e / 4][e % 4];
-  finish_logits<BF16, TN, TM>(c, sum, m, n, tile_m * Shape::kRowsA, tile_n * Shape::kRowsB, lds);
+  finish_logits<BF16, false, TN, TM>(c, sum, m, n, tile_m * Shape::kRowsA, tile_n * Shape::kRowsB, lds);
 }
 
 // the kernel with the tiles of a plan

@@ -294,6 +294,31 @@ def test_nothing_to_do(loss):
     assert not out.any() and not dh.any()
 
 
+@pytest.mark.parametrize("k", [0, 5])
+@pytest.mark.parametrize("far", [False, True])
+def test_dh_alone_of_many_logits(loss, k, far):
+    """Exponentials counted from a row's own entries; `far`: entries that the largest logit is hundreds above, for which that does not do."""
+    case = Case(1017, 20479, 1544, "bf16", k=k, left_out=0.05, temperature=1.3 if k else 1.0)
+    if far:
+        # word 7 is worth 300 to token 3 and its like, whose entries are none of it
+        case.h[3:1000:31, 0] = 40.0
+        case.weight[7, 0] = 8.0
+        if k:
+            case.ids[:, 0] = torch.where(case.ids[:, 0] == 7, 8, case.ids[:, 0])
+        else:
+            case.targets[case.targets == 7] = 8
+    case.reference().run(loss, dweight=False).check()
+    if far:
+        assert float(case.out["loss"].max()) > 150
+    case.h[10, 3] = math.nan
+    out = case.out["dh"].clone()
+    case.run(loss, dweight=False)
+    keep = torch.arange(1017) != 10
+    assert torch.isnan(case.out["loss"].cpu()[10]) == (case.want["loss"][10] != 0)
+    assert torch.isfinite(case.out["dh"].float().cpu()[keep]).all()
+    assert torch.equal(case.out["dh"].cpu()[keep], out.cpu()[keep])
+
+
 # ---- gradients against differences -------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("k,temperature", [(0, 1.0), (6, 1.5)])
