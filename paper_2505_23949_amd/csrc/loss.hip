@@ -506,9 +506,9 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   // (a row's last line goes on into the next row, but not into what lies between the rows of a wider matrix)
   const bool whole = bf16 && p.width && (p.width % line == 0 || (p.width % 8 == 0 && p.weight_ld == p.width)) && p.weight_ld % 8 == 0 &&
                      p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
-  // up to 16 tokens: straight from memory, where tiles would need a copy of the head that nothing else needs, or are few (us of the call:
+  // up to 16 tokens: straight from memory in fp32, where tiles would need a copy of the head that nothing else needs, or are few (us of the call:
   // 3 x 1216 x 2326 27.4, 10.4 so, 4 x 1650 x 6912 with dh 58.3, 39.6; but 1 x 32000 x 2048 29.0, 33.6)
-  plans.few = p.tokens <= kFewTokens && (p.vocab < 64 * kCus || (!whole && !p.dh_out));
+  plans.few = p.tokens <= kFewTokens && (!bf16 || p.vocab < 64 * kCus || (!whole && !p.dh_out));
   c.tile_n = plans.few ? kFewWords : plans.logits.kind == kLargeTile ? 128 : 64;
   c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
   size_t at = 0;
