@@ -15,7 +15,7 @@ ROOT = PKG.parent
 CSRC = PKG / "csrc"
 SOURCES = ([CSRC / "tsenor.hip"] + [CSRC / f"launch_m{m}.hip" for m in (64, 32, 16, 8, 4)]
            + [CSRC / f"layer_{name}.hip" for name in ("quantize", "norm", "product", "clip")]
-           + [CSRC / f"{name}.hip" for name in ("loss", "loss_few", "loss_logits", "loss_dh", "loss_dweight")])
+           + [CSRC / f"{name}.hip" for name in ("loss", "loss_few", "loss_logits", "loss_dh", "loss_dweight", "loss_both")])
 OUTPUT = PKG / "libtsenor.so"
 OBJ_DIR = PKG / "_build"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

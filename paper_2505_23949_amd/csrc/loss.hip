@@ -1,5 +1,6 @@
 // tsenor_cross_entropy, tsenor_distill: host side, and the kernels that go through tokens (the products: loss_tile.hpp).
 #include <algorithm>
+#include <type_traits>
 
 #include "loss.hpp"
 
@@ -257,12 +258,14 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
   }
 }
 
-// the head with rows of whole lines: a workgroup to a row
+// the head with rows of whole lines: a workgroup to a row, or to as many short ones as have 8 elements for each thread
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* head) {
-  const char* const from = static_cast<const char*>(c.weight) + (int64_t)blockIdx.x * c.weight_ld * (BF16 ? 2 : 4);
-  uint16_t* const to = head + (int64_t)blockIdx.x * c.head_ld;
-  for (int k = (int)threadIdx.x * 8; k < c.states_ld; k += kThreads * 8) {
+__global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* head, int rows) {
+  const int threads = kThreads / rows, of_group = (int)threadIdx.x / threads, row = (int)blockIdx.x * rows + of_group;
+  if (of_group >= rows || row >= c.vocab) return;
+  const char* const from = static_cast<const char*>(c.weight) + (int64_t)row * c.weight_ld * (BF16 ? 2 : 4);
+  uint16_t* const to = head + (int64_t)row * c.head_ld;
+  for (int k = (int)threadIdx.x % threads * 8; k < c.states_ld; k += threads * 8) {
     float x[8];
     load_row8<BF16>(from, k, c.width, x);
     store_planes<BF16>(to, c.states_ld, k, x);
@@ -387,20 +390,28 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   const float share = weight / total;
   uint16_t* const dz = static_cast<uint16_t*>(c.dz) + (int64_t)row * c.dz_ld * (BF16 ? 1 : 3);
   const char* const exps = static_cast<const char*>(c.exps) + (int64_t)row * c.dz_ld * kSize;
-  for (int k = (int)threadIdx.x * 8; k < c.dz_ld && !ready; k += THREADS * 8) {
-    const float scale = share * __builtin_amdgcn_exp2f(sums[min(k / c.tile_n, c.tiles - 1)].x - largest);
-    float x[8];
-    if constexpr (BF16) {
-      _Float16 y[8];
-      __builtin_memcpy(y, exps + k * 2, 16);
+  constexpr int kAtOnce = 4;  // that a thread has asked for at a time
+  for (int k0 = (int)threadIdx.x * 8; k0 < c.dz_ld && !ready; k0 += kAtOnce * THREADS * 8) {
+    typedef typename std::conditional<BF16, _Float16, float>::type Exp;
+    Exp y[kAtOnce][8];
+    float scale[kAtOnce];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (float)y[e];
-    } else {
-      __builtin_memcpy(x, exps + k * 4, 32);
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int k = k0 + u * THREADS * 8;
+      if (k >= c.dz_ld) continue;
+      __builtin_memcpy(y[u], exps + k * kSize, 8 * kSize);
+      scale[u] = sums[min(k / c.tile_n, c.tiles - 1)].x;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = k + e < c.vocab ? x[e] * scale : 0.0f;
-    store_planes<BF16>(dz, c.dz_ld, k, x);
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int k = k0 + u * THREADS * 8;
+      if (k >= c.dz_ld) continue;
+      const float factor = share * __builtin_amdgcn_exp2f(scale[u] - largest);
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = k + e < c.vocab ? (float)y[u][e] * factor : 0.0f;
+      store_planes<BF16>(dz, c.dz_ld, k, x);
+    }
   }
   __syncthreads();
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
@@ -485,6 +496,7 @@ inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; 
 struct Plans {
   ProductPlan logits, dh;
   HeadPlan dweight;
+  BothPlan both;
   bool few;  // logits by the kernel for few tokens
 };
 
@@ -503,6 +515,11 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line * (bf16 ? 1 : kPairs), true);
   if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line * (bf16 ? 1 : kPairs), false);
   if (p.dweight_out) plans.dweight = head_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs));
+  if (p.dh_out && p.dweight_out) {
+    const double apart = plans.dh.us + plans.dweight.parts[0].us + plans.dweight.parts[1].us + 4.0 * plans.dweight.count;
+    plans.both = both_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, p.width, c.dz_ld / line * (bf16 ? 1 : kPairs),
+                           (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), apart);
+  }
   // (a row's last line goes on into the next row, but not into what lies between the rows of a wider matrix)
   const bool whole = bf16 && p.width && (p.width % line == 0 || (p.width % 8 == 0 && p.weight_ld == p.width)) && p.weight_ld % 8 == 0 &&
                      p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
@@ -555,7 +572,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans)
   c.head = whole || (plans.few && !p.dh_out) ? p.weight : take(p.vocab * c.states_ld * planes * 2);
   c.head_ld = whole ? p.weight_ld : c.states_ld * planes;
   c.head_bytes = whole ? (int)p.width * 2 : c.states_ld * 2;
-  c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max({plans.logits.workspace, plans.dh.workspace, plans.dweight.parts[0].workspace, plans.dweight.parts[1].workspace})));
+  c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max({plans.logits.workspace, plans.dh.workspace, plans.dweight.parts[0].workspace, plans.dweight.parts[1].workspace, plans.both.dh.workspace + plans.both.dweight.workspace})));
   return std::max<size_t>(at, 256);
 }
 
@@ -585,7 +602,9 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
   if (!alone) order_kernel<<<1, kOrderThreads, 0, s>>>(c);
   if (c.head != c.weight) {
     uint16_t* const head = static_cast<uint16_t*>(const_cast<void*>(c.head));
-    bf16 ? head_kernel<true><<<(unsigned)c.vocab, kThreads, 0, s>>>(c, head) : head_kernel<false><<<(unsigned)c.vocab, kThreads, 0, s>>>(c, head);
+    const int rows = std::max(1, std::min(kThreads / 8, kThreads * 8 / c.states_ld));  // (93469 x 76 30 -> XXX us)
+    const unsigned groups = (unsigned)((c.vocab + rows - 1) / rows);
+    bf16 ? head_kernel<true><<<groups, kThreads, 0, s>>>(c, head, rows) : head_kernel<false><<<groups, kThreads, 0, s>>>(c, head, rows);
   }
   for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
     LossCall piece = c;
@@ -597,6 +616,11 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
       bf16 ? gather_kernel<true, false><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false, false><<<padded, kThreads, 0, s>>>(piece);
     plans.few ? launch_few_logits(piece, bf16, s) : launch_logits(piece, plans.logits, bf16, s);
     launch_rows(piece, bf16, s);
+    if (plans.both.use && c.width) {
+      piece.head_first = 0, piece.head_rows = c.vocab;
+      launch_both(piece, plans.both, bf16, s);
+      continue;
+    }
     if (c.dh && c.width) launch_dh(piece, plans.dh, bf16, s);
     if (c.dweight && c.width)
       for (int k = 0; k < plans.dweight.count; ++k) {

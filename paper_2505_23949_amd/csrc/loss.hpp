@@ -74,6 +74,7 @@ constexpr int kFewTokens = 16, kFewWords = 16;  // words of a workgroup, and of 
 void launch_few_logits(const LossCall& c, bool bf16, hipStream_t s);
 void launch_logits(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
 void launch_dh(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
+void launch_both(const LossCall& c, const BothPlan& plan, bool bf16, hipStream_t s);  // dh and dW
 void launch_dweight(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
 
 }  // namespace tsenor_dev

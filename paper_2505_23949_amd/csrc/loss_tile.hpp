@@ -340,8 +340,9 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
   }
 }
 
-// SPLIT: several workgroups share the sum of a tile, and each leaves its part in c.parts.
-template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
+// SPLIT: several workgroups share the sum of a tile, and each leaves its part in c.parts.  kMaybe: where c.groups says so.
+enum Split { kNever, kAlways, kMaybe };
+template <bool BF16, int USE, int TN, int TM, int BUFFERS, int SPLIT>
 __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* lds) {
   using Shape = TileShape<TN, TM>;
   constexpr int kPlanes = BF16 ? 1 : 3;
@@ -353,15 +354,16 @@ __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* l
   const int m = USE == kHead ? c.head_rows : piece, n = makes_logits(USE) ? c.vocab : c.width;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB;
   const int tiles = tiles_m * tiles_n;
-  const int splits = SPLIT ? splits_of(c, tiles) : 1;
+  const bool shared = SPLIT == kAlways || (SPLIT == kMaybe && c.groups > 0);
+  const int splits = shared ? splits_of(c, tiles) : 1;
   if (id >= tiles * splits) return;  // (of a piece without tokens that count, all of them)
-  const int split = SPLIT ? id / tiles : 0;
+  const int split = shared ? id / tiles : 0;
   const int per = makes_logits(USE) ? c.states_ld / 64 : USE == kStates ? c.dz_ld / 64 : (piece + 63) / 64, all_blocks = per * (BF16 ? 1 : kPairs);
   if (USE == kHead && all_blocks == 0 && c.first > 0 && !c.last) return;
   int tile_m, tile_n;
   tile_of(id - split * tiles, tiles_m, tiles_n, tile_m, tile_n);
-  const int first = SPLIT ? (int)((int64_t)all_blocks * split / splits) : 0;
-  const int last = (SPLIT ? (int)((int64_t)all_blocks * (split + 1) / splits) : all_blocks) - 1;
+  const int first = shared ? (int)((int64_t)all_blocks * split / splits) : 0;
+  const int last = (shared ? (int)((int64_t)all_blocks * (split + 1) / splits) : all_blocks) - 1;
   const int m0 = tile_m * Shape::kRowsA, n0 = tile_n * Shape::kRowsB;
   const int first_row = USE == kHead ? c.head_first : 0;
 
@@ -481,18 +483,21 @@ __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* l
 #undef LATE
   meet<0>();  // (no load into LDS outlives the workgroup)
 
-  if constexpr (makes_logits(USE) && !SPLIT) {
+  if constexpr (makes_logits(USE) && SPLIT == kNever) {
     finish_logits<BF16, is_counted(USE), TN, TM>(c, sum, m, n, m0, n0, lds);
-  } else if constexpr (SPLIT) {
-#pragma unroll
-    for (int j = 0; j < TM; ++j)
-#pragma unroll
-      for (int t = 0; t < TN; ++t)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          c.parts[((int64_t)id * (TM * TN * 4) + (j * TN + t) * 4 + g) * 256 + threadIdx.x] =
-              floatx4{sum[t][j][4 * g], sum[t][j][4 * g + 1], sum[t][j][4 * g + 2], sum[t][j][4 * g + 3]};
   } else {
+    if (shared) {
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            c.parts[((int64_t)id * (TM * TN * 4) + (j * TN + t) * 4 + g) * 256 + threadIdx.x] =
+                floatx4{sum[t][j][4 * g], sum[t][j][4 * g + 1], sum[t][j][4 * g + 2], sum[t][j][4 * g + 3]};
+      return;
+    }
+    if constexpr (makes_logits(USE)) return;
     const float scale = c.largest_weight[1];
     constexpr int kSize = BF16 ? 2 : 4;
     using Rows = Staged<TN, kSize>;
@@ -547,7 +552,7 @@ __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* l
   }
 }
 
-template <bool BF16, int USE, int TN, int TM, int BUFFERS, bool SPLIT>
+template <bool BF16, int USE, int TN, int TM, int BUFFERS, int SPLIT>
 __global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
   __shared__ __align__(1024) uint8_t lds[BUFFERS * TileShape<TN, TM>::kBuffer];
   tile<BF16, USE, TN, TM, BUFFERS, SPLIT>(c, (int)blockIdx.x, lds);
@@ -559,18 +564,18 @@ __global__ __launch_bounds__(256) void logits_again_kernel(LossCall c, int tiles
   __shared__ __align__(1024) uint8_t lds[2 * TileShape<4, 4>::kBuffer];
   if (!*c.again) return;
   for (int id = (int)blockIdx.x; id < tiles; id += (int)gridDim.x) {
-    tile<true, USE, 4, 4, 2, false>(c, id, lds);
+    tile<true, USE, 4, 4, 2, kNever>(c, id, lds);
     __syncthreads();
   }
 }
 
 // adds the parts of a tile in their order: a workgroup for each tile and 4 TN TM-th of it
 template <bool BF16, int USE, int TN, int TM>
-__global__ __launch_bounds__(256) void join_kernel(LossCall c) {
+__device__ __forceinline__ void join(const LossCall& c, const int id) {
   using Shape = TileShape<TN, TM>;
   const int piece = rows_of(c), m = USE == kHead ? c.head_rows : piece;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (c.width + Shape::kRowsB - 1) / Shape::kRowsB, tiles = tiles_m * tiles_n;
-  const int tile = (int)blockIdx.x / (TN * TM * 4), at_j = (int)blockIdx.x / (4 * TN) % TM, t = (int)blockIdx.x / 4 % TN, g = (int)blockIdx.x % 4;
+  const int tile = id / (TN * TM * 4), at_j = id / (4 * TN) % TM, t = id / 4 % TN, g = id % 4;
   if (tile >= tiles || (USE == kHead && piece == 0 && c.first > 0 && !c.last)) return;
   int tile_m, tile_n;
   tile_of(tile, tiles_m, tiles_n, tile_m, tile_n);
@@ -624,6 +629,39 @@ __global__ __launch_bounds__(256) void join_kernel(LossCall c) {
   }
 }
 
+template <bool BF16, int USE, int TN, int TM>
+__global__ __launch_bounds__(256) void join_kernel(LossCall c) {
+  join<BF16, USE, TN, TM>(c, (int)blockIdx.x);
+}
+
+// Both gradients of a small call in one launch: the first `groups` workgroups make dh, the others dW.
+template <bool BF16, int TN, int TM, int BUFFERS>
+__global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void both_kernel(LossCall dh, LossCall head, int groups) {
+  __shared__ __align__(1024) uint8_t lds[BUFFERS * TileShape<TN, TM>::kBuffer];
+  if ((int)blockIdx.x < groups)
+    tile<BF16, kStates, TN, TM, BUFFERS, kMaybe>(dh, (int)blockIdx.x, lds);
+  else
+    tile<BF16, kHead, TN, TM, BUFFERS, kMaybe>(head, (int)blockIdx.x - groups, lds);
+}
+template <bool BF16, int TN, int TM>
+__global__ __launch_bounds__(256) void join_both_kernel(LossCall dh, LossCall head, int groups) {
+  if ((int)blockIdx.x < groups)
+    join<BF16, kStates, TN, TM>(dh, (int)blockIdx.x);
+  else
+    join<BF16, kHead, TN, TM>(head, (int)blockIdx.x - groups);
+}
+template <bool BF16, int TN, int TM, int BUFFERS>
+void launch_both(const LossCall& c, const BothPlan& plan, hipStream_t s) {
+  const int tiles_dh = plan.dh.tiles_m * plan.dh.tiles_n, tiles_head = plan.dweight.tiles_m * plan.dweight.tiles_n;
+  LossCall dh = c, head = c;
+  dh.groups = plan.dh.splits > 1 ? tiles_dh * plan.dh.splits : 0, head.groups = plan.dweight.splits > 1 ? tiles_head * plan.dweight.splits : 0;
+  head.parts = c.parts + plan.dh.workspace / sizeof(floatx4);
+  const int groups = tiles_dh * plan.dh.splits;
+  both_kernel<BF16, TN, TM, BUFFERS><<<(unsigned)(groups + tiles_head * plan.dweight.splits), 256, 0, s>>>(dh, head, groups);
+  const int join_dh = dh.groups ? tiles_dh * TN * TM * 4 : 0, join_head = head.groups ? tiles_head * TN * TM * 4 : 0;
+  if (join_dh + join_head) join_both_kernel<BF16, TN, TM><<<(unsigned)(join_dh + join_head), 256, 0, s>>>(dh, head, join_dh);
+}
+
 // the same of logits: a workgroup to a tile, which takes the place of its first
 template <bool BF16, int TN, int TM>
 __global__ __launch_bounds__(256) void join_logits_kernel(LossCall c) {
@@ -660,7 +698,7 @@ void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
     if (plan.splits > 1) {
       LossCall shared = c;
       shared.groups = (int)tiles * plan.splits;
-      tile_kernel<BF16, USE, TN, TM, BUFFERS, true><<<tiles * (unsigned)plan.splits, 256, 0, s>>>(shared);
+      tile_kernel<BF16, USE, TN, TM, BUFFERS, kAlways><<<tiles * (unsigned)plan.splits, 256, 0, s>>>(shared);
       if constexpr (makes_logits(USE))
         join_logits_kernel<BF16, TN, TM><<<tiles, 256, 0, s>>>(shared);
       else
@@ -668,7 +706,7 @@ void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
       return;
     }
   }
-  tile_kernel<BF16, USE, TN, TM, BUFFERS, false><<<tiles, 256, 0, s>>>(c);
+  tile_kernel<BF16, USE, TN, TM, BUFFERS, kNever><<<tiles, 256, 0, s>>>(c);
 }
 template <bool BF16, int USE>
 void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
