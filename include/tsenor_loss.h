@@ -10,14 +10,16 @@
  * `stream`, nothing allocated, everything checked before the first launch, calls that overlap in time do not share a workspace, calls
  * can be captured in a HIP graph, sums have a fixed order and there are no atomics; counts may be zero, and pointers to arrays without
  * elements NULL).  Besides:
- *   - The logits of a call are never all kept.  They are made and used in tiles; a call that wants gradients keeps a number of the width
- *     of `dtype` for each logit of as many tokens as 2 GiB hold, and goes on to the next ones then.
+ *   - The logits of a call are never all kept.  They are made and used in tiles; a call that wants gradients keeps what becomes their
+ *     gradients, 2 bytes a logit (bf16) or 10 (fp32), for as many tokens as 2 GiB hold, and goes on to the next ones then (with a sum
+ *     of dweight in fp32 beside it, for bf16).
  *   - Loss and gradients are one call: nothing but a weight for each token comes between the loss and its gradients, and the product
  *     with the head is made once for both.
  *   - Logits, sums of exponentials and losses are in single precision, gradients are summed in single precision and rounded to `dtype`
  *     once.  Of bf16 matrices, the gradient of a logit is rounded to bf16 before it is multiplied: 2^-9 of itself, at random.
  *   - Tokens that are left out (no target, no entries) have loss, logarithm and gradients 0, whatever their hidden state is.
- *   - NaN and infinite logits make the loss of their token NaN, and with it the gradients it takes part in.
+ *   - NaN and infinite logits make the loss of their token NaN, and with it the gradients it takes part in; an infinite or NaN entry of the
+ *     head may do so to all tokens.
  */
 #ifndef TSENOR_LOSS_H
 #define TSENOR_LOSS_H

@@ -455,11 +455,8 @@ void launch_zero(void* out, int64_t count, bool bf16, hipStream_t s) {
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 constexpr int64_t kMaxTokens = (int64_t)1 << 24, kMaxVocab = (int64_t)1 << 21, kMaxWidth = (int64_t)1 << 16;
-constexpr int64_t kPieceBytes = (int64_t)1 << 31;  // of dz; a tenth of it for the sums of the tiles of a piece
 constexpr int64_t kMaxTileLd = (int64_t)1 << 21;   // (the tile kernels' offsets within a tile have 31 bits)
 constexpr double kLog2e = 1.4426950408889634;
-constexpr int64_t kWithoutPass = 20000000;          // logits (512 x 32000 x 4096, 16.4 million: 274.5 us with the pass, 279 without)
-constexpr int kPieceRows = 256;                    // pieces are a multiple of this
 
 int check(const tsenor_head& p) {
   if (p.tokens < 0 || p.tokens > kMaxTokens || p.vocab < 0 || p.vocab > kMaxVocab || p.width < 0 || p.width > kMaxWidth) return TSENOR_ERR_SHAPE;
@@ -493,95 +490,66 @@ int check(const tsenor_distill_problem* p) {
 
 inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-struct Plans {
-  ProductPlan logits, dh;
-  HeadPlan dweight;
-  BothPlan both;
-  bool few;  // logits by the kernel for few tokens
-};
-
 // describes a call to the kernels; the workspace begins at `workspace` (which may be NULL to ask for its size alone)
-size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, Plans& plans) {
+size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& plan) {
   const bool bf16 = p.dtype == TSENOR_BF16, gradients = p.dh_out || p.dweight_out;
-  const int64_t size = bf16 ? 2 : 4, planes = bf16 ? 1 : 3, line = 64;
+  const int64_t size = bf16 ? 2 : 4, planes = bf16 ? 1 : 3;
+  // (a row's last line goes on into the next row, but not into what lies between the rows of a wider matrix)
+  const bool in_place = bf16 && p.width && (p.width % 64 == 0 || (p.width % 8 == 0 && p.weight_ld == p.width)) && p.weight_ld % 8 == 0 &&
+                        p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
+  const bool states_too = p.width % 64 == 0 && p.h_ld % 8 == 0 && p.h_ld <= kMaxTileLd && aligned_to(p.h, 16);
+  plan = loss_plan({p.tokens, p.vocab, p.width, bf16, p.dh_out != nullptr, p.dweight_out != nullptr, c.k, c.teacher != nullptr, in_place, states_too});
   c.h = p.h, c.weight = p.weight, c.h_ld = p.h_ld, c.weight_ld = p.weight_ld;
   c.dloss = p.dloss, c.loss = p.loss_out, c.lse = p.lse_out, c.dh = p.dh_out, c.dweight = p.dweight_out;
-  c.tokens = (int)p.tokens, c.vocab = (int)p.vocab, c.width = (int)p.width;
-  c.states_ld = (int)std::max(round_up(p.width, line), line), c.dz_ld = (int)round_up(p.vocab, line);
-  const int64_t row_bytes = gradients ? c.dz_ld * (bf16 ? 2 : 10) : (p.vocab + 63) / 64 * 8 * 10;
-  const int64_t most = std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows);
-  const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
-  c.rows = (int)std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
-  plans.logits = product_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, c.states_ld / line * (bf16 ? 1 : kPairs), true);
-  if (p.dh_out) plans.dh = product_plan(std::min<int64_t>(c.rows, p.tokens), p.width, c.dz_ld / line * (bf16 ? 1 : kPairs), false);
-  if (p.dweight_out) plans.dweight = head_plan(p.vocab, p.width, (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs));
-  if (p.dh_out && p.dweight_out) {
-    const double apart = plans.dh.us + plans.dweight.parts[0].us + plans.dweight.parts[1].us + 4.0 * plans.dweight.count;
-    plans.both = both_plan(std::min<int64_t>(c.rows, p.tokens), p.vocab, p.width, c.dz_ld / line * (bf16 ? 1 : kPairs),
-                           (std::min<int64_t>(c.rows, p.tokens) + line - 1) / line * (bf16 ? 1 : kPairs), apart);
-  }
-  // (a row's last line goes on into the next row, but not into what lies between the rows of a wider matrix)
-  const bool whole = bf16 && p.width && (p.width % line == 0 || (p.width % 8 == 0 && p.weight_ld == p.width)) && p.weight_ld % 8 == 0 &&
-                     p.weight_ld <= kMaxTileLd && aligned_to(p.weight, 16);
-  // up to 16 tokens: straight from memory in fp32, where tiles would need a copy of the head that nothing else needs, or are few (us of the call:
-  // 3 x 1216 x 2326 27.4, 10.4 so, 4 x 1650 x 6912 with dh 58.3, 39.6; but 1 x 32000 x 2048 29.0, 33.6)
-  plans.few = p.tokens <= kFewTokens && (!bf16 || p.vocab < 64 * kCus || (!whole && !p.dh_out));
-  c.tile_n = plans.few ? kFewWords : plans.logits.kind == kLargeTile ? 128 : 64;
+  c.tokens = (int)p.tokens, c.vocab = (int)p.vocab, c.width = (int)p.width, c.rows = (int)plan.rows;
+  c.states_ld = (int)round_up(std::max<int64_t>(p.width, 1), 64), c.dz_ld = (int)round_up(p.vocab, 64);
+  c.tile_n = plan.few ? kFewWords : plan.logits.kind == kLargeTile ? 128 : 64;
   c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
   size_t at = 0;
-  const auto take = [&](int64_t bytes) {
+  const auto take = [&](size_t bytes) {
     char* const begin = workspace + at;
-    at += (size_t)round_up(bytes, 256);
+    at += (bytes + 255) / 256 * 256;
     return begin;
   };
-  // A tile has 64 rows at the least: up to there, rows of tokens that are left out cost nothing, and the states are read where they are.
-  if (!gradients && plans.few) {
-    c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
+  const size_t rows = (size_t)c.rows;
+  c.sums = reinterpret_cast<float2*>(take(rows * c.tiles * sizeof(float2)));
+  c.parts = reinterpret_cast<floatx4*>(take(std::max({plan.logits.workspace, plan.dh.workspace, plan.dweight.parts[0].workspace,
+                                                      plan.dweight.parts[1].workspace, plan.both.dh.workspace + plan.both.dweight.workspace})));
+  c.head = in_place || plan.direct || (plan.few && !p.dh_out) ? p.weight : take((size_t)p.vocab * c.states_ld * planes * 2);
+  c.head_ld = in_place ? p.weight_ld : c.states_ld * planes;
+  c.head_bytes = in_place ? (int)p.width * 2 : c.states_ld * 2;
+  if (plan.direct) {
+    c.states = const_cast<void*>(p.h), c.states_row = p.h_ld;
     return std::max<size_t>(at, 256);
   }
-  if (!gradients && whole && p.width % line == 0 && p.tokens <= 64 && p.h_ld * size % 16 == 0 && p.h_ld <= kMaxTileLd && aligned_to(p.h, 16)) {
-    c.states = const_cast<void*>(p.h), c.states_row = p.h_ld, c.head = p.weight, c.head_ld = p.weight_ld, c.head_bytes = (int)p.width * 2;
-    c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
-    c.parts = reinterpret_cast<floatx4*>(take((int64_t)plans.logits.workspace));
-    return std::max<size_t>(at, 256);
-  }
-  c.count = reinterpret_cast<int*>(take(12));
+  c.count = reinterpret_cast<int*>(take(sizeof(int) + 2 * sizeof(float)));
   c.largest_weight = reinterpret_cast<float*>(c.count + 1);
-  c.order = reinterpret_cast<int*>(take(p.tokens * 4));
-  c.counts = reinterpret_cast<uint8_t*>(c.teacher ? take(p.tokens) : nullptr);
+  c.order = reinterpret_cast<int*>(take((size_t)p.tokens * sizeof(int)));
+  c.counts = c.teacher ? reinterpret_cast<uint8_t*>(take((size_t)p.tokens)) : nullptr;
   c.states_row = c.states_ld * planes;
-  c.states = take((int64_t)round_up(c.rows, line) * c.states_ld * planes * 2);
-  c.sums = reinterpret_cast<float2*>(take((int64_t)c.rows * c.tiles * 8));
-  // Entries: the rows kernel reads their rows of the head at 4.3 TB/s, 16 (4) at a time of a token in 3 us; picked from the tiles they cost
-  // 2.5 us a round of tiles, and their order 3
-  const double read = std::max((double)c.rows * c.k * (double)p.width * (double)size / 4.3e6, 3.0 * (double)(c.k / (c.rows <= 2 * kCus ? 16 : 4)));
-  if (c.teacher && !plans.few && read > 5.0 + 2.5 * (plans.logits.tiles_m * (double)plans.logits.tiles_n / kCus)) {
-    c.dots = reinterpret_cast<float*>(take((int64_t)c.rows * c.k * 4));
-    c.sorted = reinterpret_cast<uint32_t*>(take((int64_t)c.rows * c.k * 4));
-    c.begins = reinterpret_cast<uint16_t*>(take((int64_t)c.rows * (c.tiles + 1) * 2));
+  c.states = take((size_t)round_up(c.rows, 64) * c.states_ld * planes * 2);
+  if (plan.picked) {
+    c.dots = reinterpret_cast<float*>(take(rows * c.k * sizeof(float)));
+    c.sorted = reinterpret_cast<uint32_t*>(take(rows * c.k * sizeof(uint32_t)));
+    c.begins = reinterpret_cast<uint16_t*>(take(rows * (c.tiles + 1) * sizeof(uint16_t)));
   }
-  // dh alone: without the pass that makes dz of the exponentials, where that costs more (4 bytes a logit at 4.8 TB/s) than what is in its place
-  if (bf16 && p.dh_out && !p.dweight_out && plans.logits.kind == kLargeTile && (int64_t)c.rows * p.vocab >= kWithoutPass) {
-    c.refs = reinterpret_cast<float*>(take((int64_t)c.rows * 4));
-    c.again = reinterpret_cast<int*>(take(4));
-    c.row_scale = reinterpret_cast<float2*>(take((int64_t)c.rows * 8));
+  if (plan.counted) {
+    c.refs = reinterpret_cast<float*>(take(rows * sizeof(float)));
+    c.again = reinterpret_cast<int*>(take(sizeof(int)));
+    c.row_scale = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
   }
-  c.dz = gradients ? take((int64_t)c.rows * c.dz_ld * planes * 2) : nullptr;
-  c.exps = gradients && !bf16 ? take((int64_t)c.rows * c.dz_ld * 4) : c.dz;
-  c.dweight_sum = bf16 && p.dweight_out && c.rows < p.tokens ? reinterpret_cast<float*>(take(p.vocab * p.width * 4)) : nullptr;
-  c.head = whole || (plans.few && !p.dh_out) ? p.weight : take(p.vocab * c.states_ld * planes * 2);
-  c.head_ld = whole ? p.weight_ld : c.states_ld * planes;
-  c.head_bytes = whole ? (int)p.width * 2 : c.states_ld * 2;
-  c.parts = reinterpret_cast<floatx4*>(take((int64_t)std::max({plans.logits.workspace, plans.dh.workspace, plans.dweight.parts[0].workspace, plans.dweight.parts[1].workspace, plans.both.dh.workspace + plans.both.dweight.workspace})));
-  return std::max<size_t>(at, 256);
+  c.dz = gradients ? take(rows * c.dz_ld * planes * 2) : nullptr;
+  c.exps = gradients && !bf16 ? take(rows * c.dz_ld * 4) : c.dz;
+  c.dweight_sum = bf16 && p.dweight_out && c.rows < p.tokens ? reinterpret_cast<float*>(take((size_t)p.vocab * p.width * sizeof(float))) : nullptr;
+  return at;
 }
 
 int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_bytes, hipStream_t s) {
   const bool bf16 = p.dtype == TSENOR_BF16;
-  Plans plans = {};
-  const size_t need = lay_out(p, nullptr, c, plans);
+  LossPlan plan;
+  const size_t need = lay_out(p, nullptr, c, plan);
   if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need) return TSENOR_ERR_WORKSPACE;
-  lay_out(p, static_cast<char*>(workspace), c, plans);
+  lay_out(p, static_cast<char*>(workspace), c, plan);
   if (p.vocab == 0 || p.tokens == 0 || c.k == 0) {
     launch_zero(p.loss_out, p.tokens, false, s);
     if (p.lse_out) launch_zero(p.lse_out, p.tokens, false, s);
@@ -589,10 +557,10 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     if (p.dweight_out) launch_zero(p.dweight_out, p.vocab * p.width, bf16, s);
     return status_of_launches();
   }
-  if (!c.count) {
+  if (plan.direct) {
     for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
       c.rows = std::min(c.rows, c.tokens - c.first);
-      plans.few ? launch_few_logits(c, bf16, s) : launch_logits(c, plans.logits, bf16, s);
+      plan.few ? launch_few_logits(c, bf16, s) : launch_logits(c, plan.logits, bf16, s);
       launch_rows(c, bf16, s);
     }
     return status_of_launches();
@@ -602,7 +570,7 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
   if (!alone) order_kernel<<<1, kOrderThreads, 0, s>>>(c);
   if (c.head != c.weight) {
     uint16_t* const head = static_cast<uint16_t*>(const_cast<void*>(c.head));
-    const int rows = std::max(1, std::min(kThreads / 8, kThreads * 8 / c.states_ld));  // (93469 x 76 30 -> XXX us)
+    const int rows = std::max(1, std::min(kThreads / 8, kThreads * 8 / c.states_ld));  // (93469 x 76: one to a workgroup 30 us, 16 together 6)
     const unsigned groups = (unsigned)((c.vocab + rows - 1) / rows);
     bf16 ? head_kernel<true><<<groups, kThreads, 0, s>>>(c, head, rows) : head_kernel<false><<<groups, kThreads, 0, s>>>(c, head, rows);
   }
@@ -614,18 +582,18 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
       bf16 ? gather_kernel<true, true><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false, true><<<padded, kThreads, 0, s>>>(piece);
     else
       bf16 ? gather_kernel<true, false><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false, false><<<padded, kThreads, 0, s>>>(piece);
-    plans.few ? launch_few_logits(piece, bf16, s) : launch_logits(piece, plans.logits, bf16, s);
+    plan.few ? launch_few_logits(piece, bf16, s) : launch_logits(piece, plan.logits, bf16, s);
     launch_rows(piece, bf16, s);
-    if (plans.both.use && c.width) {
+    if (plan.both.use && c.width) {
       piece.head_first = 0, piece.head_rows = c.vocab;
-      launch_both(piece, plans.both, bf16, s);
+      launch_both(piece, plan.both, bf16, s);
       continue;
     }
-    if (c.dh && c.width) launch_dh(piece, plans.dh, bf16, s);
+    if (c.dh && c.width) launch_dh(piece, plan.dh, bf16, s);
     if (c.dweight && c.width)
-      for (int k = 0; k < plans.dweight.count; ++k) {
-        piece.head_first = k ? (int)plans.dweight.rows[0] : 0, piece.head_rows = (int)plans.dweight.rows[k];
-        launch_dweight(piece, plans.dweight.parts[k], bf16, s);
+      for (int k = 0; k < plan.dweight.count; ++k) {
+        piece.head_first = k ? (int)plan.dweight.rows[0] : 0, piece.head_rows = (int)plan.dweight.rows[k];
+        launch_dweight(piece, plan.dweight.parts[k], bf16, s);
       }
   }
   return status_of_launches();
@@ -646,8 +614,8 @@ template <class Problem>
 size_t workspace_of(const Problem* p) {
   if (check(p) != TSENOR_OK) return 0;
   LossCall c = call_of(*p);
-  Plans plans = {};
-  return lay_out(p->head, nullptr, c, plans);
+  LossPlan plan;
+  return lay_out(p->head, nullptr, c, plan);
 }
 template <class Problem>
 int run(const Problem* p, void* workspace, size_t workspace_bytes, tsenor_stream_t stream) {

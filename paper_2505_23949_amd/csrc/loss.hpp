@@ -67,10 +67,7 @@ __device__ __forceinline__ int rows_of(const LossCall& c) { return c.count ? min
 // that one, and steps of 2^-39 of it below.
 constexpr float kExpBits = 15.0f;
 
-constexpr int kPairs = 6;  // of planes, that a product in single precision takes
-
 // logits of up to kFewTokens
-constexpr int kFewTokens = 16, kFewWords = 16;  // words of a workgroup, and of a part of a row then
 void launch_few_logits(const LossCall& c, bool bf16, hipStream_t s);
 void launch_logits(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
 void launch_dh(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);

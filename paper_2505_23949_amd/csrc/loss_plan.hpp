@@ -1,4 +1,5 @@
-// Which tiles the products of the losses are made in, and how many workgroups share the sum of a tile: host code that needs no GPU.
+// How a call of the losses is made: pieces, tiles of the products, workgroups that share the sum of a tile, and which way where there are
+// several: host code that needs no GPU.
 #pragma once
 #include <stddef.h>
 #include <stdint.h>
@@ -17,6 +18,16 @@ struct ProductPlan {
   size_t workspace;
 };
 
+// The kind of tiles, and how many workgroups share a tile's sum, that take least by measured us of a step (64 columns) and of what is around the
+// steps of a tile.  us of the kernels of tokens x vocab x width (bf16), no sum shared, by 64 x 128 / 128 x 128 / the same, two to a CU /
+// 256 x 128 / 256 x 256:
+//   logits  512 x 32000 x 4096  234 / 176 / 159 / 125 / 119      1433 x 50257 x 1024  305 / 224 / 181 / 185 / 172
+//           1024 x 8192 x 512    25 /  19 /  17 /  16 /  23      4096 x 32768 x 4096  1878 / 1287 / 1107 / 970 / 862
+//           128 x 16384 x 1024   10 /  12 /  15 /  17 /  27      4096 x 32000 x 256    308 / 217 / 151 / 164 / 142
+//   dh      300 x 5003 x 4096    32 /  38 /  50 /  54 /  91      4096 x 32768 x 4096  1730 / 1198 / 1112 / 882 / 798
+//   dW      300 x 5003 x 4096    50 /  33 /  25 /  30 /  31      1433 x 50257 x 1024   303 / 201 / 167 / 174 / 170
+// Shared sums: dh of 1433 x 50257 x 1024 in 32 tiles of 256 x 256 833, 8 workgroups to a tile 117-146 and 10 to add them; logits of 71 x 768 x
+// 6645 33, 7 to a tile 8 and 11 (logits in larger tiles have no CUs left to share with).
 // m rows of a, n of b, `blocks` of 64 columns of the sum; `logits`: they need whole sums, so that parts are joined by one workgroup to a tile
 inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool logits, Kind only = kNoColumns) {
   ProductPlan best = {kSmallTile, 0, 0, 1, 0.0, 0};
@@ -26,7 +37,7 @@ inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool logit
                         Cost{kLargeTile, 256, 256, 1.556, 9.0, kCus, false}}) {
     if (only != kNoColumns && c.kind != only) continue;
     const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n, tiles = tiles_m * tiles_n;
-    const int64_t most = logits ? (c.rows_m * c.rows_n <= 128 * 128 ? 16 : 1) : kMaxSplits;
+    const int64_t most = logits ? (c.kind == kSmallTile ? 16 : 1) : kMaxSplits;
     for (int64_t splits = 1; splits <= std::min<int64_t>(most, std::max<int64_t>(blocks / 4, 1)); ++splits) {
       if (splits > 1 && (splits - 1) * tiles >= c.at_once) break;
       const double steps = (double)((blocks + splits - 1) / splits) * c.step;
@@ -43,7 +54,7 @@ inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool logit
 }
 
 // The head's gradient: what does not fill a round of large or wide tiles can go to a launch of its own (us of the kernels, one launch and two:
-// 50257 x 1024 x 1433 175, XXX).
+// 1433 x 50257 x 1024 190-197, 162 + 17).
 struct HeadPlan {
   int count;
   int64_t rows[2];
@@ -79,6 +90,67 @@ inline BothPlan both_plan(int64_t tokens, int64_t vocab, int64_t width, int64_t 
     if (us < least) best = {true, a, b}, least = us;
   }
   return best;
+}
+
+// ---- a call ------------------------------------------------------------------------------------------------------------------
+constexpr int64_t kPieceBytes = (int64_t)1 << 31;  // of dz (and, without gradients, 10 times the sums of the parts of tiles)
+constexpr int kPieceRows = 256;                    // pieces are a multiple of this
+constexpr int kPairs = 6;                          // of planes, that a product in single precision takes
+constexpr int kFewTokens = 16, kFewWords = 16;     // of the kernel for few tokens: words of a workgroup
+constexpr int kTileTokens = 64;                    // of the smallest tile
+// Logits from which on dh alone is made without the pass that makes dz of the exponentials (4 bytes a logit at 4.8 TB/s): us of the call with the
+// pass and without 512 x 32000 x 4096 274.5, 279, 4096 x 128256 x 4096 6838, 6520.
+constexpr int64_t kWithoutPass = 20000000;
+
+struct LossShape {
+  int64_t tokens, vocab, width;
+  bool bf16, dh, dweight;
+  int k;            // entries of a token
+  bool teacher;     // whether they have a teacher's logits
+  bool in_place;    // whether products can read the head where it is
+  bool states_too;  // and the hidden states, in whole lines
+};
+struct LossPlan {
+  int64_t rows;  // of a piece
+  ProductPlan logits, dh;
+  HeadPlan dweight;
+  BothPlan both;
+  bool few;      // logits by the kernel for few tokens
+  bool direct;   // no gather: rows are the tokens in their order
+  bool counted;  // exponentials counted from a number for a row
+  bool picked;   // the logits of entries are picked from the tiles
+};
+
+inline LossPlan loss_plan(const LossShape& p) {
+  LossPlan plan = {};
+  const auto round_up = [](int64_t n, int64_t to) { return (n + to - 1) / to * to; };
+  const bool gradients = p.dh || p.dweight;
+  const int64_t row_bytes = gradients ? round_up(p.vocab, 64) * (p.bf16 ? 2 : 10) : (p.vocab + 63) / 64 * 8 * 10;
+  const int64_t most = std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows);
+  const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
+  plan.rows = std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
+
+  const int64_t tokens = std::min(plan.rows, p.tokens), pairs = p.bf16 ? 1 : kPairs;
+  const auto blocks = [&](int64_t n) { return (n + 63) / 64 * pairs; };
+  plan.logits = product_plan(tokens, p.vocab, blocks(std::max<int64_t>(p.width, 1)), true);
+  if (p.dh) plan.dh = product_plan(tokens, p.width, blocks(p.vocab), false);
+  if (p.dweight) plan.dweight = head_plan(p.vocab, p.width, blocks(tokens));
+  if (p.dh && p.dweight) {
+    const double apart = plan.dh.us + plan.dweight.parts[0].us + plan.dweight.parts[1].us + 4.0 * plan.dweight.count;
+    plan.both = both_plan(tokens, p.vocab, p.width, blocks(p.vocab), blocks(tokens), apart);
+  }
+  // Up to 16 tokens: straight from memory in fp32, where tiles would need a copy of the head that nothing else needs, or are few (us of the call:
+  // 3 x 1216 x 2326 27.4, 10.4 so, 4 x 1650 x 6912 with dh 58.3, 39.6; but 1 x 32000 x 2048 29.0, 33.6).
+  plan.few = p.tokens <= kFewTokens && (!p.bf16 || p.vocab < 64 * kCus || (!p.in_place && !p.dh));
+  // A tile has 64 rows at the least: up to there, rows of tokens that are left out cost nothing, and the states are read where they are (48 x
+  // 32000 x 4096 69 us, 57 so).
+  plan.direct = !gradients && (plan.few || (p.in_place && p.states_too && p.tokens <= kTileTokens));
+  // Entries: the rows kernel reads their rows of the head at 4.3 TB/s, 16 (4) at a time of a token in 3 us; picked from the tiles they cost
+  // 2.5 us a round of tiles, and their order 3 (512 x 32000 x 4096 with 32 entries 333 us, 275 so).
+  const double read = std::max((double)plan.rows * p.k * (double)p.width * (p.bf16 ? 2.0 : 4.0) / 4.3e6, 3.0 * (double)(p.k / (plan.rows <= 2 * kCus ? 16 : 4)));
+  plan.picked = p.teacher && !plan.few && !plan.direct && read > 5.0 + 2.5 * (plan.logits.tiles_m * (double)plan.logits.tiles_n / kCus);
+  plan.counted = p.bf16 && p.dh && !p.dweight && plan.logits.kind == kLargeTile && plan.rows * p.vocab >= kWithoutPass;
+  return plan;
 }
 
 }  // namespace tsenor_dev

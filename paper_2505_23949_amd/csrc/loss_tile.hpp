@@ -694,7 +694,7 @@ __global__ __launch_bounds__(256) void join_logits_kernel(LossCall c) {
 template <bool BF16, int USE, int TN, int TM, int BUFFERS>
 void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
   const unsigned tiles = (unsigned)(plan.tiles_m * plan.tiles_n);
-  if constexpr (!makes_logits(USE) || TN * TM <= 4) {
+  if constexpr (!makes_logits(USE) || TM == 1) {
     if (plan.splits > 1) {
       LossCall shared = c;
       shared.groups = (int)tiles * plan.splits;

@@ -1,7 +1,8 @@
-"""A layer with a transposable mask, found, run and retrained in 8-bit floating point: the mask finder and the layer operators as
-a program uses them together.
+"""A layer with a transposable mask, found, run and retrained in 8-bit floating point: the mask finder, the layer operators and the
+losses as a program uses them together.
 
     python -m paper_2505_23949_amd.masked_layer        # a layer learns to do what a dense one does
+    python -m paper_2505_23949_amd.masked_layer words  # a layer under a head of words learns what a dense one would answer
 
 ``MaskedLayer`` is residual addition, root-mean-square norm and a linear map whose weights carry an N:M mask that holds in the
 rows and in the columns of every block, so that its forward pass and its input gradient both read masked weights:
@@ -9,10 +10,13 @@ rows and in the columns of every block, so that its forward pass and its input g
     forward    h = x + residual;  y = norm(h) gain;  out = y (W . S)^T             norm and product in 8 bits
     backward   dy = dout (W . S);  dW = (dout^T y) . S;  dh, dgain from dy          products in 8 bits, operands along their sums
     step       all gradients scaled down to a largest norm, masters updated, weights into 8 bits again, both ways
+
+``Head`` is what a model of words ends in, a matrix with a row for each word, with the two losses that a pruned model is retrained by:
+cross entropy against the next word and divergence from a teacher's top words.  Neither keeps the logits.
 """
 from __future__ import annotations
 
-from . import binding, layer
+from . import binding, layer, loss
 
 
 def _scratch(size: int, device):
@@ -101,6 +105,51 @@ class MaskedLayer:
         self.refresh()
 
 
+class Head:
+    """A head of words, weight (vocab, width): bfloat16 or float32, like the hidden states.  ``trained``: it has a gradient too,
+    ``dweight``, which training passes write (they do not add to it)."""
+
+    def __init__(self, weight, *, trained: bool = False):
+        import torch
+
+        self.weight = weight
+        self.dweight = torch.empty_like(weight, memory_format=torch.contiguous_format) if trained else None
+
+    def cross_entropy(self, h, targets, *, training: bool = False):
+        """(losses, dh): the cross entropy of each token of h (tokens, width) against its target, 0 for targets outside the
+        vocabulary; dh is the gradient of the mean over those inside, of a training pass (None of others)."""
+        count = ((targets >= 0) & (targets < self.weight.shape[0])).sum()
+        return self._run("cross_entropy", h, (targets,), count, training)
+
+    def distill(self, h, ids, logits, *, temperature: float = 1.0, training: bool = False):
+        """(losses, dh): the divergence of each token from its teacher's top words, ``ids`` and ``logits`` (tokens, k), both sides'
+        logits divided by ``temperature``; dh as of ``cross_entropy``, times the square of the temperature, which keeps its size."""
+        import torch
+
+        counts = (ids >= 0) & (ids < self.weight.shape[0]) & (logits != -torch.inf)
+        return self._run("distill", h, (ids, logits), counts.any(1).sum(), training, temperature=temperature)
+
+    def _run(self, name, h, words, count, training, **more):
+        import torch
+
+        out = {"loss": torch.empty(h.shape[0], device=h.device)}
+        if training:
+            scale = more.get("temperature", 1.0) ** 2
+            out["dloss"] = (scale / count.clamp(min=1).float()).expand(h.shape[0]).contiguous()
+            out["dh"] = torch.empty_like(h, memory_format=torch.contiguous_format)
+            out["dweight"] = self.dweight
+        p = getattr(loss, f"make_{name}")(h, self.weight, *words, **out, **more)
+        getattr(loss, f"tsenor_{name}")(p, _scratch(getattr(loss, f"tsenor_{name}_workspace_bytes")(p), h.device))
+        return out["loss"], out.get("dh")
+
+    def gradients(self):
+        return [] if self.dweight is None else [self.dweight]
+
+    def update(self, rate: float) -> None:
+        if self.dweight is not None:
+            self.weight.add_(self.dweight, alpha=-rate)
+
+
 def clip_gradients(layers, max_norm: float):
     """The gradients of all layers scaled down, in place, to ``max_norm``; returns (norm, factor) on the GPU."""
     import torch
@@ -147,5 +196,44 @@ def main(tokens: int = 1024, rows: int = 768, cols: int = 512, steps: int = 30, 
     return losses
 
 
+def words(tokens: int = 1024, vocab: int = 8000, width: int = 512, steps: int = 30, rate: float = 0.5, k: int = 32,
+          temperature: float = 1.0) -> list[tuple[float, float]]:
+    """A masked 8:16 layer under a head that is kept learns to answer what the dense layer it was pruned from does: by the dense one's
+    top ``k`` words, and by its first one (inputs as of ``main``).  Returns (mean divergence, mean cross entropy) of each step."""
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(0)
+
+    def normal(*shape):
+        return torch.randn(*shape, device="cuda", generator=gen)
+
+    dense = normal(width, width) / width ** 0.5
+    mixture = normal(width // 4, width) / (width // 4) ** 0.5
+    head = Head((3.0 / width ** 0.5 * normal(vocab, width)).bfloat16())
+    one = MaskedLayer(dense.clone(), torch.ones(width, device="cuda"), 8, 16)
+    losses = []
+    for step in range(steps):
+        x = (normal(tokens, width // 4) @ mixture).bfloat16()
+        wide = x.float()
+        answers = (wide * torch.rsqrt(wide.square().mean(1, keepdim=True) + one.eps)) @ dense.t() + wide
+        top, ids = (answers @ head.weight.float().t()).topk(k)
+        targets = ids[:, 0].contiguous()
+        targets[:tokens // 8] = -100               # a prompt: its words are given, not learned
+        out, h = one.forward(x, training=True)
+        state = h + out
+        divergence, dstate = head.distill(state, ids, top, temperature=temperature, training=True)
+        entropy, more = head.cross_entropy(state, targets, training=True)
+        dstate = dstate + more
+        one.backward(dstate, dstate)
+        losses.append((float(divergence.mean()), float(entropy.sum() / (targets >= 0).sum())))
+        norm, factor = clip_gradients([one, head], 1.0).tolist()
+        one.update(rate)
+        if step % 5 == 0 or step == steps - 1:
+            print(f"step {step}: divergence {losses[-1][0]:.4f}, cross entropy {losses[-1][1]:.4f}, gradient norm {norm:.4f}", flush=True)
+    return losses
+
+
 if __name__ == "__main__":
-    main()
+    import sys
+
+    words() if sys.argv[1:] == ["words"] else main()
