@@ -6,8 +6,8 @@ using namespace tsenor_dev;
 // counted from c.refs, and the other way should that not do
 template <int COUNTED, int PLAIN>
 void launch_counted(const LossCall& c, unsigned tiles, hipStream_t s) {
-  tile_kernel<true, COUNTED, 4, 4, 2, false><<<tiles, 256, 0, s>>>(c);
-  logits_again_kernel<PLAIN><<<std::min<unsigned>(tiles, kCus), 256, 0, s>>>(c, (int)tiles);
+  tile_kernel<true, COUNTED, 4, 2, 4, 2, kNever><<<tiles, TileShape<4, 2, 4>::kThreads, 0, s>>>(c);
+  logits_again_kernel<PLAIN><<<std::min<unsigned>(tiles, kCus), TileShape<4, 2, 4>::kThreads, 0, s>>>(c, (int)tiles);
 }
 }  // namespace
 

@@ -37,11 +37,15 @@ constexpr bool is_in_place(int use) { return use == kLogitsInPlace || use == kLo
 // two such sums six are made, x1 y1, x1 y2, x2 y1, x2 y2, x1 y3 and x3 y1; the others are below 2^-25 of x y.  bf16 products run 16 times as
 // fast as those of fp32, so six of them take 0.4 of one in fp32.  Rows of the operands then hold three planes one behind the other, and the
 // sum goes over six pairs of planes, as if it were six times as long.
-template <int TN, int TM>
+// WM: rows of waves (there are two columns of them).  Four instead of two put two waves on a SIMD, of which one works while the other waits, for
+// half as much again of LDS reads.
+template <int TN, int TM, int WM>
 struct TileShape {
-  static constexpr int kRowsB = 64 * TN, kRowsA = 64 * TM;
-  static constexpr int kBuffer = (kRowsB + kRowsA) * 128;  // bytes of a block; b's rows first
-  static constexpr int kPieces = 2 * TN + 2 * TM;          // loads that a wave makes for a block
+  static constexpr int kWaves = 2 * WM, kThreads = kWaves * kWave;
+  static constexpr int kRowsB = 64 * TN, kRowsA = 32 * TM * WM;
+  static constexpr int kBuffer = (kRowsB + kRowsA) * 128;                                // bytes of a block; b's rows first
+  static constexpr int kPiecesB = kRowsB / 8 / kWaves, kPiecesA = kRowsA / 8 / kWaves;  // loads that a wave makes for a block
+  static constexpr int kPieces = kPiecesB + kPiecesA;
 };
 
 // Which planes of a and b block `block` of the sum takes, and which of their `per` blocks.  The five pairs whose products are small come first
@@ -65,28 +69,28 @@ struct Place {
   }
 };
 
-// Loads a wave's share of 64 T rows of an operand; `plane_bytes`: from plane to plane of a row.
+// Loads a wave's share of ROWS rows of an operand, PIECES times 8; `plane_bytes`: from plane to plane of a row.
 // PART: rows end inside a line: what follows them is read for its rest, and behind the last row something inside (the other operand has
 // zeros there).  A kernel of its own, because the choice costs each load a branch: 10 % of the product.
-// INTERLEAVED: row 32 t + r of each 32 T rows of LDS is row T r + t of memory, so that a lane gets T times as many neighbouring columns.
-template <int T, bool INTERLEAVED, bool PART>
+// T > 1: row 32 t + r of each 32 T rows of LDS is row T r + t of memory, so that a lane gets T times as many neighbouring columns.
+template <int ROWS, int PIECES, int T, bool PART>
 struct LoaderAlong {
   intx4 from;
   uint32_t to, past;  // past: offset of the last 16 bytes
-  int plane_bytes, whole, lane[2 * T];
+  int plane_bytes, whole, lane[PIECES];
   __device__ __forceinline__ LoaderAlong(const void* p, int64_t ld_bytes, int plane_bytes_, int row_bytes, int first, int rows, int lane_id, int wave,
                                          uint32_t lds) {
-    const int count = min(64 * T, rows - first);
+    const int count = min(ROWS, rows - first);
     past = (uint32_t)(count - 1) * (uint32_t)ld_bytes + row_bytes - 16;
     from = resource_of(static_cast<const char*>(p) + first * ld_bytes, (int64_t)past + 16);
 #pragma unroll
     for (int k = 0; k < 4; ++k) from[k] = __builtin_amdgcn_readfirstlane(from[k]);  // (the same in all lanes: it has to be in scalar registers)
-    to = lds + wave * 16 * T * 128;
+    to = lds + wave * PIECES * 1024;
     plane_bytes = plane_bytes_, whole = row_bytes / 128;
 #pragma unroll
-    for (int j = 0; j < 2 * T; ++j) {
-      const int at = wave * 16 * T + 8 * j + lane_id / 8;
-      const int row = INTERLEAVED ? at / (32 * T) * (32 * T) + at % 32 * T + at % (32 * T) / 32 : at;
+    for (int j = 0; j < PIECES; ++j) {
+      const int at = (wave * PIECES + j) * 8 + lane_id / 8;
+      const int row = at / (32 * T) * (32 * T) + at % 32 * T + at % (32 * T) / 32;
       lane[j] = (int)((uint32_t)min(row, count - 1) * (uint32_t)ld_bytes + (lane_id % 8 ^ at / 2 % 8) * 16);  // (32 bits, unsigned)
     }
   }
@@ -100,9 +104,10 @@ struct LoaderAlong {
 
 // `count` columns of the sum, `row_bytes` bytes of operand in each plane.  What lies past either end is read as something inside: past the
 // last column the other operand is zero, and past the last row nothing is written.
-template <int T>
+template <int ROWS, int WAVES>
 struct LoaderAcross {
-  static constexpr int kRowBytes = 128 * T, kAtOnce = 1024 / kRowBytes;
+  static constexpr int kRowBytes = 2 * ROWS, kAtOnce = 1024 / kRowBytes;
+  static_assert(WAVES * kAtOnce % 4 == 0 && kRowBytes >= 128);
   const char* base;
   int64_t ld_bytes, past;  // past: offset of the last 16 bytes of a plane
   uint32_t to;
@@ -112,21 +117,21 @@ struct LoaderAcross {
     to = lds + wave * 1024;
     const int k = wave * kAtOnce + lane_id * 16 / kRowBytes, at = lane_id * 16 % kRowBytes, swap = kRowBytes >= 256 ? k % 4 : k / 2 % 2;
     lane = k * (int)ld_bytes + min(first * 2 + (at ^ swap * 64), row_bytes - 16);
-    step = 4 * kAtOnce * (int)ld_bytes;
+    step = WAVES * kAtOnce * (int)ld_bytes;
   }
   __device__ __forceinline__ void load(int buffer, int j, int plane, int at) const {
     const int64_t begin = at * (64 * ld_bytes);
     const int limit = (int)min(past - begin, (int64_t)INT32_MAX - 16), offset = min(j * step, limit);
-    load_to_lds(to + buffer + j * 4096, min(lane, limit - offset), resource_of(base + begin + plane * plane_bytes, (int64_t)limit + 16), offset);
+    load_to_lds(to + buffer + j * WAVES * 1024, min(lane, limit - offset), resource_of(base + begin + plane * plane_bytes, (int64_t)limit + 16), offset);
   }
 };
 
 // Reads one of a wave's T tiles of 32 rows: half h of the sum's columns of a block.
-template <int T, bool ALONG>
+template <int T, int ROWS, bool ALONG>
 struct Reader {
-  static constexpr int kRowBytes = 128 * T;
+  static constexpr int kRowBytes = 2 * ROWS;
   int place[ALONG ? 2 : T];
-  __device__ __forceinline__ Reader(int lane, int wave) {  // wave: which half of the 64 T rows
+  __device__ __forceinline__ Reader(int lane, int wave) {  // wave: which 32 T of the ROWS rows
     const int r = lane % 32, q = lane / 32;
     if constexpr (ALONG) {
       place[0] = wave * 32 * T * 128 + r * 128 + ((2 * q) ^ (r / 2 % 8)) * 16;
@@ -210,8 +215,8 @@ __device__ __forceinline__ void add_gradient(const LossCall& c, int row, int64_t
 // How many workgroups share the sum of each of `tiles` tiles: more than planned where tokens that are left out leave fewer of them.
 __device__ __forceinline__ int splits_of(const LossCall& c, int tiles) { return min(c.groups / max(tiles, 1), kMaxSplits); }
 
-template <int TN, int TM, int BUFFERS>
-constexpr int kGroupsPerCu = BUFFERS * TileShape<TN, TM>::kBuffer <= 80 * 1024 ? 2 : 1;
+template <int TN, int TM, int WM, int BUFFERS>
+constexpr int kWavesPerSimd = BUFFERS * TileShape<TN, TM, WM>::kBuffer <= 80 * 1024 ? 2 : WM / 2;
 
 // Gradients leave a wave 32 rows at a time, through LDS, so that a store writes whole lines: the lanes hold a few columns of 32 rows each.
 // (1 x 116621 x 5083 in fp32, whose dW is 2.4 GB: 3584 -> 3397 us.  The exponentials, 32 to 64 bytes of a row to a lane, gain nothing by it.)
@@ -219,6 +224,9 @@ template <int TN, int SIZE>
 struct Staged {
   static constexpr int kRowBytes = 32 * TN * SIZE, kStride = kRowBytes + 16;
 };
+// bytes of LDS of a workgroup: its buffers, or 32 rows of fp32 results for each wave
+template <int TN, int TM, int WM, int BUFFERS>
+constexpr int kLds = std::max(BUFFERS * TileShape<TN, TM, WM>::kBuffer, TileShape<TN, TM, WM>::kWaves * 32 * Staged<TN, 4>::kStride);
 // row_at(row): where a row's columns go, NULL for none; `valid`: bytes of a row that there are
 template <int TN, int SIZE, class RowAt>
 __device__ __forceinline__ void store_staged(const uint8_t* staged, int valid, RowAt row_at) {
@@ -342,12 +350,11 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
 
 // SPLIT: several workgroups share the sum of a tile, and each leaves its part in c.parts.  kMaybe: where c.groups says so.
 enum Split { kNever, kAlways, kMaybe };
-template <bool BF16, int USE, int TN, int TM, int BUFFERS, int SPLIT>
+template <bool BF16, int USE, int TN, int TM, int WM, int BUFFERS, int SPLIT>
 __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* lds) {
-  using Shape = TileShape<TN, TM>;
+  using Shape = TileShape<TN, TM, WM>;
   constexpr int kPlanes = BF16 ? 1 : 3;
   constexpr bool kAlongB = makes_logits(USE), kAlongA = USE != kHead;
-  static_assert(4 * 32 * Staged<TN, 4>::kStride <= BUFFERS * Shape::kBuffer);
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int wave_n = wave % 2, wave_m = wave / 2, r = lane % 32, q = lane / 32;
   const int piece = __builtin_amdgcn_readfirstlane(rows_of(c));
@@ -379,29 +386,29 @@ __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* l
   const int states = c.states_ld * 2, dz = c.dz_ld * 2;  // bytes of a row of a plane (of the head: as of the states)
   const auto of_b = [&] {
     if constexpr (makes_logits(USE))
-      return LoaderAlong<TN, true, is_in_place(USE)>(c.head, c.head_ld * 2, states, c.head_bytes * kPlanes, n0, n, lane, wave, lds_at);
+      return LoaderAlong<Shape::kRowsB, Shape::kPiecesB, TN, is_in_place(USE)>(c.head, c.head_ld * 2, states, c.head_bytes * kPlanes, n0, n, lane, wave, lds_at);
     else if constexpr (USE == kStates)
-      return LoaderAcross<TN>(c.head, c.head_ld * 2, c.head_bytes, n0, c.vocab, lane, wave, lds_at);
+      return LoaderAcross<Shape::kRowsB, Shape::kWaves>(c.head, c.head_ld * 2, c.head_bytes, n0, c.vocab, lane, wave, lds_at);
     else
-      return LoaderAcross<TN>(c.states, (int64_t)states * kPlanes, states, n0, (piece + 63) / 64 * 64, lane, wave, lds_at);
+      return LoaderAcross<Shape::kRowsB, Shape::kWaves>(c.states, (int64_t)states * kPlanes, states, n0, (piece + 63) / 64 * 64, lane, wave, lds_at);
   }();
   const uint32_t lds_a = lds_at + Shape::kRowsB * 128;
   const auto of_a = [&] {
     if constexpr (makes_logits(USE))
-      return LoaderAlong<TM, false, false>(c.states, c.states_row * 2, states, states * kPlanes, m0, m, lane, wave, lds_a);
+      return LoaderAlong<Shape::kRowsA, Shape::kPiecesA, 1, false>(c.states, c.states_row * 2, states, states * kPlanes, m0, m, lane, wave, lds_a);
     else if constexpr (USE == kStates)
-      return LoaderAlong<TM, false, false>(c.dz, (int64_t)dz * kPlanes, dz, dz * kPlanes, m0, m, lane, wave, lds_a);
+      return LoaderAlong<Shape::kRowsA, Shape::kPiecesA, 1, false>(c.dz, (int64_t)dz * kPlanes, dz, dz * kPlanes, m0, m, lane, wave, lds_a);
     else
-      return LoaderAcross<TM>(c.dz, (int64_t)dz * kPlanes, dz, first_row + m0, piece, lane, wave, lds_a);
+      return LoaderAcross<Shape::kRowsA, Shape::kWaves>(c.dz, (int64_t)dz * kPlanes, dz, first_row + m0, piece, lane, wave, lds_a);
   }();
   const auto load = [&](int buffer, int k, const Place<BF16>& place) {
-    if (k < 2 * TN)
+    if (k < Shape::kPiecesB)
       of_b.load(buffer, k, place.plane_b, place.at);
     else
-      of_a.load(buffer, k - 2 * TN, place.plane_a, place.at);
+      of_a.load(buffer, k - Shape::kPiecesB, place.plane_a, place.at);
   };
-  const Reader<TN, kAlongB> read_b(lane, wave_n);
-  const Reader<TM, kAlongA> read_a(lane, wave_m);
+  const Reader<TN, Shape::kRowsB, kAlongB> read_b(lane, wave_n);
+  const Reader<TM, Shape::kRowsA, kAlongA> read_a(lane, wave_m);
   const uint8_t *const rows_b = lds, *const rows_a = lds + Shape::kRowsB * 128;
 
   // With more than two buffers the loads of a block are spread over the second half of a step and the first of the next.
@@ -418,7 +425,6 @@ __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* l
     for (int h = 0; h < 2; ++h) {
       b[0][h] = read_b.fetch(rows_b, 0, h), a[0][h] = read_a.fetch(rows_a, 0, h);
       if constexpr (TN == 4) b[1][h] = read_b.fetch(rows_b, 1, h);
-      if constexpr (TN == 2 && TM == 4) a[1][h] = read_a.fetch(rows_a, 1, h);
     }
   }
 
@@ -430,45 +436,31 @@ __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* l
   TSENOR_IN_ORDER();
 #define FETCH_B(buffer, t, h) b[t][h] = read_b.fetch(rows_b + buffer, t, h); TSENOR_IN_ORDER();
 #define FETCH_A(buffer, t, h) a[t][h] = read_a.fetch(rows_a + buffer, t, h); TSENOR_IN_ORDER();
-#define LOAD(k) if constexpr (k < kEarly) { load(buffer, k, ahead); TSENOR_IN_ORDER(); }
-#define LATE(k) if constexpr (k >= kEarly) { load(old_buffer, k, ahead_of_old); TSENOR_IN_ORDER(); }
+#define LOAD(k) if constexpr (k < kEarly && k < Shape::kPieces) { load(buffer, k, ahead); TSENOR_IN_ORDER(); }
+#define LATE(k) if constexpr (k >= kEarly && k < Shape::kPieces) { load(old_buffer, k, ahead_of_old); TSENOR_IN_ORDER(); }
   constexpr int kPending = (BUFFERS - 2) * Shape::kPieces;  // loads of the blocks after the next
   int buffer = 0, next_buffer = Shape::kBuffer, old_buffer = (BUFFERS - 1) * Shape::kBuffer;
   for (int block = first; block <= last; ++block) {
     const Place<BF16> ahead(min(block + BUFFERS, last), per), ahead_of_old(min(block + BUFFERS - 1, last), per);
     TSENOR_IN_ORDER();
-    if constexpr (TN == 4 && TM == 4) {
-      MULTIPLY(0, 0, 0) FETCH_A(buffer, 1, 0) MULTIPLY(1, 0, 0) FETCH_A(buffer, 1, 1) MULTIPLY(0, 0, 1) FETCH_A(buffer, 2, 0)
-      MULTIPLY(1, 0, 1) FETCH_A(buffer, 2, 1) MULTIPLY(0, 1, 0) FETCH_A(buffer, 3, 0) MULTIPLY(1, 1, 0) FETCH_A(buffer, 3, 1)
-      MULTIPLY(0, 1, 1) FETCH_B(buffer, 2, 0) MULTIPLY(1, 1, 1) FETCH_B(buffer, 2, 1) MULTIPLY(0, 2, 0) FETCH_B(buffer, 3, 0)
-      MULTIPLY(1, 2, 0) FETCH_B(buffer, 3, 1) MULTIPLY(0, 2, 1) MULTIPLY(1, 2, 1)
-      MULTIPLY(0, 3, 0) MULTIPLY(1, 3, 0) MULTIPLY(0, 3, 1) MULTIPLY(1, 3, 1)
+    if constexpr (TN == 4 && TM == 2) {
+      MULTIPLY(0, 0, 0) FETCH_A(buffer, 1, 0) MULTIPLY(1, 0, 0) FETCH_A(buffer, 1, 1) MULTIPLY(0, 0, 1) FETCH_B(buffer, 2, 0)
+      MULTIPLY(1, 0, 1) FETCH_B(buffer, 2, 1) MULTIPLY(0, 1, 0) FETCH_B(buffer, 3, 0) MULTIPLY(1, 1, 0) FETCH_B(buffer, 3, 1)
+      MULTIPLY(0, 1, 1) MULTIPLY(1, 1, 1)
       meet<kAnyPending>();
-      MULTIPLY(2, 2, 0) LOAD(0) MULTIPLY(3, 2, 0) LOAD(1) MULTIPLY(2, 2, 1) LOAD(2) MULTIPLY(3, 2, 1) LOAD(3)
-      MULTIPLY(2, 3, 0) LOAD(4) MULTIPLY(3, 3, 0) LOAD(5) MULTIPLY(2, 3, 1) LOAD(6) MULTIPLY(3, 3, 1) LOAD(7)
-      // only here the next block has to have come: a quarter of a step more for its loads, which two buffers leave little time
-      meet<8, false>();
-      MULTIPLY(2, 0, 0) FETCH_B(next_buffer, 0, 0) LOAD(8) MULTIPLY(3, 0, 0) FETCH_B(next_buffer, 1, 0) LOAD(9)
-      MULTIPLY(2, 0, 1) FETCH_B(next_buffer, 0, 1) LOAD(10) MULTIPLY(3, 0, 1) FETCH_B(next_buffer, 1, 1) LOAD(11)
-      MULTIPLY(2, 1, 0) FETCH_A(next_buffer, 0, 0) LOAD(12) MULTIPLY(3, 1, 0) FETCH_A(next_buffer, 0, 1) LOAD(13)
-      MULTIPLY(2, 1, 1) LOAD(14) MULTIPLY(3, 1, 1) LOAD(15)
-    } else if constexpr (TN == 2 && TM == 4) {
-      MULTIPLY(0, 0, 0) FETCH_B(buffer, 1, 0) MULTIPLY(0, 1, 0) FETCH_B(buffer, 1, 1) LATE(6) MULTIPLY(0, 0, 1) FETCH_A(buffer, 2, 0) LATE(7)
-      MULTIPLY(0, 1, 1) FETCH_A(buffer, 2, 1) LATE(8) MULTIPLY(1, 0, 0) FETCH_A(buffer, 3, 0) LATE(9) MULTIPLY(1, 1, 0) FETCH_A(buffer, 3, 1) LATE(10)
-      MULTIPLY(1, 0, 1) LATE(11) MULTIPLY(1, 1, 1)
-      meet<kPending>();
-      MULTIPLY(0, 2, 0) LOAD(0) FETCH_A(next_buffer, 0, 0) MULTIPLY(0, 3, 0) LOAD(1) MULTIPLY(0, 2, 1) LOAD(2) FETCH_A(next_buffer, 0, 1)
-      MULTIPLY(0, 3, 1) LOAD(3) MULTIPLY(1, 2, 0) LOAD(4) FETCH_B(next_buffer, 0, 0)
-      MULTIPLY(1, 3, 0) LOAD(5) FETCH_B(next_buffer, 0, 1) MULTIPLY(1, 2, 1) FETCH_A(next_buffer, 1, 0) MULTIPLY(1, 3, 1) FETCH_A(next_buffer, 1, 1)
+      MULTIPLY(2, 0, 0) LOAD(0) MULTIPLY(3, 0, 0) LOAD(1) MULTIPLY(2, 0, 1) LOAD(2) MULTIPLY(3, 0, 1) LOAD(3)
+      meet<4, false>();
+      MULTIPLY(2, 1, 0) FETCH_B(next_buffer, 0, 0) LOAD(4) MULTIPLY(3, 1, 0) FETCH_B(next_buffer, 0, 1) LOAD(5) FETCH_B(next_buffer, 1, 0)
+      MULTIPLY(2, 1, 1) FETCH_B(next_buffer, 1, 1) LOAD(6) FETCH_A(next_buffer, 0, 0) MULTIPLY(3, 1, 1) LOAD(7) FETCH_A(next_buffer, 0, 1)
     } else if constexpr (TN == 2 && TM == 2) {
-      MULTIPLY(0, 0, 0) FETCH_A(buffer, 1, 0) FETCH_A(buffer, 1, 1) LATE(4) MULTIPLY(0, 0, 1) FETCH_B(buffer, 1, 0) FETCH_B(buffer, 1, 1) LATE(5)
+      MULTIPLY(0, 0, 0) FETCH_A(buffer, 1, 0) FETCH_A(buffer, 1, 1) LATE(3) LATE(4) MULTIPLY(0, 0, 1) FETCH_B(buffer, 1, 0) FETCH_B(buffer, 1, 1) LATE(5)
       MULTIPLY(0, 1, 0) LATE(6) LATE(7) MULTIPLY(0, 1, 1)
       meet<kPending>();
       MULTIPLY(1, 0, 0) LOAD(0) LOAD(1) FETCH_B(next_buffer, 0, 0) MULTIPLY(1, 0, 1) LOAD(2) LOAD(3) FETCH_B(next_buffer, 0, 1)
       MULTIPLY(1, 1, 0) LOAD(4) LOAD(5) FETCH_A(next_buffer, 0, 0) MULTIPLY(1, 1, 1) LOAD(6) LOAD(7) FETCH_A(next_buffer, 0, 1)
     } else {
       static_assert(TN == 2 && TM == 1);
-      MULTIPLY(0, 0, 0) FETCH_B(buffer, 1, 0) FETCH_B(buffer, 1, 1) LATE(3) LATE(4) LATE(5) MULTIPLY(0, 0, 1)
+      MULTIPLY(0, 0, 0) FETCH_B(buffer, 1, 0) FETCH_B(buffer, 1, 1) LATE(2) LATE(3) LATE(4) LATE(5) MULTIPLY(0, 0, 1)
       meet<kPending>();
       MULTIPLY(1, 0, 0) LOAD(0) LOAD(1) FETCH_B(next_buffer, 0, 0) LOAD(2) FETCH_B(next_buffer, 0, 1) LOAD(3)
       MULTIPLY(1, 0, 1) LOAD(4) LOAD(5) FETCH_A(next_buffer, 0, 0) FETCH_A(next_buffer, 0, 1)
@@ -493,7 +485,7 @@ __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* l
         for (int t = 0; t < TN; ++t)
 #pragma unroll
           for (int g = 0; g < 4; ++g)
-            c.parts[((int64_t)id * (TM * TN * 4) + (j * TN + t) * 4 + g) * 256 + threadIdx.x] =
+            c.parts[((int64_t)id * (TM * TN * 4) + (j * TN + t) * 4 + g) * Shape::kThreads + threadIdx.x] =
                 floatx4{sum[t][j][4 * g], sum[t][j][4 * g + 1], sum[t][j][4 * g + 2], sum[t][j][4 * g + 3]};
       return;
     }
@@ -552,35 +544,35 @@ __device__ __forceinline__ void tile(const LossCall& c, const int id, uint8_t* l
   }
 }
 
-template <bool BF16, int USE, int TN, int TM, int BUFFERS, int SPLIT>
-__global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void tile_kernel(LossCall c) {
-  __shared__ __align__(1024) uint8_t lds[BUFFERS * TileShape<TN, TM>::kBuffer];
-  tile<BF16, USE, TN, TM, BUFFERS, SPLIT>(c, (int)blockIdx.x, lds);
+template <bool BF16, int USE, int TN, int TM, int WM, int BUFFERS, int SPLIT>
+__global__ __launch_bounds__((TileShape<TN, TM, WM>::kThreads), (kWavesPerSimd<TN, TM, WM, BUFFERS>)) void tile_kernel(LossCall c) {
+  __shared__ __align__(1024) uint8_t lds[kLds<TN, TM, WM, BUFFERS>];
+  tile<BF16, USE, TN, TM, WM, BUFFERS, SPLIT>(c, (int)blockIdx.x, lds);
 }
 
 // all of them once more, should that be needed, by as many workgroups as run at a time
 template <int USE>
-__global__ __launch_bounds__(256) void logits_again_kernel(LossCall c, int tiles) {
-  __shared__ __align__(1024) uint8_t lds[2 * TileShape<4, 4>::kBuffer];
+__global__ __launch_bounds__((TileShape<4, 2, 4>::kThreads)) void logits_again_kernel(LossCall c, int tiles) {
+  __shared__ __align__(1024) uint8_t lds[kLds<4, 2, 4, 2>];
   if (!*c.again) return;
   for (int id = (int)blockIdx.x; id < tiles; id += (int)gridDim.x) {
-    tile<true, USE, 4, 4, 2, kNever>(c, id, lds);
+    tile<true, USE, 4, 2, 4, 2, kNever>(c, id, lds);
     __syncthreads();
   }
 }
 
 // adds the parts of a tile in their order: a workgroup for each tile and 4 TN TM-th of it
-template <bool BF16, int USE, int TN, int TM>
+template <bool BF16, int USE, int TN, int TM, int WM>
 __device__ __forceinline__ void join(const LossCall& c, const int id) {
-  using Shape = TileShape<TN, TM>;
+  using Shape = TileShape<TN, TM, WM>;
   const int piece = rows_of(c), m = USE == kHead ? c.head_rows : piece;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (c.width + Shape::kRowsB - 1) / Shape::kRowsB, tiles = tiles_m * tiles_n;
   const int tile = id / (TN * TM * 4), at_j = id / (4 * TN) % TM, t = id / 4 % TN, g = id % 4;
   if (tile >= tiles || (USE == kHead && piece == 0 && c.first > 0 && !c.last)) return;
   int tile_m, tile_n;
   tile_of(tile, tiles_m, tiles_n, tile_m, tile_n);
-  const floatx4* part = c.parts + ((int64_t)tile * (TM * TN * 4) + (at_j * TN + t) * 4 + g) * 256 + threadIdx.x;
-  const int64_t step = (int64_t)tiles * (TM * TN * 4) * 256;
+  const floatx4* part = c.parts + ((int64_t)tile * (TM * TN * 4) + (at_j * TN + t) * 4 + g) * Shape::kThreads + threadIdx.x;
+  const int64_t step = (int64_t)tiles * (TM * TN * 4) * Shape::kThreads;
   const int splits = splits_of(c, tiles);
   floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
   int k = 0;
@@ -629,56 +621,56 @@ __device__ __forceinline__ void join(const LossCall& c, const int id) {
   }
 }
 
-template <bool BF16, int USE, int TN, int TM>
-__global__ __launch_bounds__(256) void join_kernel(LossCall c) {
-  join<BF16, USE, TN, TM>(c, (int)blockIdx.x);
+template <bool BF16, int USE, int TN, int TM, int WM>
+__global__ __launch_bounds__((TileShape<TN, TM, WM>::kThreads)) void join_kernel(LossCall c) {
+  join<BF16, USE, TN, TM, WM>(c, (int)blockIdx.x);
 }
 
 // Both gradients of a small call in one launch: the first `groups` workgroups make dh, the others dW.
-template <bool BF16, int TN, int TM, int BUFFERS>
-__global__ __launch_bounds__(256, (kGroupsPerCu<TN, TM, BUFFERS>)) void both_kernel(LossCall dh, LossCall head, int groups) {
-  __shared__ __align__(1024) uint8_t lds[BUFFERS * TileShape<TN, TM>::kBuffer];
+template <bool BF16, int TN, int TM, int WM, int BUFFERS>
+__global__ __launch_bounds__((TileShape<TN, TM, WM>::kThreads), (kWavesPerSimd<TN, TM, WM, BUFFERS>)) void both_kernel(LossCall dh, LossCall head, int groups) {
+  __shared__ __align__(1024) uint8_t lds[kLds<TN, TM, WM, BUFFERS>];
   if ((int)blockIdx.x < groups)
-    tile<BF16, kStates, TN, TM, BUFFERS, kMaybe>(dh, (int)blockIdx.x, lds);
+    tile<BF16, kStates, TN, TM, WM, BUFFERS, kMaybe>(dh, (int)blockIdx.x, lds);
   else
-    tile<BF16, kHead, TN, TM, BUFFERS, kMaybe>(head, (int)blockIdx.x - groups, lds);
+    tile<BF16, kHead, TN, TM, WM, BUFFERS, kMaybe>(head, (int)blockIdx.x - groups, lds);
 }
-template <bool BF16, int TN, int TM>
-__global__ __launch_bounds__(256) void join_both_kernel(LossCall dh, LossCall head, int groups) {
+template <bool BF16, int TN, int TM, int WM>
+__global__ __launch_bounds__((TileShape<TN, TM, WM>::kThreads)) void join_both_kernel(LossCall dh, LossCall head, int groups) {
   if ((int)blockIdx.x < groups)
-    join<BF16, kStates, TN, TM>(dh, (int)blockIdx.x);
+    join<BF16, kStates, TN, TM, WM>(dh, (int)blockIdx.x);
   else
-    join<BF16, kHead, TN, TM>(head, (int)blockIdx.x - groups);
+    join<BF16, kHead, TN, TM, WM>(head, (int)blockIdx.x - groups);
 }
-template <bool BF16, int TN, int TM, int BUFFERS>
+template <bool BF16, int TN, int TM, int WM, int BUFFERS>
 void launch_both(const LossCall& c, const BothPlan& plan, hipStream_t s) {
   const int tiles_dh = plan.dh.tiles_m * plan.dh.tiles_n, tiles_head = plan.dweight.tiles_m * plan.dweight.tiles_n;
   LossCall dh = c, head = c;
   dh.groups = plan.dh.splits > 1 ? tiles_dh * plan.dh.splits : 0, head.groups = plan.dweight.splits > 1 ? tiles_head * plan.dweight.splits : 0;
   head.parts = c.parts + plan.dh.workspace / sizeof(floatx4);
   const int groups = tiles_dh * plan.dh.splits;
-  both_kernel<BF16, TN, TM, BUFFERS><<<(unsigned)(groups + tiles_head * plan.dweight.splits), 256, 0, s>>>(dh, head, groups);
+  both_kernel<BF16, TN, TM, WM, BUFFERS><<<(unsigned)(groups + tiles_head * plan.dweight.splits), TileShape<TN, TM, WM>::kThreads, 0, s>>>(dh, head, groups);
   const int join_dh = dh.groups ? tiles_dh * TN * TM * 4 : 0, join_head = head.groups ? tiles_head * TN * TM * 4 : 0;
-  if (join_dh + join_head) join_both_kernel<BF16, TN, TM><<<(unsigned)(join_dh + join_head), 256, 0, s>>>(dh, head, join_dh);
+  if (join_dh + join_head) join_both_kernel<BF16, TN, TM, WM><<<(unsigned)(join_dh + join_head), TileShape<TN, TM, WM>::kThreads, 0, s>>>(dh, head, join_dh);
 }
 
 // the same of logits: a workgroup to a tile, which takes the place of its first
-template <bool BF16, int TN, int TM>
-__global__ __launch_bounds__(256) void join_logits_kernel(LossCall c) {
-  using Shape = TileShape<TN, TM>;
-  __shared__ __align__(16) uint8_t lds[4 * 32 * Staged<TN, 4>::kStride];
+template <bool BF16, int TN, int TM, int WM>
+__global__ __launch_bounds__((TileShape<TN, TM, WM>::kThreads)) void join_logits_kernel(LossCall c) {
+  using Shape = TileShape<TN, TM, WM>;
+  __shared__ __align__(16) uint8_t lds[TileShape<TN, TM, WM>::kWaves * 32 * Staged<TN, 4>::kStride];
   const int m = rows_of(c), n = c.vocab;
   const int tiles_m = (m + Shape::kRowsA - 1) / Shape::kRowsA, tiles_n = (n + Shape::kRowsB - 1) / Shape::kRowsB, tiles = tiles_m * tiles_n;
   if ((int)blockIdx.x >= tiles) return;
   int tile_m, tile_n;
   tile_of((int)blockIdx.x, tiles_m, tiles_n, tile_m, tile_n);
-  const floatx4* const part = c.parts + (int64_t)blockIdx.x * (TM * TN * 4) * 256 + threadIdx.x;
-  const int64_t step = (int64_t)tiles * (TM * TN * 4) * 256;
+  const floatx4* const part = c.parts + (int64_t)blockIdx.x * (TM * TN * 4) * Shape::kThreads + threadIdx.x;
+  const int64_t step = (int64_t)tiles * (TM * TN * 4) * Shape::kThreads;
   floatx4 v[TM * TN * 4] = {};
   const int splits = splits_of(c, tiles);
   for (int k = 0; k < splits; ++k) {
 #pragma unroll
-    for (int at = 0; at < TM * TN * 4; ++at) v[at] += part[k * step + at * 256];
+    for (int at = 0; at < TM * TN * 4; ++at) v[at] += part[k * step + at * Shape::kThreads];
   }
   floatx16 sum[TN][TM];
 #pragma unroll
@@ -691,31 +683,31 @@ __global__ __launch_bounds__(256) void join_logits_kernel(LossCall c) {
 }
 
 // the kernel with the tiles of a plan
-template <bool BF16, int USE, int TN, int TM, int BUFFERS>
+template <bool BF16, int USE, int TN, int TM, int WM, int BUFFERS>
 void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
   const unsigned tiles = (unsigned)(plan.tiles_m * plan.tiles_n);
-  if constexpr (!makes_logits(USE) || TM == 1) {
+  if constexpr (!makes_logits(USE) || (TM == 1 && WM == 2)) {
     if (plan.splits > 1) {
       LossCall shared = c;
       shared.groups = (int)tiles * plan.splits;
-      tile_kernel<BF16, USE, TN, TM, BUFFERS, kAlways><<<tiles * (unsigned)plan.splits, 256, 0, s>>>(shared);
+      tile_kernel<BF16, USE, TN, TM, WM, BUFFERS, kAlways><<<tiles * (unsigned)plan.splits, TileShape<TN, TM, WM>::kThreads, 0, s>>>(shared);
       if constexpr (makes_logits(USE))
-        join_logits_kernel<BF16, TN, TM><<<tiles, 256, 0, s>>>(shared);
+        join_logits_kernel<BF16, TN, TM, WM><<<tiles, TileShape<TN, TM, WM>::kThreads, 0, s>>>(shared);
       else
-        join_kernel<BF16, USE, TN, TM><<<tiles * TN * TM * 4, 256, 0, s>>>(shared);
+        join_kernel<BF16, USE, TN, TM, WM><<<tiles * TN * TM * 4, TileShape<TN, TM, WM>::kThreads, 0, s>>>(shared);
       return;
     }
   }
-  tile_kernel<BF16, USE, TN, TM, BUFFERS, kNever><<<tiles, 256, 0, s>>>(c);
+  tile_kernel<BF16, USE, TN, TM, WM, BUFFERS, kNever><<<tiles, TileShape<TN, TM, WM>::kThreads, 0, s>>>(c);
 }
 template <bool BF16, int USE>
 void launch_tiles(const LossCall& c, const ProductPlan& plan, hipStream_t s) {
   switch (plan.kind) {
-    case kLargeTile: launch_tiles<BF16, USE, 4, 4, 2>(c, plan, s); break;
-    case kWideTile: launch_tiles<BF16, USE, 2, 4, 3>(c, plan, s); break;
-    case kTile: launch_tiles<BF16, USE, 2, 2, 4>(c, plan, s); break;
-    case kTilePairs: launch_tiles<BF16, USE, 2, 2, 2>(c, plan, s); break;
-    default: launch_tiles<BF16, USE, 2, 1, 6>(c, plan, s); break;
+    case kLargeTile: launch_tiles<BF16, USE, 4, 2, 4, 2>(c, plan, s); break;
+    case kWideTile: launch_tiles<BF16, USE, 2, 2, 4, 3>(c, plan, s); break;
+    case kTile: launch_tiles<BF16, USE, 2, 1, 4, 4>(c, plan, s); break;
+    case kTilePairs: launch_tiles<BF16, USE, 2, 2, 2, 2>(c, plan, s); break;
+    default: launch_tiles<BF16, USE, 2, 1, 2, 6>(c, plan, s); break;
   }
 }
 
