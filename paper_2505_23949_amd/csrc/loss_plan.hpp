@@ -21,20 +21,20 @@ struct ProductPlan {
 // The kind of tiles, and how many workgroups share a tile's sum, that take least by measured us of a step (64 columns) and of what is around the
 // steps of a tile.  us of the kernels of tokens x vocab x width (bf16), no sum shared, by 64 x 128 / 128 x 128 / the same, two to a CU /
 // 256 x 128 / 256 x 256:
-//   logits  512 x 32000 x 4096  234 / 176 / 159 / 125 / 119      1433 x 50257 x 1024  305 / 224 / 181 / 185 / 172
-//           1024 x 8192 x 512    25 /  19 /  17 /  16 /  23      4096 x 32768 x 4096  1878 / 1287 / 1107 / 970 / 862
-//           128 x 16384 x 1024   10 /  12 /  15 /  17 /  27      4096 x 32000 x 256    308 / 217 / 151 / 164 / 142
-//   dh      300 x 5003 x 4096    32 /  38 /  50 /  54 /  91      4096 x 32768 x 4096  1730 / 1198 / 1112 / 882 / 798
-//   dW      300 x 5003 x 4096    50 /  33 /  25 /  30 /  31      1433 x 50257 x 1024   303 / 201 / 167 / 174 / 170
-// Shared sums: dh of 1433 x 50257 x 1024 in 32 tiles of 256 x 256 833, 8 workgroups to a tile 117-146 and 10 to add them; logits of 71 x 768 x
-// 6645 33, 7 to a tile 8 and 11 (logits in larger tiles have no CUs left to share with).
+//   logits  512 x 32000 x 4096  240 / 177 / 162 / 129 / 120      1433 x 50257 x 1024  302 / 212 / 184 / 183 / 166
+//           1024 x 8192 x 512    25 /  20 /  18 /  16 /  23      4096 x 32768 x 4096  1867 / 1276 / 1103 / 988 / 856
+//           128 x 16384 x 1024   11 /  11 /  16 /  16 /  28      4096 x 32000 x 256    298 / 201 / 151 / 161 / 132
+//   dh      300 x 5003 x 4096    32 /  36 /  51 /  50 /  86      4096 x 32768 x 4096  1726 / 1204 / 1118 / 909 / 813
+//   dW      300 x 5003 x 4096    50 /  30 /  25 /  26 /  27      1433 x 50257 x 1024   315 / 204 / 169 / 169 / 157
+// Shared sums, and what adds them: dh of 1433 x 50257 x 1024 with 256 x 256 787 alone, 2 workgroups to a tile 393 + 6, 4 207 + 8, 8 139 + 12;
+// logits of 71 x 768 x 6645 with 64 x 128 33 alone, 7 to a tile 8 + 11 (logits in larger tiles have no CUs left to share with).
 // m rows of a, n of b, `blocks` of 64 columns of the sum; `logits`: they need whole sums, so that parts are joined by one workgroup to a tile
 inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool logits, Kind only = kNoColumns) {
   ProductPlan best = {kSmallTile, 0, 0, 1, 0.0, 0};
   if (m == 0 || n == 0) return best;
   for (const Cost& c : {Cost{kSmallTile, 64, 128, 0.42, 3.0, kCus, false}, Cost{kTile, 128, 128, 0.585, 4.0, kCus, false},
-                        Cost{kTilePairs, 128, 128, 1.085, 4.5, 2 * kCus, true}, Cost{kWideTile, 256, 128, 0.86, 6.0, kCus, false},
-                        Cost{kLargeTile, 256, 256, 1.556, 9.0, kCus, false}}) {
+                        Cost{kTilePairs, 128, 128, 1.085, 4.5, 2 * kCus, true}, Cost{kWideTile, 256, 128, 0.88, 5.5, kCus, false},
+                        Cost{kLargeTile, 256, 256, 1.556, 8.0, kCus, false}}) {
     if (only != kNoColumns && c.kind != only) continue;
     const int64_t tiles_m = (m + c.rows_m - 1) / c.rows_m, tiles_n = (n + c.rows_n - 1) / c.rows_n, tiles = tiles_m * tiles_n;
     const int64_t most = logits ? (c.kind == kSmallTile ? 16 : 1) : kMaxSplits;
@@ -46,7 +46,7 @@ inline ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool logit
       const double fill = c.fluid ? (rest <= kCus ? 0.7 : 1.0) : 0.75 + 0.25 * (double)rest / c.at_once;
       double us = (double)rounds * (steps + c.around) + (rest ? steps * fill + c.around : 0.0);
       const double parts = splits > 1 ? (double)groups * c.rows_m * c.rows_n * 4.0 : 0.0;
-      if (splits > 1) us += 4.0 + 2.0 * parts / 5.0e6 + (logits ? 0.5 : 0.1) * (double)splits;
+      if (splits > 1) us += 4.0 + parts / 4.0e6 + (logits ? 0.5 : 0.1) * (double)splits;  // (written and added up)
       if (best.us == 0.0 || us < best.us) best = {c.kind, (int)tiles_m, (int)tiles_n, (int)splits, us, (size_t)parts};
     }
   }
@@ -64,9 +64,10 @@ inline HeadPlan head_plan(int64_t m, int64_t n, int64_t blocks) {
   const ProductPlan whole = product_plan(m, n, blocks, false);
   HeadPlan best = {1, {m, 0}, {whole, {}}};
   double least = whole.us;
-  for (int rows_n : {128, 256}) {
-    const int64_t tiles_m = (m + 255) / 256, tiles_n = (n + rows_n - 1) / rows_n, rounds = tiles_m * tiles_n / kCus;
-    const int64_t m1 = tiles_n ? rounds * kCus / tiles_n * 256 : 0;
+  for (int kind = 0; kind < 3; ++kind) {  // by tiles of 256 x 256, 256 x 128 and 128 x 128
+    const int rows_m = kind == 2 ? 128 : 256, rows_n = kind == 0 ? 256 : 128;
+    const int64_t tiles_m = (m + rows_m - 1) / rows_m, tiles_n = (n + rows_n - 1) / rows_n, rounds = tiles_m * tiles_n / kCus;
+    const int64_t m1 = tiles_n ? rounds * kCus / tiles_n * rows_m : 0;
     if (m1 <= 0 || m1 >= m) continue;
     const ProductPlan first = product_plan(m1, n, blocks, false), rest = product_plan(m - m1, n, blocks, false);
     if (first.us + rest.us + 4.0 < least) best = {2, {m1, m - m1}, {first, rest}}, least = first.us + rest.us + 4.0;

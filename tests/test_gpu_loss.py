@@ -156,7 +156,8 @@ LARGER = [(137, 34211, 64, 0, 0), (66, 17572, 64, 1, 1), (18, 34795, 64, 0, 0), 
           (2794, 3762, 136, 1, 0), (162, 6137, 5384, 1, 0), (16, 1220, 64, 1, 0), (17, 33043, 144, 1, 1), (16, 17269, 144, 1, 1), (2178, 277, 1840, 1, 1),
           (579, 1819, 1272, 1, 1), (265, 37543, 64, 1, 1), (7147, 654, 5384, 0, 1), (6797, 336, 5408, 0, 1), (4718, 130, 800, 0, 1), (3831, 467, 1344, 0, 1),
           (6635, 136, 5384, 0, 1), (19, 52402, 1192, 1, 1), (67, 35502, 1968, 0, 1), (1376, 32990, 144, 1, 1), (4005, 2790, 3000, 0, 1),
-          (18, 1083, 1888, 1, 1)]
+          (18, 1083, 1888, 1, 1), (1, 129, 64, 0, 1), (1, 18232, 64, 0, 1), (65, 39796, 944, 0, 1), (1632, 33074, 144, 0, 1), (403, 8072, 5424, 1, 0),
+          (144, 38235, 64, 1, 1), (3021, 7272, 1168, 0, 1)]
 PICKED = [(512, 2000, 1024, "bf16", 64, 0.0), (700, 1031, 960, "bf16", 130, 0.2), (300, 1500, 1000, "f32", 100, 0.1), (2100, 4099, 512, "bf16", 256, 0.0)]
 
 
