@@ -570,7 +570,7 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
   if (!alone) order_kernel<<<1, kOrderThreads, 0, s>>>(c);
   if (c.head != c.weight) {
     uint16_t* const head = static_cast<uint16_t*>(const_cast<void*>(c.head));
-    const int rows = std::max(1, std::min(kThreads / 8, kThreads * 8 / c.states_ld));  // (93469 x 76: one to a workgroup 30 us, 16 together 6)
+    const int rows = std::max(1, std::min(kThreads / 8, kThreads * 8 / c.states_ld));  // (93469 x 76: one to a workgroup 30 us, 16 together 11)
     const unsigned groups = (unsigned)((c.vocab + rows - 1) / rows);
     bf16 ? head_kernel<true><<<groups, kThreads, 0, s>>>(c, head, rows) : head_kernel<false><<<groups, kThreads, 0, s>>>(c, head, rows);
   }

@@ -5,7 +5,7 @@
 // so that it ends up with four neighbouring words of a token.  Single precision takes the fp32 instruction: 16 rows are too few for its
 // rate to matter (8 operations a byte).
 // Against tiles of 64 x 128, which need operands in whole lines, and where few of them fill the GPU (us of the kernel): 2 x 534 x 6848
-// 30.6, 7.5 so.
+// 31, 12 so.
 #include "loss.hpp"
 
 namespace {

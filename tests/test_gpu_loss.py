@@ -471,3 +471,25 @@ def test_pieces(loss):
         want = sum(p["dweight"].float() for p in parts)
         assert (whole["dweight"].float() - want).norm() <= 2 * off * want.norm()
         assert whole["dweight"].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,vocab,width,k", [(40, 300, 64, 0), (40, 300, 64, 9), (1400, 515, 136, 0), (10, 129, 72, 3), (300, 70000, 64, 2)])
+def test_weights_and_teachers_that_are_no_numbers(loss, tokens, vocab, width, k, dtype):
+    """An infinite or NaN weight, or a teacher's NaN, is its own token's: losses and dh of the others are what they are without it."""
+    case = Case(tokens, vocab, width, dtype, k=k)
+    case.dloss[2], case.dloss[4] = 0.0, 0.0
+    case.reference("cuda")
+    case.dloss[2], case.dloss[4] = math.inf, math.nan
+    if k:
+        case.logits[6, 1] = math.nan
+    out = case.run(loss, dweight=False).out
+    got = {name: v.double().cpu() for name, v in out.items()}
+    assert not got["dh"][[2, 4]].isfinite().any()
+    rest = torch.ones(tokens, dtype=torch.bool)
+    if k:
+        rest[6] = False
+        assert got["loss"][6].isnan() and got["dh"][6].isnan().all()
+    assert ((got["loss"] - case.want["loss"]).abs() <= case.off["loss"])[rest].all()  # (a weight does not touch the loss)
+    rest[[2, 4]] = False
+    assert ((got["dh"] - case.want["dh"]).abs() <= case.off["dh"])[rest].all()
