@@ -514,8 +514,9 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& pla
   const size_t rows = (size_t)c.rows;
   c.sums = reinterpret_cast<float2*>(take(rows * c.tiles * sizeof(float2)));
   c.parts = reinterpret_cast<floatx4*>(take(std::max({plan.logits.workspace, plan.dh.workspace, plan.dweight.parts[0].workspace,
-                                                      plan.dweight.parts[1].workspace, plan.both.dh.workspace + plan.both.dweight.workspace})));
-  c.head = in_place || plan.direct || (plan.few && !p.dh_out) ? p.weight : take((size_t)p.vocab * c.states_ld * planes * 2);
+                                                      plan.dweight.parts[1].workspace, plan.both.dh.workspace + plan.both.dweight.workspace,
+                                                      plan.dh_of_few.workspace})));
+  c.head = in_place || plan.direct || (plan.few && (!p.dh_out || plan.few_dh)) ? p.weight : take((size_t)p.vocab * c.states_ld * planes * 2);
   c.head_ld = in_place ? p.weight_ld : c.states_ld * planes;
   c.head_bytes = in_place ? (int)p.width * 2 : c.states_ld * 2;
   if (plan.direct) {
@@ -589,7 +590,7 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
       launch_both(piece, plan.both, bf16, s);
       continue;
     }
-    if (c.dh && c.width) launch_dh(piece, plan.dh, bf16, s);
+    if (c.dh && c.width) plan.few_dh ? launch_few_dh(piece, plan.dh_of_few, bf16, s) : launch_dh(piece, plan.dh, bf16, s);
     if (c.dweight && c.width)
       for (int k = 0; k < plan.dweight.count; ++k) {
         piece.head_first = k ? (int)plan.dweight.rows[0] : 0, piece.head_rows = (int)plan.dweight.rows[k];

@@ -69,6 +69,7 @@ constexpr float kExpBits = 15.0f;
 
 // logits of up to kFewTokens
 void launch_few_logits(const LossCall& c, bool bf16, hipStream_t s);
+void launch_few_dh(const LossCall& c, const FewDhPlan& plan, bool bf16, hipStream_t s);  // dh of up to kFewTokens
 void launch_logits(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
 void launch_dh(const LossCall& c, const ProductPlan& plan, bool bf16, hipStream_t s);
 void launch_both(const LossCall& c, const BothPlan& plan, bool bf16, hipStream_t s);  // dh and dW

@@ -103,6 +103,23 @@ constexpr int kTileTokens = 64;                    // of the smallest tile
 // pass and without 512 x 32000 x 4096 274.5, 279, 4096 x 128256 x 4096 6838, 6520.
 constexpr int64_t kWithoutPass = 20000000;
 
+// dh of up to kFewTokens from the head as it stands, in blocks of columns; `words` (whole lines of 64) to a workgroup, four workgroups to a CU
+constexpr int kFewDhWords = 512, kFewDhColumns = 128;  // kFewDhWords: whose dz a workgroup holds at a time
+struct FewDhPlan {
+  int blocks, words, splits;  // splits: workgroups that share a block's words
+  size_t workspace;
+};
+inline FewDhPlan few_dh_plan(int64_t tokens, int64_t vocab, int64_t width) {
+  FewDhPlan plan = {1, 64, 1, 0};
+  if (tokens == 0 || vocab == 0 || width == 0) return plan;
+  plan.blocks = (int)((width + kFewDhColumns - 1) / kFewDhColumns);
+  const int64_t most = std::max<int64_t>(4 * kCus / plan.blocks, 1), lines = (vocab + 63) / 64;
+  plan.words = (int)((lines + most - 1) / most) * 64;
+  plan.splits = (int)((vocab + plan.words - 1) / plan.words);
+  plan.workspace = plan.splits > 1 ? (size_t)plan.splits * tokens * width * sizeof(float) : 0;
+  return plan;
+}
+
 struct LossShape {
   int64_t tokens, vocab, width;
   bool bf16, dh, dweight;
@@ -117,6 +134,8 @@ struct LossPlan {
   HeadPlan dweight;
   BothPlan both;
   bool few;      // logits by the kernel for few tokens
+  bool few_dh;   // and dh
+  FewDhPlan dh_of_few;
   bool direct;   // no gather: rows are the tokens in their order
   bool counted;  // exponentials counted from a number for a row
   bool picked;   // the logits of entries are picked from the tiles
@@ -141,8 +160,13 @@ inline LossPlan loss_plan(const LossShape& p) {
     plan.both = both_plan(tokens, p.vocab, p.width, blocks(p.vocab), blocks(tokens), apart);
   }
   // Up to 16 tokens: straight from memory in fp32, where tiles would need a copy of the head that nothing else needs, or are few (us of the call:
-  // 3 x 1216 x 2326 27.4, 10.4 so, 4 x 1650 x 6912 with dh 58.3, 39.6; but 1 x 32000 x 2048 29.0, 33.6).
-  plan.few = p.tokens <= kFewTokens && (!p.bf16 || p.vocab < 64 * kCus || (!p.in_place && !p.dh));
+  // 3 x 1216 x 2326 27.4, 10.4 so, 4 x 1650 x 6912 with dh 58.3, 39.6; but in whole lines 1 x 32000 x 2048 29.0, 33.6).
+  plan.few = p.tokens <= kFewTokens && (!p.bf16 || p.vocab < 64 * kCus || !p.in_place);
+  // dh likewise, where tiles would need that copy (us of the call, with copy and tiles and so: fp32 1 x 116621 x 5083 2553, 1096, 16 x 1000 x 513 31.8,
+  // 25.3, bf16 2 x 4484 x 897 40.0, 30.6, 16 x 30001 x 1027 75.3, 77.2; without a need for the copy as well as tiles: bf16 3 x 4096 x 1024 24.0,
+  // 20.9, 16 x 16000 x 4096 75.5, 79.2).
+  plan.few_dh = plan.few && p.dh && !p.in_place;
+  if (plan.few_dh) plan.dh_of_few = few_dh_plan(tokens, p.vocab, p.width), plan.dh = {}, plan.both = {};
   // A tile has 64 rows at the least: up to there, rows of tokens that are left out cost nothing, and the states are read where they are (48 x
   // 32000 x 4096 69 us, 57 so).
   plan.direct = !gradients && (plan.few || (p.in_place && p.states_too && p.tokens <= kTileTokens));
@@ -150,7 +174,7 @@ inline LossPlan loss_plan(const LossShape& p) {
   // 2.5 us a round of tiles, and their order 3 (512 x 32000 x 4096 with 32 entries 333 us, 275 so).
   const double read = std::max((double)plan.rows * p.k * (double)p.width * (p.bf16 ? 2.0 : 4.0) / 4.3e6, 3.0 * (double)(p.k / (plan.rows <= 2 * kCus ? 16 : 4)));
   plan.picked = p.teacher && !plan.few && !plan.direct && read > 5.0 + 2.5 * (plan.logits.tiles_m * (double)plan.logits.tiles_n / kCus);
-  plan.counted = p.bf16 && p.dh && !p.dweight && plan.logits.kind == kLargeTile && plan.rows * p.vocab >= kWithoutPass;
+  plan.counted = p.bf16 && p.dh && !p.dweight && !plan.few && plan.logits.kind == kLargeTile && plan.rows * p.vocab >= kWithoutPass;
   return plan;
 }
 

@@ -161,6 +161,26 @@ LARGER = [(137, 34211, 64, 0, 0), (66, 17572, 64, 1, 1), (18, 34795, 64, 0, 0), 
 PICKED = [(512, 2000, 1024, "bf16", 64, 0.0), (700, 1031, 960, "bf16", 130, 0.2), (300, 1500, 1000, "f32", 100, 0.1), (2100, 4099, 512, "bf16", 256, 0.0)]
 
 
+# up to 16 tokens, whose dh is made from the head as it stands: words by one workgroup and by many, rows of many blocks of columns, more words
+# than stand in LDS at a time
+FEW = [(1, 30, 12), (4, 33, 515), (5, 31, 1029), (16, 700, 1003), (13, 3001, 1203), (3, 901, 5083), (2, 70001, 77), (15, 70003, 133), (7, 513, 9), (1, 1025, 3), (14, 1601, 32769)]
+
+
+@pytest.mark.parametrize("left_out", [0.0, 0.5])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,vocab,width", FEW)
+def test_few_tokens(loss, tokens, vocab, width, dtype, left_out):
+    for k, dweight in ((0, True), (3, False)):
+        Case(tokens, vocab, width, dtype, k=k, left_out=left_out).reference("cuda").run(loss, dweight=dweight).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [64, 515, 1208])
+def test_few_tokens_with_a_head_in_a_wider_matrix(loss, width, dtype):
+    """Rows that begin at any element, NaN between them."""
+    Case(9, 800, width, dtype).reference("cuda").run(loss, ld=3, offset=1).check()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("tokens,vocab,width,dh,dweight", LARGER)
 def test_larger_calls(loss, tokens, vocab, width, dh, dweight, dtype):

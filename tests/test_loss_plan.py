@@ -6,7 +6,7 @@ import subprocess
 
 import pytest
 
-from test_gpu_loss import LARGER, PICKED, SIZES
+from test_gpu_loss import FEW, LARGER, PICKED, SIZES
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PROGRAM = r"""
@@ -27,7 +27,8 @@ int main() {
     if (p.both.use) {
       tell("both_dh", p.both.dh), tell("both_dweight", p.both.dweight);
     } else {
-      if (dh) tell("dh", p.dh);
+      if (p.few_dh) printf(" few_dh%s%s", p.dh_of_few.splits > 1 ? "+" : "", p.dh_of_few.words > kFewDhWords ? "long" : "");
+      else if (dh) tell("dh", p.dh);
       for (int k = 0; k < p.dweight.count; ++k) tell(k ? "rest" : "dweight", p.dweight.parts[k]);
     }
     printf("%s%s%s%s rows:%ld\n", p.direct ? " direct" : "", p.counted ? " counted" : "", p.picked ? " picked" : "", tokens > p.rows ? " pieces" : "", (long)p.rows);
@@ -59,6 +60,7 @@ def shape(tokens, vocab, width, dtype="bf16", dh=True, dweight=True, k=1, teache
 
 def test_every_kernel_is_reached_by_a_tested_call(plans):
     calls = [shape(*s, dtype) for s in SIZES for dtype in ("bf16", "f32")]
+    calls += [shape(*s, dtype) for s in FEW for dtype in ("bf16", "f32")]
     calls += [shape(t, v, w, dh=dh, dweight=dweight) for t, v, w, dh, dweight in LARGER]
     calls += [shape(t, v, w, dtype, k=k, teacher=True) for t, v, w, dtype, k, _ in PICKED]
     calls += [shape(t, 700, 192, dh=False, dweight=False) for t in (1, 7, 40, 300)]            # outputs that are wanted
@@ -68,6 +70,7 @@ def test_every_kernel_is_reached_by_a_tested_call(plans):
     want = {f"logits:{k}" for k in kinds} | {"logits:small+"}
     want |= {f"{p}:{k}{split}" for p in ("dh", "dweight") for k in kinds for split in ("", "+")} | {"rest:small", "rest:small+", "rest:tile+", "rest:pairs"}
     want |= {f"both_{p}:{k}" for p in ("dh", "dweight") for k in ("small", "tile")} | {"both_dh:small+", "both_dh:tile+", "both_dweight:small+"}
+    want |= {"few_dh", "few_dh+", "few_dh+long"}
     want |= {"few", "direct", "counted", "picked", "pieces"}
     assert want <= got, sorted(want - got)
 
