@@ -15,8 +15,9 @@
  *     of dweight in fp32 beside it, for bf16).
  *   - Loss and gradients are one call: nothing but a weight for each token comes between the loss and its gradients, and the product
  *     with the head is made once for both.
- *   - Logits, sums of exponentials and losses are in single precision, gradients are summed in single precision and rounded to `dtype`
- *     once.  Of bf16 matrices, the gradient of a logit is rounded to bf16 before it is multiplied: 2^-9 of itself, at random.
+ *   - Logits, sums of exponentials and losses are in single precision, and a cross entropy near 0 is right to its own digits and never below 0.
+ *     Gradients are summed in single precision and rounded to `dtype` once.  Of bf16 matrices, the gradient of a logit is rounded to bf16
+ *     before it is multiplied: 2^-9 of itself, at random.
  *   - Tokens that are left out (no target, no entries) have loss, logarithm and gradients 0, whatever their hidden state is.
  *   - NaN and infinite logits make the loss of their token NaN, and with it the gradients it takes part in; an infinite or NaN entry of the
  *     head may do so to all tokens.

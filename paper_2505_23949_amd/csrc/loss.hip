@@ -10,7 +10,6 @@ using namespace tsenor_dev;
 
 constexpr int kThreads = 256;
 constexpr int kMaxEntries = TSENOR_LOSS_MAX_ENTRIES;
-constexpr float kLn2 = 0.693147180559945f;
 
 __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, lane_xor<1>(v)), v = fmaxf(v, lane_xor<2>(v)), v = fmaxf(v, lane_xor<7>(v));
@@ -222,11 +221,12 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
     if (lane == 0) most[wave] = z;
     __syncthreads();
     if (threadIdx.x == 0) {
-      c.refs[row] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * c.scale;
+      c.refs[row] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
       if (row == 0) *c.again = 0;
     }
   }
-  if (!c.dots) return;
+  if (c.words && threadIdx.x == 0) c.words[row] = (int)c.ids[token * c.ids_ld];
+  if (!c.sorted) return;
 
   // its entries by word, and where those of each part of a tile begin
   static_assert(kThreads == kMaxEntries);
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* he
 
 // A workgroup to a token: lse, the logits of its entries, loss; exponentials into dz.  1024 threads where there are few tokens (126 x 116032 x
 // 128: 36 -> 23 us), a wave where a token has little to do, so that more of them wait at a time (7744 x 512, one entry: 32 -> 15 us).
-// Exponents here are of 2 and counted from `largest`.
+// Exponents here are counted from `largest`.
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   constexpr int kSize = BF16 ? 2 : 4, kWaves = THREADS / kWave, kMine = 2;
@@ -284,6 +284,8 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   if (row >= rows_of(c)) return;
   const int token = c.count ? c.order[c.first + row] : c.first + row;
   const float2* const sums = c.sums + (int64_t)row * c.tiles;
+  const bool ready = c.refs && !*c.again;  // the exponentials are dz but for 1 / total and the weight
+  const float bits = exp_bits(BF16, ready), one = __builtin_amdgcn_exp2f(-bits);
 
   // what has to be read, asked for at once
   float2 mine[kMine];
@@ -322,10 +324,10 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   float total = 0.0f, all = 0.0f;
 #pragma unroll
   for (int u = 0; u < kMine; ++u)
-    if (u * THREADS + (int)threadIdx.x < c.tiles) total += mine[u].y * __builtin_amdgcn_exp2f(mine[u].x - largest);
-  for (int t = kMine * THREADS + (int)threadIdx.x; t < c.tiles; t += THREADS) total += sums[t].y * __builtin_amdgcn_exp2f(sums[t].x - largest);
+    if (u * THREADS + (int)threadIdx.x < c.tiles) total += mine[u].y * exp_from(mine[u].x, largest, c.scale, 0.0f);
+  for (int t = kMine * THREADS + (int)threadIdx.x; t < c.tiles; t += THREADS) total += sums[t].y * exp_from(sums[t].x, largest, c.scale, 0.0f);
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) all += expf(teacher[i] - top);
-  const int waves = c.k == 1 ? kWaves : 1;  // of an entry: all of them for the only one of a token
+  const int waves = c.teacher && c.k == 1 ? kWaves : 1;  // of an entry: all of them for the only one of a token
   if (!c.dots) {
     for (int i = c.k == 1 ? 0 : wave; i < c.k; i += kWaves) {
       const int word = words[i];
@@ -354,19 +356,21 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) total += part[0][w], all += part[1][w];
 
-  const float lse = log2f(total), log_all = logf(all);
+  const float rest = total;  // (with a teacher: of all words)
+  if (!c.teacher) total += exp_from(dots[0], largest, c.scale, bits);
+  const float log_total = logf(total * one), log_all = logf(all);
   const float unit = c.dz ? c.largest_weight[0] : 1.0f, weight = c.dloss ? (unit > 0.0f ? c.dloss[token] / unit : c.dloss[token]) : 1.0f;
   float loss = 0.0f;
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
     float s = dots[i];
     for (int w = 1; w < waves; ++w) s += dots[w];
-    s = fmaf(s, c.scale, -largest);
-    const float u = teacher[i] - top, p = c.teacher ? expf(u) / all : 1.0f;
-    q[i] = p, dentry[i] = __builtin_amdgcn_exp2f(s) / total;
+    const float u = teacher[i] - top, p = c.teacher ? expf(u) / all : 1.0f, own = exp_from(s, largest, c.scale, bits);
+    const float off = fmaf(largest - s, c.inverse_temperature, log_total);  // lse - z
+    q[i] = p, dentry[i] = own / total;
     if (!c.teacher)
-      loss = (lse - s) * kLn2;
+      loss = own > rest ? log1pf(rest / own) : off;
     else if (p != 0.0f)
-      loss = fmaf(p, u - log_all + (lse - s) * kLn2, loss);
+      loss = fmaf(p, u - log_all + off, loss);
   }
   loss = wave_sum(loss);
   __syncthreads();
@@ -375,17 +379,16 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   if (threadIdx.x == 0) {
     for (int w = 1; w < kWaves; ++w) loss += part[0][w];
     c.loss[token] = loss;
-    if (c.lse) c.lse[token] = (largest + lse) * kLn2;
+    if (c.lse) c.lse[token] = fmaf(largest, c.inverse_temperature, log_total);
   }
   if (!c.dz) return;
-  const bool ready = c.refs && !*c.again;  // the exponentials are dz but for 1 / total and the weight
   if (c.row_scale && threadIdx.x == 0) c.row_scale[row] = ready ? make_float2(1.0f / total, weight) : make_float2(1.0f, 1.0f);
   // (the same word twice: both write what belongs to both)
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
     float p = 0.0f;
     for (int j = 0; j < c.k; ++j)
       if (words[j] == words[i]) p += q[j];
-    dentry[i] = (ready ? total : weight) * (dentry[i] - p);
+    dentry[i] = (ready ? total : weight) * (c.teacher ? dentry[i] - p : -rest / total);
   }
   const float share = weight / total;
   uint16_t* const dz = static_cast<uint16_t*>(c.dz) + (int64_t)row * c.dz_ld * (BF16 ? 1 : 3);
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
     for (int u = 0; u < kAtOnce; ++u) {
       const int k = k0 + u * THREADS * 8;
       if (k >= c.dz_ld) continue;
-      const float factor = share * __builtin_amdgcn_exp2f(scale[u] - largest);
+      const float factor = share * exp_from(scale[u], largest, c.scale, 0.0f);
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = k + e < c.vocab ? (float)y[u][e] * factor : 0.0f;
@@ -505,6 +508,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& pla
   c.states_ld = (int)round_up(std::max<int64_t>(p.width, 1), 64), c.dz_ld = (int)round_up(p.vocab, 64);
   c.tile_n = plan.few ? kFewWords : plan.logits.kind == kLargeTile ? 128 : 64;
   c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
+  const bool picked = plan.picked || !c.teacher;
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     char* const begin = workspace + at;
@@ -516,6 +520,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& pla
   c.parts = reinterpret_cast<floatx4*>(take(std::max({plan.logits.workspace, plan.dh.workspace, plan.dweight.parts[0].workspace,
                                                       plan.dweight.parts[1].workspace, plan.both.dh.workspace + plan.both.dweight.workspace,
                                                       plan.dh_of_few.workspace})));
+  if (picked) c.dots = reinterpret_cast<float*>(take(rows * c.k * sizeof(float)));
   c.head = in_place || plan.direct || (plan.few && (!p.dh_out || plan.few_dh)) ? p.weight : take((size_t)p.vocab * c.states_ld * planes * 2);
   c.head_ld = in_place ? p.weight_ld : c.states_ld * planes;
   c.head_bytes = in_place ? (int)p.width * 2 : c.states_ld * 2;
@@ -529,8 +534,8 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& pla
   c.counts = c.teacher ? reinterpret_cast<uint8_t*>(take((size_t)p.tokens)) : nullptr;
   c.states_row = c.states_ld * planes;
   c.states = take((size_t)round_up(c.rows, 64) * c.states_ld * planes * 2);
+  if (!c.teacher) c.words = reinterpret_cast<int*>(take(rows * sizeof(int)));
   if (plan.picked) {
-    c.dots = reinterpret_cast<float*>(take(rows * c.k * sizeof(float)));
     c.sorted = reinterpret_cast<uint32_t*>(take(rows * c.k * sizeof(uint32_t)));
     c.begins = reinterpret_cast<uint16_t*>(take(rows * (c.tiles + 1) * sizeof(uint16_t)));
   }

@@ -59,6 +59,7 @@ __global__ __launch_bounds__(kWaves* kWave) void few_logits_kernel(LossCall c) {
   const int row = min(lane % 16, rows - 1), word = min(first + lane % 16, c.vocab - 1), at = lane / 16 * 8;  // (what lies past the last is not written)
   const char* const h = static_cast<const char*>(c.h) + (int64_t)(c.count ? c.order[c.first + row] : c.first + row) * c.h_ld * kSize;
   const char* const w = static_cast<const char*>(c.weight) + (int64_t)word * c.weight_ld * kSize;
+  const int target = wave == 0 && !c.teacher ? word_of(c, row) : -1;
   floatx4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
   const int whole = c.width / 32;
   int k = wave;
@@ -88,13 +89,14 @@ __global__ __launch_bounds__(kWaves* kWave) void few_logits_kernel(LossCall c) {
     largest = fmaxf(largest, sum[e]);
   }
   largest = fmaxf(largest, lane_xor<16>(largest));
-  largest = fmaxf(largest, lane_xor<32>(largest)) * c.scale - kExpBits;
+  largest = fmaxf(largest, lane_xor<32>(largest));
   const float base = largest == -__builtin_inff() ? 0.0f : largest;
   float x[4], total = 0.0f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    x[e] = __builtin_amdgcn_exp2f(fmaf(sum[e], c.scale, -base));
-    total += x[e];
+    x[e] = exp_from(sum[e], base, c.scale, exp_bits(BF16, false));
+    if (col + e != target) total += x[e];
+    else if (token < rows) c.dots[token] = sum[e];
   }
   total += lane_xor<16>(total);
   total += lane_xor<32>(total);

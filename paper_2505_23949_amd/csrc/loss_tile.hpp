@@ -258,9 +258,9 @@ __device__ __forceinline__ void store_staged(const uint8_t* staged, int valid, R
   }
 }
 
-// Exponentials of a row counted from one number: sums up to here are taken (2^21 of them stay far inside single precision, and what they
+// Exponentials of a row counted from one number: a lane's sums up to here are taken (2^22 of them stay far inside single precision, and what they
 // are divided by, times a weight, inside its other end).
-constexpr float kMostOverRef = 0x1p60f;
+constexpr float kMostOverRef = 0x1p59f;
 
 // What becomes of a tile of logits.
 template <bool BF16, bool COUNTED, int TN, int TM>
@@ -271,15 +271,19 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
   // a lane holds, of row 32 j + r of its wave's rows of a, columns TN (8 g + 4 q + e) + t of its wave's rows of b.  The sums of a row are
   // of those 32 TN columns: no wave waits for another.
   const int wave_col = n0 + wave_n * 32 * TN, col0 = wave_col + 4 * TN * q;
+  constexpr float kBits = exp_bits(BF16, COUNTED);
   // Entries: a wave puts 32 rows into LDS, where their entries' columns can be picked.  (distill 4096 x 128256 x 4096 with 128 entries:
   // the rows kernel would read 4 GB of the head again for them, 1 ms)
-  uint32_t entries[TM];
-  if (c.dots) {
+  uint32_t entries[TM];  // (of a target: its column among the wave's)
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int row = m0 + (wave_m * TM + j) * 32 + r;
-      entries[j] = 0;
-      if (row < m && wave_col < n) __builtin_memcpy(&entries[j], c.begins + (int64_t)row * (c.tiles + 1) + wave_col / (32 * TN), 4);
+  for (int j = 0; j < TM; ++j) {
+    const int row = m0 + (wave_m * TM + j) * 32 + r;
+    entries[j] = c.teacher ? 0 : UINT32_MAX;
+    if (row < m && wave_col < n) {
+      if (!c.teacher)
+        entries[j] = (uint32_t)(word_of(c, row) - wave_col);
+      else if (c.sorted)
+        __builtin_memcpy(&entries[j], c.begins + (int64_t)row * (c.tiles + 1) + wave_col / (32 * TN), 4);
     }
   }
 #pragma unroll
@@ -298,7 +302,8 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
         for (int e = 0; e < 16; ++e)
           if (col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
     }
-    if (c.dots && __any((entries[j] & 0xFFFFu) != entries[j] >> 16)) {
+    const bool apart = !c.teacher && __any(entries[j] < 32 * TN);  // a target among them
+    if (apart || (c.teacher && __any((entries[j] & 0xFFFFu) != entries[j] >> 16))) {
       float* const logits = reinterpret_cast<float*>(staged + r * Staged<TN, 4>::kStride);
 #pragma unroll
       for (int g = 0; g < 4; ++g)
@@ -309,9 +314,13 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
           for (int k = 0; k < 4; ++k) v[k] = sum[k % TN][j][4 * g + e + k / TN];
           *reinterpret_cast<floatx4*>(logits + TN * (8 * g + 4 * q + e)) = v;
         }
-      for (int i = (int)(entries[j] & 0xFFFFu) + q; i < (int)(entries[j] >> 16); i += 2) {
-        const uint32_t key = c.sorted[(int64_t)row * c.k + i];
-        c.dots[(int64_t)row * c.k + (key & 255)] = logits[(int)(key >> 8) - wave_col];
+      if (apart) {
+        if (q == 0 && entries[j] < 32 * TN) c.dots[row] = logits[entries[j]];
+      } else {
+        for (int i = (int)(entries[j] & 0xFFFFu) + q; i < (int)(entries[j] >> 16); i += 2) {
+          const uint32_t key = c.sorted[(int64_t)row * c.k + i];
+          c.dots[(int64_t)row * c.k + (key & 255)] = logits[(int)(key >> 8) - wave_col];
+        }
       }
     }
     float largest = -__builtin_inff();
@@ -319,7 +328,7 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
     for (int t = 0; t < TN; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) largest = fmaxf(largest, sum[t][j][e]);
-    largest = fmaxf(largest, lane_xor<32>(largest)) * c.scale - kExpBits;
+    largest = fmaxf(largest, lane_xor<32>(largest));
     if (COUNTED && row < m) largest = c.refs[row];
     const float base = largest == -__builtin_inff() ? 0.0f : largest;
     float v = 0.0f;
@@ -330,7 +339,7 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int t = 0; t < TN; ++t) {
-          x[e * TN + t] = __builtin_amdgcn_exp2f(fmaf(sum[t][j][4 * g + e], c.scale, -base));
+          x[e * TN + t] = exp_from(sum[t][j][4 * g + e], base, c.scale, kBits);
           v += x[e * TN + t];
         }
       const int col = col0 + 8 * TN * g;
@@ -346,8 +355,19 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
         }
       }
     }
-    v += lane_xor<32>(v);
     if (COUNTED && row < m && v > kMostOverRef) *c.again = 1;  // (whoever finds one writes the same)
+    if (apart) {  // (rare where there are many words: once more, rather than a comparison with each)
+      const int target = (int)entries[j] - 4 * TN * q;
+      v = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int t = 0; t < TN; ++t) {
+          const float x = exp_from(sum[t][j][e], base, c.scale, kBits);
+          v += TN * (e / 4 * 8 + e % 4) + t == target ? 0.0f : x;
+        }
+    }
+    v += lane_xor<32>(v);
     if (q == 0 && row < m && wave_col < n) c.sums[(int64_t)row * c.tiles + wave_col / (32 * TN)] = make_float2(largest, v);
   }
 }
