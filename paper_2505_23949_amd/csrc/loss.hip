@@ -327,7 +327,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
     if (u * THREADS + (int)threadIdx.x < c.tiles) total += mine[u].y * exp_from(mine[u].x, largest, c.scale, 0.0f);
   for (int t = kMine * THREADS + (int)threadIdx.x; t < c.tiles; t += THREADS) total += sums[t].y * exp_from(sums[t].x, largest, c.scale, 0.0f);
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) all += expf(teacher[i] - top);
-  const int waves = c.teacher && c.k == 1 ? kWaves : 1;  // of an entry: all of them for the only one of a token
+  const int waves = c.k == 1 && !c.dots ? kWaves : 1;  // of an entry: all of them for the only one of a token, unless its logit is there already
   if (!c.dots) {
     for (int i = c.k == 1 ? 0 : wave; i < c.k; i += kWaves) {
       const int word = words[i];
