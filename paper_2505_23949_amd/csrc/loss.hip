@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
       if (row == 0) *c.again = 0;
     }
   }
-  if (c.words && threadIdx.x == 0) c.words[row] = (int)c.ids[token * c.ids_ld];
+  if (c.words && threadIdx.x == 0) c.words[row] = (int)c.ids[token * c.ids_ld];  // (it counts: it has a word of the vocabulary)
   if (!c.sorted) return;
 
   // its entries by word, and where those of each part of a tile begin
@@ -272,8 +272,9 @@ __global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* he
   }
 }
 
-// A workgroup to a token: lse, the logits of its entries, loss; exponentials into dz.  1024 threads where there are few tokens (126 x 116032 x
-// 128: 36 -> 23 us), a wave where a token has little to do, so that more of them wait at a time (7744 x 512, one entry: 32 -> 15 us).
+// A workgroup to a token: lse, loss; exponentials into dz.  1024 threads where there are few tokens with many words (126 x 116032 x 128: 36 -> 23 us) or
+// several entries (100 x 32000 x 1024 with 8 and both gradients, the call: 88 -> 82; scores of it lose 0.6), a wave where a token has little to do, so
+// that more of them wait at a time (7744 x 512, one entry: 32 -> 15 us).
 // Exponents here are counted from `largest`.
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
@@ -301,7 +302,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
     const bool valid = id >= 0 && id < c.vocab;
     const float u = c.teacher ? teacher_of(c, token, i) : valid ? 0.0f : -__builtin_inff();
     words[i] = valid ? (int)id : -1, teacher[i] = u;
-    if (c.dots) dots[i] = valid ? c.dots[(int64_t)row * c.k + i] : 0.0f;
+    dots[i] = valid ? c.dots[(int64_t)row * c.k + i] : 0.0f;
     top = fmaxf(top, u), any |= u != -__builtin_inff();  // (NaN takes part)
   }
   if (!c.count && !__syncthreads_or(any)) {  // nothing has left it out before
@@ -327,27 +328,6 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
     if (u * THREADS + (int)threadIdx.x < c.tiles) total += mine[u].y * exp_from(mine[u].x, largest, c.scale, 0.0f);
   for (int t = kMine * THREADS + (int)threadIdx.x; t < c.tiles; t += THREADS) total += sums[t].y * exp_from(sums[t].x, largest, c.scale, 0.0f);
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) all += expf(teacher[i] - top);
-  const int waves = c.k == 1 && !c.dots ? kWaves : 1;  // of an entry: all of them for the only one of a token, unless its logit is there already
-  if (!c.dots) {
-    for (int i = c.k == 1 ? 0 : wave; i < c.k; i += kWaves) {
-      const int word = words[i];
-      float s = 0.0f;
-      if (word >= 0) {
-        const char* const h = static_cast<const char*>(c.h) + (int64_t)token * c.h_ld * kSize;
-        const char* const w = static_cast<const char*>(c.weight) + word * c.weight_ld * kSize;
-#pragma unroll 2
-        for (int k = (wave % waves * kWave + lane) * 8; k < c.width; k += waves * kWave * 8) {
-          float x[8], y[8];
-          load_row8<BF16>(h, k, c.width, x);
-          load_row8<BF16>(w, k, c.width, y);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
-        }
-      }
-      s = wave_sum(s);
-      if (lane == 0) dots[waves == 1 ? i : wave] = s;
-    }
-  }
   total = wave_sum(total), all = wave_sum(all);
   __syncthreads();
   if (lane == 0) part[0][wave] = total, part[1][wave] = all;
@@ -356,19 +336,17 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) total += part[0][w], all += part[1][w];
 
-  const float rest = total;  // (with a teacher: of all words)
-  if (!c.teacher) total += exp_from(dots[0], largest, c.scale, bits);
+  const float rest = total;  // (of several entries: of all words)
+  if (c.k == 1) total += exp_from(dots[0], largest, c.scale, bits);
   const float log_total = logf(total * one), log_all = logf(all);
   const float unit = c.dz ? c.largest_weight[0] : 1.0f, weight = c.dloss ? (unit > 0.0f ? c.dloss[token] / unit : c.dloss[token]) : 1.0f;
   float loss = 0.0f;
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
-    float s = dots[i];
-    for (int w = 1; w < waves; ++w) s += dots[w];
-    const float u = teacher[i] - top, p = c.teacher ? expf(u) / all : 1.0f, own = exp_from(s, largest, c.scale, bits);
+    const float s = dots[i], u = teacher[i] - top, p = c.teacher ? expf(u) / all : 1.0f, own = exp_from(s, largest, c.scale, bits);
     const float off = fmaf(largest - s, c.inverse_temperature, log_total);  // lse - z
     q[i] = p, dentry[i] = own / total;
-    if (!c.teacher)
-      loss = own > rest ? log1pf(rest / own) : off;
+    if (c.k == 1)
+      loss = p * (own > rest ? log1pf(rest / own) : off);  // (p is 1, or a teacher's NaN)
     else if (p != 0.0f)
       loss = fmaf(p, u - log_all + off, loss);
   }
@@ -388,7 +366,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
     float p = 0.0f;
     for (int j = 0; j < c.k; ++j)
       if (words[j] == words[i]) p += q[j];
-    dentry[i] = (ready ? total : weight) * (c.teacher ? dentry[i] - p : -rest / total);
+    dentry[i] = (ready ? total : weight) * (c.k == 1 ? -(rest / total) * p : dentry[i] - p);
   }
   const float share = weight / total;
   uint16_t* const dz = static_cast<uint16_t*>(c.dz) + (int64_t)row * c.dz_ld * (BF16 ? 1 : 3);
@@ -433,7 +411,7 @@ void launch_rows(const LossCall& c, hipStream_t s) {
   const unsigned rows = (unsigned)c.rows;
   if (rows <= 2 * kCus && (c.k > 4 || c.tiles > 1024))
     rows_kernel<BF16, 1024><<<rows, 1024, 0, s>>>(c);
-  else if (rows > 4 * kCus && c.vocab <= 2048 && c.k <= kWave && (c.k == 1 || c.dots))
+  else if (rows > 4 * kCus && c.vocab <= 2048 && c.k <= kWave)
     rows_kernel<BF16, kWave><<<rows, kWave, 0, s>>>(c);
   else
     rows_kernel<BF16, kThreads><<<rows, kThreads, 0, s>>>(c);
@@ -508,7 +486,6 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& pla
   c.states_ld = (int)round_up(std::max<int64_t>(p.width, 1), 64), c.dz_ld = (int)round_up(p.vocab, 64);
   c.tile_n = plan.few ? kFewWords : plan.logits.kind == kLargeTile ? 128 : 64;
   c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
-  const bool picked = plan.picked || !c.teacher;
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     char* const begin = workspace + at;
@@ -520,7 +497,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& pla
   c.parts = reinterpret_cast<floatx4*>(take(std::max({plan.logits.workspace, plan.dh.workspace, plan.dweight.parts[0].workspace,
                                                       plan.dweight.parts[1].workspace, plan.both.dh.workspace + plan.both.dweight.workspace,
                                                       plan.dh_of_few.workspace})));
-  if (picked) c.dots = reinterpret_cast<float*>(take(rows * c.k * sizeof(float)));
+  c.dots = reinterpret_cast<float*>(take(rows * c.k * sizeof(float)));
   c.head = in_place || plan.direct || (plan.few && (!p.dh_out || plan.few_dh)) ? p.weight : take((size_t)p.vocab * c.states_ld * planes * 2);
   c.head_ld = in_place ? p.weight_ld : c.states_ld * planes;
   c.head_bytes = in_place ? (int)p.width * 2 : c.states_ld * 2;
@@ -534,7 +511,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& pla
   c.counts = c.teacher ? reinterpret_cast<uint8_t*>(take((size_t)p.tokens)) : nullptr;
   c.states_row = c.states_ld * planes;
   c.states = take((size_t)round_up(c.rows, 64) * c.states_ld * planes * 2);
-  if (!c.teacher) c.words = reinterpret_cast<int*>(take(rows * sizeof(int)));
+  if (c.k == 1) c.words = reinterpret_cast<int*>(take(rows * sizeof(int)));
   if (plan.picked) {
     c.sorted = reinterpret_cast<uint32_t*>(take(rows * c.k * sizeof(uint32_t)));
     c.begins = reinterpret_cast<uint16_t*>(take(rows * (c.tiles + 1) * sizeof(uint16_t)));

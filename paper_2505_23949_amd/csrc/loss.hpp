@@ -4,11 +4,11 @@
 //   order     (once) the tokens that count in front, those left out behind them: the products then have no rows for nothing
 //   gather    the piece's hidden states, one behind the other; outputs of those left out are cleared
 //   logits    z = h W^T in tiles: of each tile's rows the largest logit and the sum of exponentials, and, where gradients are wanted,
-//             the exponentials; the target's logit, whose exponential the sum does not have
+//             the exponentials; the logits of entries, and of a token's only one not its exponential in the sum
 //   rows      for each token: the sums of its tiles joined, the logits of its entries, its loss; the exponentials become dz
 //
-// A target's own exponential stays apart from the sum of all others, `rest`, until the end: loss = log(1 + rest / own), and the gradient of its
-// logit is -rest / (rest + own).  Of a word that a model has learned both are small, and as lse - z and p - 1 they would be what is left of
+// The exponential of a target (or of a teacher's only entry) stays apart from the sum of all others, `rest`, until the end: loss = log(1 + rest / own),
+// and the gradient of its logit is -rest / (rest + own).  Of a word that a model has learned both are small, and as lse - z and p - 1 they would be what is left of
 // numbers thousands of times as large; and its logit is the one that the sum would have had, from the same product.  (Losses of 1e-6 to
 // 0.1, 8192 words of width 512 to 37543 of 64: from a second product and lse - z up to 4.6e-6 off, which can be more than all of one, and some below 0; at
 // most 3.9e-6 of itself off so, none below 0, in the same time.)
@@ -43,10 +43,10 @@ struct LossCall {
   void* states;            // hidden states of the piece, states_ld to a row and plane, zeros behind the width and the last row
   const void* head;        // the head (its own memory, where its rows begin at multiples of 16 bytes and end there), head_ld to a row
   float2* sums;            // of each row and tile: a logit c, the sum of 2^((z - c) scale + bits) (bits: exp_bits)
-  // the logits of the entries, where the tiles that they are in leave them (NULL: the rows kernel makes them)
+  // the logits of the entries, by the workgroups that make them
   float* dots;             // of each row and entry
-  int* words;              // of each row: its target (NULL: they are read where they are; of a teacher's entries not needed)
-  uint32_t* sorted;        // of each row: its k entries by word, word << 8 | entry, those that take no part behind
+  int* words;              // of each row: its only entry (NULL: they are read where they are, or there are several)
+  uint32_t* sorted;        // of each row: its k entries by word, word << 8 | entry, those that take no part behind (NULL likewise, or k is 1)
   uint16_t* begins;        // of each row and part of a tile, and once more: how many entries stand before it
   // Exponentials counted from one number for a row (bf16, dh alone): they are dz but for a factor of the row, which dh takes at the end, and
   // its entries.  The number comes from the logits of some of the row's entries before all others are known.
@@ -76,7 +76,7 @@ __host__ __device__ constexpr float exp_bits(bool bf16, bool counted) { return b
 // The difference is taken before the scaling, so that the largest is 2^bits whatever the scale is.
 __device__ __forceinline__ float exp_from(float z, float from, float scale, float bits) { return __builtin_amdgcn_exp2f(fmaf(z - from, scale, bits)); }
 
-// the target of a row, -1 for none
+// the only entry of a row, -1 for none
 __device__ __forceinline__ int word_of(const LossCall& c, int row) {
   if (c.words) return c.words[row];
   const int64_t id = c.ids[(int64_t)(c.first + row) * c.ids_ld];

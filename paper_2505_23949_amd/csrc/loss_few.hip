@@ -4,6 +4,7 @@
 // columns 8 (l / 16) to 8 (l / 16) + 7 of row l % 16, of a word and of a token; the words are the first operand of the matrix instruction,
 // so that it ends up with four neighbouring words of a token.  Single precision takes the fp32 instruction: 16 rows are too few for its
 // rate to matter (8 operations a byte).
+// Of several entries to a token, all threads look for those among the workgroup's words, in logits that LDS holds.
 // Against tiles of 64 x 128, which need operands in whole lines, and where few of them fill the GPU (us of the kernel): 2 x 534 x 6848
 // 31, 12 so.
 #include "loss.hpp"
@@ -52,6 +53,7 @@ __device__ __forceinline__ Raw8<BF16> load_end(const char* row, int k, int width
 template <bool BF16>
 __global__ __launch_bounds__(kWaves* kWave) void few_logits_kernel(LossCall c) {
   __shared__ floatx4 parts[kWaves][kWave];
+  __shared__ float logits[kFewTokens][kFewWords];
   constexpr int kSize = BF16 ? 2 : 4;
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int rows = rows_of(c), first = (int)blockIdx.x * kFewWords;
@@ -59,7 +61,13 @@ __global__ __launch_bounds__(kWaves* kWave) void few_logits_kernel(LossCall c) {
   const int row = min(lane % 16, rows - 1), word = min(first + lane % 16, c.vocab - 1), at = lane / 16 * 8;  // (what lies past the last is not written)
   const char* const h = static_cast<const char*>(c.h) + (int64_t)(c.count ? c.order[c.first + row] : c.first + row) * c.h_ld * kSize;
   const char* const w = static_cast<const char*>(c.weight) + (int64_t)word * c.weight_ld * kSize;
-  const int target = wave == 0 && !c.teacher ? word_of(c, row) : -1;
+  const int target = wave == 0 && c.k == 1 ? word_of(c, row) : -1;
+  const int pairs = c.k > 1 ? rows * c.k : 0;
+  const auto id_of = [&](int i) {
+    const int of = i / c.k;
+    return c.ids[(int64_t)(c.count ? c.order[c.first + of] : c.first + of) * c.ids_ld + (i - of * c.k)];
+  };
+  int64_t id = (int)threadIdx.x < pairs ? id_of((int)threadIdx.x) : -1;  // (asked for before the rows)
   floatx4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
   const int whole = c.width / 32;
   int k = wave;
@@ -76,9 +84,19 @@ __global__ __launch_bounds__(kWaves* kWave) void few_logits_kernel(LossCall c) {
     sum = multiply<BF16>(load_end<BF16>(w, whole * 32 + at, c.width), load_end<BF16>(h, whole * 32 + at, c.width), sum);
   parts[wave][lane] = sum;
   __syncthreads();
-  if (wave != 0) return;
+  if (wave == 0) {
 #pragma unroll
-  for (int k = 1; k < kWaves; ++k) sum += parts[k][lane];
+    for (int k = 1; k < kWaves; ++k) sum += parts[k][lane];
+    if (pairs) *reinterpret_cast<floatx4*>(&logits[lane % 16][lane / 16 * 4]) = sum;
+  }
+  if (pairs) {
+    if (pairs > kWave) __syncthreads();  // (up to there only the first wave has any)
+    for (int i = (int)threadIdx.x; i < pairs; i += kWaves * kWave) {
+      if (i != (int)threadIdx.x) id = id_of(i);
+      if (id >= first && id < min(first + kFewWords, c.vocab)) c.dots[i] = logits[i / c.k][(int)id - first];
+    }
+  }
+  if (wave != 0) return;
 
   // token lane % 16, words first + 4 (lane / 16) to + 3
   const int col = first + lane / 16 * 4, token = lane % 16;

@@ -138,7 +138,7 @@ struct LossPlan {
   FewDhPlan dh_of_few;
   bool direct;   // no gather: rows are the tokens in their order
   bool counted;  // exponentials counted from a number for a row
-  bool picked;   // the logits of entries are picked from the tiles
+  bool picked;   // several entries to a token, put in order for the tiles that they are in
 };
 
 inline LossPlan loss_plan(const LossShape& p) {
@@ -169,11 +169,9 @@ inline LossPlan loss_plan(const LossShape& p) {
   if (plan.few_dh) plan.dh_of_few = few_dh_plan(tokens, p.vocab, p.width), plan.dh = {}, plan.both = {};
   // A tile has 64 rows at the least: up to there, rows of tokens that are left out cost nothing, and the states are read where they are (48 x
   // 32000 x 4096 69 us, 57 so).
-  plan.direct = !gradients && (plan.few || (p.in_place && p.states_too && p.tokens <= kTileTokens));
-  // Entries: the rows kernel reads their rows of the head at 4.3 TB/s, 16 (4) at a time of a token in 3 us; picked from the tiles they cost
-  // 2.5 us a round of tiles, and their order 3 (512 x 32000 x 4096 with 32 entries 333 us, 275 so).
-  const double read = std::max((double)plan.rows * p.k * (double)p.width * (p.bf16 ? 2.0 : 4.0) / 4.3e6, 3.0 * (double)(p.k / (plan.rows <= 2 * kCus ? 16 : 4)));
-  plan.picked = p.teacher && !plan.few && !plan.direct && read > 5.0 + 2.5 * (plan.logits.tiles_m * (double)plan.logits.tiles_n / kCus);
+  plan.direct = !gradients && (plan.few || (p.in_place && p.states_too && p.tokens <= kTileTokens && plan.logits.kind == kSmallTile));
+  // (few tokens and direct tiles look through all entries)
+  plan.picked = p.teacher && p.k > 1 && !plan.few && !plan.direct;
   plan.counted = p.bf16 && p.dh && !p.dweight && !plan.few && plan.logits.kind == kLargeTile && plan.rows * p.vocab >= kWithoutPass;
   return plan;
 }

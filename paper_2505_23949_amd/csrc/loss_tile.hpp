@@ -273,19 +273,29 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
   const int wave_col = n0 + wave_n * 32 * TN, col0 = wave_col + 4 * TN * q;
   constexpr float kBits = exp_bits(BF16, COUNTED);
   // Entries: a wave puts 32 rows into LDS, where their entries' columns can be picked.  (distill 4096 x 128256 x 4096 with 128 entries:
-  // the rows kernel would read 4 GB of the head again for them, 1 ms)
-  uint32_t entries[TM];  // (of a target: its column among the wave's)
+  // read again, their rows of the head would be 4 GB, 1 ms)
+  const bool only = c.k == 1;
+  uint32_t entries[TM];  // of the only one of a row, its column among the wave's; of several, where they begin and end
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
     const int row = m0 + (wave_m * TM + j) * 32 + r;
-    entries[j] = c.teacher ? 0 : UINT32_MAX;
+    entries[j] = only ? UINT32_MAX : 0;
     if (row < m && wave_col < n) {
-      if (!c.teacher)
-        entries[j] = (uint32_t)(word_of(c, row) - wave_col);
-      else if (c.sorted)
+      if (only)
+        entries[j] = (uint32_t)((TM > 1 ? c.words[row] : word_of(c, row)) - wave_col);
+      else if (TM > 1 || c.sorted)
         __builtin_memcpy(&entries[j], c.begins + (int64_t)row * (c.tiles + 1) + wave_col / (32 * TN), 4);
     }
   }
+  // several entries that nothing has put in order (direct calls, which have small tiles): the wave looks at all of its rows'.  use(row of the 32, entry, column)
+  const auto look = [&](auto use) {
+    const int rows = min(m - (m0 + wave_m * 32), 32);
+    for (int i = lane; i < rows * c.k; i += kWave) {
+      const int row = i / c.k;
+      const int64_t id = c.ids[(int64_t)(c.first + m0 + wave_m * 32 + row) * c.ids_ld + (i - row * c.k)];
+      if (id >= wave_col && id < min(wave_col + 32 * TN, n)) use(row, i - row * c.k, (int)id - wave_col);
+    }
+  };
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
     const int row = m0 + (wave_m * TM + j) * 32 + r;
@@ -302,8 +312,11 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
         for (int e = 0; e < 16; ++e)
           if (col0 + TN * (e / 4 * 8 + e % 4) + t >= n) sum[t][j][e] = -__builtin_inff();
     }
-    const bool apart = !c.teacher && __any(entries[j] < 32 * TN);  // a target among them
-    if (apart || (c.teacher && __any((entries[j] & 0xFFFFu) != entries[j] >> 16))) {
+    const bool apart = only && __any(entries[j] < 32 * TN);  // the exponential of one among them
+    bool some = (entries[j] & 0xFFFFu) != entries[j] >> 16;
+    if constexpr (TM == 1)
+      if (!only && !c.sorted) look([&](int, int, int) { some = true; });
+    if (apart || (!only && __any(some))) {
       float* const logits = reinterpret_cast<float*>(staged + r * Staged<TN, 4>::kStride);
 #pragma unroll
       for (int g = 0; g < 4; ++g)
@@ -314,8 +327,12 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
           for (int k = 0; k < 4; ++k) v[k] = sum[k % TN][j][4 * g + e + k / TN];
           *reinterpret_cast<floatx4*>(logits + TN * (8 * g + 4 * q + e)) = v;
         }
-      if (apart) {
+      if (only) {
         if (q == 0 && entries[j] < 32 * TN) c.dots[row] = logits[entries[j]];
+      } else if (TM == 1 && !c.sorted) {
+        look([&](int k, int i, int col) {
+          c.dots[(int64_t)(m0 + wave_m * 32 + k) * c.k + i] = reinterpret_cast<const float*>(staged + k * Staged<TN, 4>::kStride)[col];
+        });
       } else {
         for (int i = (int)(entries[j] & 0xFFFFu) + q; i < (int)(entries[j] >> 16); i += 2) {
           const uint32_t key = c.sorted[(int64_t)row * c.k + i];

@@ -89,3 +89,50 @@ def test_learned_words_with_weights(loss, dtype):  # noqa: F811
     case.dloss = torch.randn(300, generator=torch.Generator().manual_seed(2))
     expect(case, True).run(loss)
     check(case)
+
+
+# few tokens alone and with gradients, tiles that read everything in place, tiles with rows by 256, 64 and 1024 threads, shared sums, large tiles,
+# exponentials counted from one number for a row
+DISTILLED = [(1, 8192, 512, 0, 0), (9, 1000, 256, 1, 1), (1, 17000, 64, 0, 0), (48, 17000, 256, 0, 0), (300, 2048, 64, 1, 1), (300, 2048, 2048, 1, 1),
+             (1100, 2048, 64, 1, 1), (18, 130, 2048, 1, 0), (265, 37543, 64, 1, 1), (538, 40884, 64, 1, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("whole", [True, False])
+@pytest.mark.parametrize("tokens,vocab,width,dh,dweight", DISTILLED)
+def test_learned_from_a_teacher_with_one_entry(loss, tokens, vocab, width, dh, dweight, whole, dtype):  # noqa: F811
+    """As of a target: q is 1, whatever the teacher's logit is."""
+    case = expect(learned(tokens, vocab, width, dtype, whole, seed=1), whole)
+    case.k, case.ids, case.logits = 1, case.targets[:, None].clone(), 5.0 * torch.randn(tokens, 1, generator=torch.Generator().manual_seed(3))
+    case.run(loss, dh=bool(dh), dweight=bool(dweight))
+    check(case)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,vocab,width", [c[:3] for c in DISTILLED])
+def test_divergence_of_what_is_learned(loss, tokens, vocab, width, dtype):  # noqa: F811
+    """Several entries, of which the teacher means one: an error of the logits counts by how far the two distributions are apart, as the loss and
+    its sum of exponentials have the same ones."""
+    case, k = learned(tokens, vocab, width, dtype, False, seed=2), 8
+    gen = torch.Generator().manual_seed(4)
+    case.k, case.ids = k, torch.randint(0, vocab, (tokens, k), generator=gen)
+    case.ids[:, 0] = case.targets
+    case.logits = torch.randn(tokens, k, generator=gen) - 14.0
+    case.logits[:, 0] = 0.0
+    case.run(loss, dh=False, dweight=False)
+    h, w, u = case.h.double(), case.weight.double(), case.logits.double()
+    z, log_q = h @ w.t(), torch.log_softmax(u, 1)
+    q, lse = log_q.exp(), torch.logsumexp(z, 1)
+    off, p = lse[:, None] - z.gather(1, case.ids), (z - lse[:, None]).exp()
+    want = (q * (log_q + off)).sum(1)
+    apart = p.scatter_add(1, case.ids, -q).abs()
+    rest = 1.0 - p.gather(1, case.targets[:, None])[:, 0]
+    # logits: sums of `width` products; the sum of exponentials: arguments of those that are not the largest, and additions.  It has the largest in it, here
+    # about all of it, from the first lane that adds it on: each of the at most 4 + 64 + 16 + vocab / 64 additions behind each other that follow
+    # rounds a number of at least 1/2 and below 2, by U at the most, however small what is added is, and an error of a sum near 1 is one of its logarithm;
+    # q, of 8 exponentials, their sum and a division; what is summed with it
+    bound = 2 * (apart * ((width + 2) * U * (h.abs() @ w.abs().t()))).sum(1) + 2 * (z.amax(1) - z.amin(1)) * U * rest + (84 + vocab / 64 + 8) * U
+    bound += (q * ((2 * log_q.abs() + 40) * U * (log_q + off).abs() + 8 * U * (u.abs() + log_q.abs() + off))).sum(1)
+    err = (case.out["loss"].double().cpu() - want).abs()
+    assert (err <= bound).all(), (float((err / bound).max()), float(err.max()))
+    assert float(bound.median()) < (100 + vocab / 64) * U + 2e-5
