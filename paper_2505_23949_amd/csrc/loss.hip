@@ -272,9 +272,7 @@ __global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* he
   }
 }
 
-// A workgroup to a token: lse, loss; exponentials into dz.  1024 threads where there are few tokens with many words (126 x 116032 x 128: 36 -> 23 us) or
-// several entries (100 x 32000 x 1024 with 8 and both gradients, the call: 88 -> 82; scores of it lose 0.6), a wave where a token has little to do, so
-// that more of them wait at a time (7744 x 512, one entry: 32 -> 15 us).
+// A workgroup to a token: lse, loss; exponentials into dz.
 // Exponents here are counted from `largest`.
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
@@ -407,16 +405,16 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
 }
 
 template <bool BF16>
-void launch_rows(const LossCall& c, hipStream_t s) {
+void launch_rows(const LossCall& c, int threads, hipStream_t s) {
   const unsigned rows = (unsigned)c.rows;
-  if (rows <= 2 * kCus && (c.k > 4 || c.tiles > 1024))
+  if (threads == 1024)
     rows_kernel<BF16, 1024><<<rows, 1024, 0, s>>>(c);
-  else if (rows > 4 * kCus && c.vocab <= 2048 && c.k <= kWave)
+  else if (threads == kWave)
     rows_kernel<BF16, kWave><<<rows, kWave, 0, s>>>(c);
   else
     rows_kernel<BF16, kThreads><<<rows, kThreads, 0, s>>>(c);
 }
-void launch_rows(const LossCall& c, bool bf16, hipStream_t s) { bf16 ? launch_rows<true>(c, s) : launch_rows<false>(c, s); }
+void launch_rows(const LossCall& c, int threads, bool bf16, hipStream_t s) { bf16 ? launch_rows<true>(c, threads, s) : launch_rows<false>(c, threads, s); }
 
 // no token counts, or there is none: zeros
 template <bool BF16>
@@ -484,8 +482,7 @@ size_t lay_out(const tsenor_head& p, char* workspace, LossCall& c, LossPlan& pla
   c.dloss = p.dloss, c.loss = p.loss_out, c.lse = p.lse_out, c.dh = p.dh_out, c.dweight = p.dweight_out;
   c.tokens = (int)p.tokens, c.vocab = (int)p.vocab, c.width = (int)p.width, c.rows = (int)plan.rows;
   c.states_ld = (int)round_up(std::max<int64_t>(p.width, 1), 64), c.dz_ld = (int)round_up(p.vocab, 64);
-  c.tile_n = plan.few ? kFewWords : plan.logits.kind == kLargeTile ? 128 : 64;
-  c.tiles = (int)((p.vocab + c.tile_n - 1) / c.tile_n);
+  c.tile_n = plan.tile_n, c.tiles = plan.tiles;
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     char* const begin = workspace + at;
@@ -544,7 +541,7 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     for (c.first = 0; c.first < c.tokens; c.first += c.rows) {
       c.rows = std::min(c.rows, c.tokens - c.first);
       plan.few ? launch_few_logits(c, bf16, s) : launch_logits(c, plan.logits, bf16, s);
-      launch_rows(c, bf16, s);
+      launch_rows(c, plan.row_threads, bf16, s);
     }
     return status_of_launches();
   }
@@ -566,7 +563,7 @@ int run(const tsenor_head& p, LossCall c, void* workspace, size_t workspace_byte
     else
       bf16 ? gather_kernel<true, false><<<padded, kThreads, 0, s>>>(piece) : gather_kernel<false, false><<<padded, kThreads, 0, s>>>(piece);
     plan.few ? launch_few_logits(piece, bf16, s) : launch_logits(piece, plan.logits, bf16, s);
-    launch_rows(piece, bf16, s);
+    launch_rows(piece, plan.row_threads, bf16, s);
     if (plan.both.use && c.width) {
       piece.head_first = 0, piece.head_rows = c.vocab;
       launch_both(piece, plan.both, bf16, s);

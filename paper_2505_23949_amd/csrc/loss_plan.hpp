@@ -139,6 +139,8 @@ struct LossPlan {
   bool direct;   // no gather: rows are the tokens in their order
   bool counted;  // exponentials counted from a number for a row
   bool picked;   // several entries to a token, put in order for the tiles that they are in
+  int row_threads;  // of the workgroup that goes through a token's sums and exponentials
+  int tile_n, tiles;  // words of a part of a row's sums, such parts
 };
 
 inline LossPlan loss_plan(const LossShape& p) {
@@ -172,6 +174,12 @@ inline LossPlan loss_plan(const LossShape& p) {
   plan.direct = !gradients && (plan.few || (p.in_place && p.states_too && p.tokens <= kTileTokens && plan.logits.kind == kSmallTile));
   // (few tokens and direct tiles look through all entries)
   plan.picked = p.teacher && p.k > 1 && !plan.few && !plan.direct;
+  plan.tile_n = plan.few ? kFewWords : plan.logits.kind == kLargeTile ? 128 : 64;
+  plan.tiles = (int)((p.vocab + plan.tile_n - 1) / plan.tile_n);
+  // 1024 threads where there are few tokens with many words (126 x 116032 x 128: 36 -> 23 us) or several entries (100 x 32000 x 1024 with 8 and both
+  // gradients, the call: 88 -> 82; scores of it lose 0.6), a wave where a token has little to do, so that more of them wait at a time (7744 x 512, one
+  // entry: 32 -> 15 us).
+  plan.row_threads = tokens <= 2 * kCus && (p.k > 4 || plan.tiles > 1024) ? 1024 : tokens > 4 * kCus && p.vocab <= 2048 && p.k <= 64 ? 64 : 256;
   plan.counted = p.bf16 && p.dh && !p.dweight && !plan.few && plan.logits.kind == kLargeTile && plan.rows * p.vocab >= kWithoutPass;
   return plan;
 }

@@ -6,13 +6,42 @@ from test_gpu_loss import Case, loss  # noqa: F401  (loss: a fixture)
 
 pytestmark = pytest.mark.gpu
 
-# (tokens, vocab, width, dtype, k): so much to read again that the entries' logits come from the tiles, of one entry and of several; rows by 64, by 256
+# (tokens, vocab, width, dtype, k): gathered calls whose entries' logits come from the tiles, of one entry and of several; rows by 64, by 256
 # and by 1024 threads
 FROM_TILES = [(4096, 2500, 4096, "bf16", 1), (2100, 130, 8192, "bf16", 1), (1000, 600, 8192, "f32", 1), (1500, 2500, 4096, "bf16", 3), (2100, 1500, 8192, "bf16", 16),
-              (400, 900, 2048, "f32", 40)]
+              (400, 900, 2048, "f32", 40), (60, 70001, 64, "bf16", 1), (18, 66000, 72, "f32", 1)]
 
 
 @pytest.mark.parametrize("tokens,vocab,width,dtype,k", FROM_TILES)
 def test_entries_from_the_tiles(loss, tokens, vocab, width, dtype, k):  # noqa: F811
     case = Case(tokens, vocab, width, dtype, k=k, left_out=0.1, temperature=1.5).reference("cuda")
     case.run(loss).check()
+
+
+# (tokens, vocab, width, dtype, k) of scores that look through all entries: few tokens, tiles that read everything in place; one round of entries and many
+SCORES = [(1, 700, 72, "bf16", 2), (1, 700, 72, "f32", 256), (16, 1003, 64, "bf16", 33), (16, 1003, 515, "f32", 5), (7, 40, 64, "bf16", 40), (1, 17000, 64, "bf16", 8),
+          (17, 900, 192, "bf16", 3), (48, 17000, 64, "bf16", 70), (64, 333, 128, "bf16", 256), (33, 130, 1856, "bf16", 9), (40, 700, 64, "bf16", 1)]
+
+
+@pytest.mark.parametrize("tokens,vocab,width,dtype,k", SCORES)
+def test_scores_look_for_their_entries(loss, tokens, vocab, width, dtype, k):  # noqa: F811
+    case = Case(tokens, vocab, width, dtype, k=k, left_out=0.1 * (tokens > 1), temperature=0.8)
+    gen = torch.Generator().manual_seed(k)
+    case.ids[torch.rand(tokens, k, generator=gen) < 0.2] = vocab                     # outside the vocabulary, by one
+    case.ids[torch.rand(tokens, k, generator=gen) < 0.1] = -2 ** 40
+    case.ids[0, 0], case.ids[0, -1] = vocab - 1, vocab - 1                           # the last word, twice where there are several
+    case.reference().run(loss, dh=False, dweight=False).check()
+
+
+@pytest.mark.parametrize("tokens,dh", [(5, False), (40, False), (40, True), (300, True)])
+@pytest.mark.parametrize("k", [1, 6])
+def test_entries_in_a_wider_matrix(loss, tokens, dh, k):  # noqa: F811
+    case = Case(tokens, 700, 64, "bf16", k=k).reference()
+    case.describe(loss, dh=dh, dweight=dh)
+    ids, logits = torch.full((tokens, k + 5), -7, device="cuda"), torch.full((tokens, k + 3), float("nan"), device="cuda")
+    ids[:, 2:2 + k], logits[:, 3:] = case.ids.cuda(), case.logits.cuda()
+    p = loss.make_distill(case.gpu["h"], case.gpu["weight"], ids[:, 2:2 + k], logits[:, 3:], dloss=case.gpu["dloss"], **case.out)
+    assert loss.tsenor_distill_workspace_bytes(p) == case.work.numel()
+    loss.tsenor_distill(p, case.work)
+    torch.cuda.synchronize()
+    case.check()
