@@ -19,8 +19,9 @@
  *     Gradients are summed in single precision and rounded to `dtype` once.  Of bf16 matrices, the gradient of a logit is rounded to bf16
  *     before it is multiplied: 2^-9 of itself, at random.
  *   - Tokens that are left out (no target, no entries) have loss, logarithm and gradients 0, whatever their hidden state is.
- *   - NaN and infinite logits make the loss of their token NaN, and with it the gradients it takes part in; an infinite or NaN entry of the
- *     head may do so to all tokens.
+ *   - A logit that is NaN or infinite makes the loss of its token NaN, and with it the gradients it takes part in; but a word whose logit is
+ *     minus infinity has probability 0: the loss is infinite if the word is the target (or an entry with a share of q), and what it is without the
+ *     word if not.  (Of fp32 matrices a product beyond single precision may be NaN.)  An infinite or NaN entry of the head may make NaN of all tokens.
  */
 #ifndef TSENOR_LOSS_H
 #define TSENOR_LOSS_H

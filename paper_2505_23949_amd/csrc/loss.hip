@@ -221,7 +221,8 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossCall c) {
     if (lane == 0) most[wave] = z;
     __syncthreads();
     if (threadIdx.x == 0) {
-      c.refs[row] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+      const float ref = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), sum = most[0] + most[1] + most[2] + most[3];
+      c.refs[row] = sum == sum ? ref : sum;  // (NaN if there is one: its row is NaN whatever it is counted from, and needs no other way)
       if (row == 0) *c.again = 0;
     }
   }

@@ -259,7 +259,7 @@ __device__ __forceinline__ void store_staged(const uint8_t* staged, int valid, R
 }
 
 // Exponentials of a row counted from one number: a lane's sums up to here are taken (2^22 of them stay far inside single precision, and what they
-// are divided by, times a weight, inside its other end).
+// are divided by, times a weight, inside its other end).  Nothing can be counted from minus infinity, either.
 constexpr float kMostOverRef = 0x1p59f;
 
 // What becomes of a tile of logits.
@@ -372,7 +372,7 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
         }
       }
     }
-    if (COUNTED && row < m && v > kMostOverRef) *c.again = 1;  // (whoever finds one writes the same)
+    if (COUNTED && row < m && (v > kMostOverRef || largest == -__builtin_inff())) *c.again = 1;  // (whoever finds one writes the same)
     if (apart) {  // (rare where there are many words: once more, rather than a comparison with each)
       const int target = (int)entries[j] - 4 * TN * q;
       v = 0.0f;
