@@ -26,7 +26,12 @@ __device__ __forceinline__ float teacher_of(const LossCall& c, int64_t token, in
   return u * c.inverse_temperature;
 }
 
-// what is left of x (infinities and NaN have nothing left; the largest numbers round up to infinity, which they are then)
+// two values rounded to bf16, but the largest numbers of single precision, which would round up to infinity, to the largest of bf16
+__device__ __forceinline__ uint32_t plane_of(float a, float b) {
+  const auto near = [](float x) { return fabsf(x) < __builtin_inff() ? __builtin_amdgcn_fmed3f(x, -0x1.FEp127f, 0x1.FEp127f) : x; };
+  return pack_bf16(near(a), near(b));
+}
+// what is left of x (infinities and NaN have nothing left)
 __device__ __forceinline__ float remainder_of(float x, uint32_t rounded) {
   return (rounded & kInfinityBits) == kInfinityBits ? 0.0f : x - __uint_as_float(rounded);
 }
@@ -44,7 +49,7 @@ __device__ __forceinline__ void store_planes(void* row, int ld, int c, const flo
       uint32_t w[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        w[k] = pack_bf16(rest[2 * k], rest[2 * k + 1]);
+        w[k] = plane == 0 ? plane_of(rest[2 * k], rest[2 * k + 1]) : pack_bf16(rest[2 * k], rest[2 * k + 1]);
         rest[2 * k] = remainder_of(rest[2 * k], w[k] << 16), rest[2 * k + 1] = remainder_of(rest[2 * k + 1], w[k] & 0xFFFF0000u);
       }
       __builtin_memcpy(static_cast<uint16_t*>(row) + plane * ld + c, w, 16);

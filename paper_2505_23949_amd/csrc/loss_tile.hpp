@@ -33,7 +33,7 @@ constexpr bool is_in_place(int use) { return use == kLogitsInPlace || use == kLo
 //   The order of the columns in the sum is free as long as both operands agree on it: half q of a wave holds, of half h of a block, its
 //   columns 32 h + 16 q to 32 h + 16 q + 15.
 //
-// Single precision: x = x1 + x2 + x3 exactly, with x1 the nearest bf16 value to x, x2 to x - x1 and x3 the rest, and of the nine products of
+// Single precision: x = x1 + x2 + x3 exactly, with x1 the nearest (finite) bf16 value to x, x2 to x - x1 and x3 the rest, and of the nine products of
 // two such sums six are made, x1 y1, x1 y2, x2 y1, x2 y2, x1 y3 and x3 y1; the others are below 2^-25 of x y.  bf16 products run 16 times as
 // fast as those of fp32, so six of them take 0.4 of one in fp32.  Rows of the operands then hold three planes one behind the other, and the
 // sum goes over six pairs of planes, as if it were six times as long.

@@ -45,3 +45,18 @@ def test_a_word_of_probability_zero(loss, tokens, vocab, width, dtype, dh, dweig
         assert ((got["dh"][its, 0] - want).abs() <= (2.02 * 2.0 ** -8 if dtype == "bf16" else 128 * 2.0 ** -24) * want.abs()).all()
     if dweight:
         assert ((got["dweight"] - case.want["dweight"]).abs() <= case.off["dweight"])[:, 1:].all()
+
+
+@pytest.mark.parametrize("k", [0, 3])
+@pytest.mark.parametrize("tokens,vocab,width,dh,dweight", [(100, 300, 64, True, True), (100, 300, 77, False, False), (400, 2000, 64, True, False), (9, 300, 64, True, True)])
+def test_the_largest_numbers_of_single_precision(loss, tokens, vocab, width, dh, dweight, k):  # noqa: F811
+    """They round up to infinity in bf16, of which matrices in single precision are put together."""
+    most = torch.finfo(torch.float32).max
+    case = Case(tokens, vocab, width, "f32", k=k)
+    case.h[:, 0], case.weight[:, 0] = 2.0 ** -125, 0.0
+    case.h[:, 1], case.weight[:, 1] = 0.0, 2.0 ** -125
+    case.weight[3, 0], case.h[5, 1] = most, -most
+    case.weight[vocab - 1, 0], case.h[tokens - 1, 1] = -3.3999e38, 3.395e38
+    case.dloss = 0.25 + 0.5 * torch.rand(tokens, generator=torch.Generator().manual_seed(1))  # (half the largest, or its neighbour in dweight has no room)
+    case.dloss[5] = case.dloss[tokens - 1] = 0.1
+    case.reference().run(loss, dh=dh, dweight=dweight).check()
