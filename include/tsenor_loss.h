@@ -11,8 +11,9 @@
  * can be captured in a HIP graph, sums have a fixed order and there are no atomics; counts may be zero, and pointers to arrays without
  * elements NULL).  Besides:
  *   - The logits of a call are never all kept.  They are made and used in tiles; a call that wants gradients keeps what becomes their
- *     gradients, 2 bytes a logit (bf16) or 10 (fp32), for as many tokens as 2 GiB hold, and goes on to the next ones then (with a sum
- *     of dweight in fp32 beside it, for bf16).
+ *     gradients, 2 bytes a logit (bf16) or 10 (fp32), for as many tokens as 2 GiB hold, and goes
+ *     on to the next ones then (with a sum of dweight in fp32 beside it, for bf16).  Copies of the tokens' hidden states take up to as much, and
+ *     so do sums with entries.
  *   - Loss and gradients are one call: nothing but a weight for each token comes between the loss and its gradients, and the product
  *     with the head is made once for both.
  *   - Logits, sums of exponentials and losses are in single precision, and a cross entropy near 0 is right to its own digits and never below 0.

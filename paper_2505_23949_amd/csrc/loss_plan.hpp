@@ -94,7 +94,8 @@ inline BothPlan both_plan(int64_t tokens, int64_t vocab, int64_t width, int64_t 
 }
 
 // ---- a call ------------------------------------------------------------------------------------------------------------------
-constexpr int64_t kPieceBytes = (int64_t)1 << 31;  // of dz (and, without gradients, 10 times the sums of the parts of tiles)
+// Of dz (or, without gradients, 10 times the sums of the parts of tiles), of the hidden states, and of sums and entries: each.
+constexpr int64_t kPieceBytes = (int64_t)1 << 31;
 constexpr int kPieceRows = 256;                    // pieces are a multiple of this
 constexpr int64_t kMostRows = (int64_t)1 << 22;    // (a grid has fewer than 2^32 threads; a row takes 256 of them)
 constexpr int kPairs = 6;                          // of planes, that a product in single precision takes
@@ -148,8 +149,9 @@ inline LossPlan loss_plan(const LossShape& p) {
   LossPlan plan = {};
   const auto round_up = [](int64_t n, int64_t to) { return (n + to - 1) / to * to; };
   const bool gradients = p.dh || p.dweight;
-  const int64_t row_bytes = gradients ? round_up(p.vocab, 64) * (p.bf16 ? 2 : 10) : (p.vocab + 63) / 64 * 8 * 10;
-  const int64_t most = std::min(std::max<int64_t>(kPieceBytes / std::max<int64_t>(row_bytes, 1) / kPieceRows * kPieceRows, kPieceRows), kMostRows);
+  const int64_t parts = (p.vocab + 63) / 64, of_states = round_up(std::max<int64_t>(p.width, 1), 64) * (p.bf16 ? 2 : 6);
+  const int64_t row_bytes = std::max({gradients ? parts * 64 * (p.bf16 ? 2 : 10) : parts * 8 * 10, of_states, parts * 10 + 8 * (int64_t)p.k + 8});
+  const int64_t most = std::min(std::max<int64_t>(kPieceBytes / row_bytes / kPieceRows * kPieceRows, kPieceRows), kMostRows);
   const int64_t pieces = std::max<int64_t>((p.tokens + most - 1) / most, 1);
   plan.rows = std::min(round_up((p.tokens + pieces - 1) / pieces, kPieceRows), round_up(p.tokens, 16));
 
