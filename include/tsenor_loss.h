@@ -11,7 +11,7 @@
  * can be captured in a HIP graph, sums have a fixed order and there are no atomics; counts may be zero, and pointers to arrays without
  * elements NULL).  Besides:
  *   - The logits of a call are never all kept.  They are made and used in tiles; a call that wants gradients keeps what becomes their
- *     gradients, 2 bytes a logit (bf16) or 10 (fp32), for as many tokens as 2 GiB hold, and goes
+ *     gradients, 2 bytes a logit (bf16) or 10 (fp32), for as many tokens as 2 GiB hold but 256 at the least (5 GiB at 2^21 words in fp32), and goes
  *     on to the next ones then (with a sum of dweight in fp32 beside it, for bf16).  Copies of the tokens' hidden states take up to as much, and
  *     so do sums with entries.
  *   - Loss and gradients are one call: nothing but a weight for each token comes between the loss and its gradients, and the product
