@@ -17,13 +17,12 @@ __device__ __forceinline__ float wave_max(float v) {
   return fmaxf(v, lane_xor<32>(v));
 }
 
-// logit of an entry by the teacher, over the temperature; -infinity where it takes no part
+// logit of an entry by the teacher; -infinity where it takes no part
 __device__ __forceinline__ float teacher_of(const LossCall& c, int64_t token, int i) {
   const int64_t id = c.ids[token * c.ids_ld + i];
   if (id < 0 || id >= c.vocab) return -__builtin_inff();
   const int64_t at = token * c.teacher_ld + i;
-  const float u = c.teacher_bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(c.teacher)[at] << 16) : static_cast<const float*>(c.teacher)[at];
-  return u * c.inverse_temperature;
+  return c.teacher_bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(c.teacher)[at] << 16) : static_cast<const float*>(c.teacher)[at];
 }
 
 // two values rounded to bf16, but the largest numbers of single precision, which would round up to infinity, to the largest of bf16
@@ -279,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void head_kernel(LossCall c, uint16_t* he
 }
 
 // A workgroup to a token: lse, loss; exponentials into dz.
-// Exponents here are counted from `largest`.
+// Exponents here are counted from `largest`, the teacher's from `top` (before the temperature, which may take either beyond single precision).
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   constexpr int kSize = BF16 ? 2 : 4, kWaves = THREADS / kWave, kMine = 2;
@@ -331,7 +330,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   for (int u = 0; u < kMine; ++u)
     if (u * THREADS + (int)threadIdx.x < c.tiles) total += mine[u].y * exp_from(mine[u].x, largest, c.scale, 0.0f);
   for (int t = kMine * THREADS + (int)threadIdx.x; t < c.tiles; t += THREADS) total += sums[t].y * exp_from(sums[t].x, largest, c.scale, 0.0f);
-  for (int i = (int)threadIdx.x; i < c.k; i += THREADS) all += expf(teacher[i] - top);
+  for (int i = (int)threadIdx.x; i < c.k; i += THREADS) all += expf((teacher[i] - top) * c.inverse_temperature);
   total = wave_sum(total), all = wave_sum(all);
   __syncthreads();
   if (lane == 0) part[0][wave] = total, part[1][wave] = all;
@@ -346,7 +345,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(LossCall c) {
   const float unit = c.dz ? c.largest_weight[0] : 1.0f, weight = c.dloss ? (unit > 0.0f ? c.dloss[token] / unit : c.dloss[token]) : 1.0f;
   float loss = 0.0f;
   for (int i = (int)threadIdx.x; i < c.k; i += THREADS) {
-    const float s = dots[i], u = teacher[i] - top, p = c.teacher ? expf(u) / all : 1.0f, own = exp_from(s, largest, c.scale, bits);
+    const float s = dots[i], u = (teacher[i] - top) * c.inverse_temperature, p = c.teacher ? expf(u) / all : 1.0f, own = exp_from(s, largest, c.scale, bits);
     const float off = fmaf(largest - s, c.inverse_temperature, log_total);  // lse - z
     q[i] = p, dentry[i] = own / total;
     if (c.k == 1)

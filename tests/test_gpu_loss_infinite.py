@@ -60,3 +60,15 @@ def test_the_largest_numbers_of_single_precision(loss, tokens, vocab, width, dh,
     case.dloss = 0.25 + 0.5 * torch.rand(tokens, generator=torch.Generator().manual_seed(1))  # (half the largest, or its neighbour in dweight has no room)
     case.dloss[5] = case.dloss[tokens - 1] = 0.1
     case.reference().run(loss, dh=dh, dweight=dweight).check()
+
+
+@pytest.mark.parametrize("teacher", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,dh", [(5, False), (40, False), (40, True), (200, True)])
+def test_teachers_of_the_largest_and_lowest_numbers(loss, tokens, dh, teacher):  # noqa: F811
+    """Finite logits take part, though over the temperature they are beyond single precision (a mask of the type's lowest value)."""
+    case = Case(tokens, 300, 64, "bf16", k=4, temperature=0.25, teacher=teacher)
+    most = torch.finfo(teacher).max
+    case.logits[0, :], case.logits[1, 1:], case.logits[2, :2], case.logits[3, :] = -most, -most, most, torch.tensor([most, -most, 0.0, -math.inf])
+    case.logits[4, :] = torch.tensor([-math.inf, -most, -math.inf, -most])
+    case.reference().run(loss, dh=dh, dweight=dh).check()
+    assert (case.out["loss"][:5] != 0).all()
