@@ -53,7 +53,7 @@ __device__ __forceinline__ Raw8<BF16> load_end(const char* row, int k, int width
 template <bool BF16>
 __global__ __launch_bounds__(kWaves* kWave) void few_logits_kernel(LossCall c) {
   __shared__ floatx4 parts[kWaves][kWave];
-  __shared__ float logits[kFewTokens][kFewWords];
+  __shared__ __align__(16) float logits[kFewTokens][kFewWords];
   constexpr int kSize = BF16 ? 2 : 4;
   const int lane = (int)threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int rows = rows_of(c), first = (int)blockIdx.x * kFewWords;
