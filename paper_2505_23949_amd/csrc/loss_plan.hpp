@@ -101,8 +101,10 @@ constexpr int64_t kMostRows = (int64_t)1 << 22;    // (a grid has fewer than 2^3
 constexpr int kPairs = 6;                          // of planes, that a product in single precision takes
 constexpr int kFewTokens = 16, kFewWords = 16;     // of the kernel for few tokens: words of a workgroup
 constexpr int kTileTokens = 64;                    // of the smallest tile
-// Logits from which on dh alone is made without the pass that makes dz of the exponentials (4 bytes a logit at 4.8 TB/s): us of the call with the
-// pass and without 512 x 32000 x 4096 274.5, 279, 4096 x 128256 x 4096 6838, 6520.
+// Logits from which on dh alone is made without the pass that makes dz of the exponentials (4 bytes a logit at 4.8 TB/s, and a launch and the looks at
+// c.refs for it): us of the call with the pass and without 512 x 32000 x 4096 (16 million) 273, 271, 4096 x 4096 x 4096 (17) 259, 267, 700 x 32000 x 2048
+// (22) 223, 222, 1024 x 32000 x 1024 (33) 200, 184, 2048 x 32000 x 2048 with 8 entries (66) 525, 495, 2048 x 50257 x 1024 (103) 508, 446, 8192 x 16384 x
+// 4096 (134) 1785, 1774, 4096 x 50264 x 2048 with 32 (206) 1603, 1485, 8192 x 32000 x 512 (262) 845, 670, 4096 x 128256 x 1024 (525) 2464, 2115.
 constexpr int64_t kWithoutPass = 20000000;
 
 // dh of up to kFewTokens from the head as it stands, in blocks of columns; `words` (whole lines of 64) to a workgroup, four workgroups to a CU
@@ -165,7 +167,13 @@ inline LossPlan loss_plan(const LossShape& p) {
     plan.both = both_plan(tokens, p.vocab, p.width, blocks(p.vocab), blocks(tokens), apart);
   }
   // Up to 16 tokens: straight from memory in fp32, where tiles would need a copy of the head that nothing else needs, or are few (us of the call:
-  // 3 x 1216 x 2326 27.4, 10.4 so, 4 x 1650 x 6912 with dh 58.3, 39.6; but in whole lines 1 x 32000 x 2048 29.0, 33.6).
+  // 3 x 1216 x 2326 27.4, 10.4 so, 4 x 1650 x 6912 with dh 58.3, 39.6).  In whole lines, scores of 1 token and of 16 with 8 entries, tiles and so:
+  //   4096 x 512  11.0, 8.6 and 12.5, 9.4     x 4096  18.9, 11.8 and 21.0, 15.2
+  //   8192 x 512  10.9, 8.7 and 12.4, 10.2    x 4096  22.8, 18.9 and 24.8, 22.7
+  //  12288 x 512  10.6, 9.6 and 12.5, 11.0    x 4096  25.8, 24.4 and 28.0, 29.5
+  //  16384 x 512  11.1, 10.6 and 12.7, 12.1   x 4096  30.8, 29.7 and 32.5, 36.5
+  //  32000 x 512  11.5, 12.8 and 13.1, 16.0   x 4096  44.4, 48.8 and 46.0, 64.6
+  // 128256 x 512  34.8, 31.2 and 37.0, 40.1   x 4096  175, 186 and 177, 288
   plan.few = p.tokens <= kFewTokens && (!p.bf16 || p.vocab < 64 * kCus || !p.in_place);
   // dh likewise, where tiles would need that copy (us of the call, with copy and tiles and so: fp32 1 x 116621 x 5083 2553, 1096, 16 x 1000 x 513 31.8,
   // 25.3, bf16 2 x 4484 x 897 40.0, 30.6, 16 x 30001 x 1027 75.3, 77.2; without a need for the copy as well as tiles: bf16 3 x 4096 x 1024 24.0,
