@@ -18,7 +18,10 @@
  *     with the head is made once for both.
  *   - Logits, sums of exponentials and losses are in single precision, and a cross entropy near 0 is right to its own digits and never below 0.
  *     Gradients are summed in single precision and rounded to `dtype` once.  Of bf16 matrices, the gradient of a logit is rounded to bf16
- *     before it is multiplied: 2^-9 of itself, at random.
+ *     before it is multiplied, by at most 2^-8 of itself to either side (and its exponential, in calls with dweight_out or of few logits, to fp16
+ *     before that, by 2^-11).
+ *   - Gradients are made relative to the largest finite weight (dloss) of the call's tokens: of a token whose weight is less than 2^-90 of it they
+ *     lose digits, and may be 0.
  *   - Tokens that are left out (no target, no entries) have loss, logarithm and gradients 0, whatever their hidden state is.
  *   - A logit that is NaN or infinite makes the loss of its token NaN, and with it the gradients it takes part in; but a word whose logit is
  *     minus infinity has probability 0: the loss is infinite if the word is the target (or an entry with a share of q), and what it is without the

@@ -187,9 +187,9 @@ inline LossPlan loss_plan(const LossShape& p) {
   plan.picked = p.teacher && p.k > 1 && !plan.few && !plan.direct;
   plan.tile_n = plan.few ? kFewWords : plan.logits.kind == kLargeTile ? 128 : 64;
   plan.tiles = (int)((p.vocab + plan.tile_n - 1) / plan.tile_n);
-  // 1024 threads where there are few tokens with many words (126 x 116032 x 128: 36 -> 23 us) or several entries (100 x 32000 x 1024 with 8 and both
-  // gradients, the call: 88 -> 82; scores of it lose 0.6), a wave where a token has little to do, so that more of them wait at a time (7744 x 512, one
-  // entry: 32 -> 15 us).
+  // 1024 threads where there are few tokens with many words or several entries, a wave where a token has little to do, so that more of them wait at a time.
+  // us of the call so and with 256 threads: 126 x 116032 x 128 with both gradients 83, 102, 100 x 32000 x 1024 with 8 entries 84, 89 (but scores, 1 x
+  // 32000 x 2048 with 8, 26.2, 25.5); 7744 x 512 x 1216 91, 100, 4000 x 1500 x 256 with 64 entries 67, 74.
   plan.row_threads = tokens <= 2 * kCus && (p.k > 4 || plan.tiles > 1024) ? 1024 : tokens > 4 * kCus && p.vocab <= 2048 && p.k <= 64 ? 64 : 256;
   plan.counted = p.bf16 && p.dh && !p.dweight && !plan.few && plan.logits.kind == kLargeTile && plan.rows * p.vocab >= kWithoutPass;
   return plan;

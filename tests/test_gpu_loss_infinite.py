@@ -72,3 +72,15 @@ def test_teachers_of_the_largest_and_lowest_numbers(loss, tokens, dh, teacher): 
     case.logits[4, :] = torch.tensor([-math.inf, -most, -math.inf, -most])
     case.reference().run(loss, dh=dh, dweight=dh).check()
     assert (case.out["loss"][:5] != 0).all()
+
+
+@pytest.mark.parametrize("k", [0, 3])
+@pytest.mark.parametrize("tokens,vocab,width,dtype,dweight", [(100, 300, 64, "bf16", True), (100, 300, 64, "f32", True), (9, 300, 64, "f32", False), (538, 40884, 64, "bf16", False)])
+def test_weights_far_apart(loss, tokens, vocab, width, dtype, dweight, k):  # noqa: F811
+    """Gradients are made relative to the largest weight: those of a token whose own is 2^-80 of it are as right as its neighbours'."""
+    case = Case(tokens, vocab, width, dtype, k=k)
+    case.dloss[1::2] *= 2.0 ** -80
+    case.dloss[0] = 2.0 ** 20
+    case.reference("cuda").run(loss, dweight=dweight).check()
+    small = case.out["dh"].float().cpu()[1::2]
+    assert (small.abs().amax(1) > 0).all() and float(small.abs().max()) < 2.0 ** -60
