@@ -348,16 +348,17 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
     largest = fmaxf(largest, lane_xor<32>(largest));
     if (COUNTED && row < m) largest = c.refs[row];
     const float base = largest == -__builtin_inff() ? 0.0f : largest;
-    float v = 0.0f;
+    float v = 0.0f, of_group[4];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float x[4 * TN];
+      of_group[g] = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int t = 0; t < TN; ++t) {
           x[e * TN + t] = exp_from(sum[t][j][4 * g + e], base, c.scale, kBits);
-          v += x[e * TN + t];
+          of_group[g] += x[e * TN + t];
         }
       const int col = col0 + 8 * TN * g;
       if (c.exps && row < m && col < c.dz_ld) {
@@ -372,18 +373,24 @@ __device__ __forceinline__ void finish_logits(const LossCall& c, floatx16 (&sum)
         }
       }
     }
-    if (COUNTED && row < m && (v > kMostOverRef || largest == -__builtin_inff())) *c.again = 1;  // (whoever finds one writes the same)
-    if (apart) {  // (rare where there are many words: once more, rather than a comparison with each)
-      const int target = (int)entries[j] - 4 * TN * q;
-      v = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-#pragma unroll
-        for (int t = 0; t < TN; ++t) {
-          const float x = exp_from(sum[t][j][e], base, c.scale, kBits);
-          v += TN * (e / 4 * 8 + e % 4) + t == target ? 0.0f : x;
-        }
+    if constexpr (COUNTED) {
+      v = (of_group[0] + of_group[1]) + (of_group[2] + of_group[3]);
+      if (row < m && (v > kMostOverRef || largest == -__builtin_inff())) *c.again = 1;  // (whoever finds one writes the same)
     }
+    if (apart) {  // a row's only entry: the group that it is in once more, without it, rather than a comparison with each word
+      const int target = (int)min(entries[j], (uint32_t)(32 * TN - 1)), group = target / (4 * TN);  // (of other rows, the last: not used)
+      const float* const logits = reinterpret_cast<const float*>(staged + r * Staged<TN, 4>::kStride) + group * 4 * TN;
+      float rest = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4 * TN; ++e) {
+        const float x = exp_from(logits[e], base, c.scale, kBits);
+        rest += e == target % (4 * TN) ? 0.0f : x;
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        if (entries[j] < 32 * TN && group == 2 * g + q) of_group[g] = rest;
+    }
+    v = (of_group[0] + of_group[1]) + (of_group[2] + of_group[3]);
     v += lane_xor<32>(v);
     if (q == 0 && row < m && wave_col < n) c.sums[(int64_t)row * c.tiles + wave_col / (32 * TN)] = make_float2(largest, v);
   }
