@@ -38,8 +38,8 @@ constexpr bool is_in_place(int use) { return use == kLogitsInPlace || use == kLo
 // fast as those of fp32, so six of them take 0.4 of one in fp32.  Rows of the operands then hold three planes one behind the other, and the
 // sum goes over six pairs of planes, as if it were six times as long.
 //
-// What bounds it: 256 x 256 is held by the card's power (8192 tokens x 128256 x 4096: 1.5-1.6 GHz, matrix cores busy 76-80 % of the cycles;
-// the loss alone of 4096 x 128256 x 4096 3.40 ms, of operands that are all zeros 2.51).  dh of 8192 x 128256 x 4096, two rounds of 2004 blocks,
+// What bounds it: 256 x 256 is held by the card's power (8192 tokens x 128256 x 4096: 1.5-1.6 GHz, matrix cores busy 74-81 % of the cycles;
+// the loss alone of 4096 x 128256 x 4096 3.22-3.37 ms, of operands that are all zeros 2.51).  dh of 8192 x 128256 x 4096, two rounds of 2004 blocks,
 // 6.29 ms: 1.57 us a block of one tile on each CU, 1.37 PFLOP/s.  Logits of 1433 x 50257 x 1024, five rounds of 16 blocks, 164 us: 33 us a round, of
 // which 8 are not its blocks.  Four rows of waves (WM) put two waves on a SIMD, of which one works while the other waits: with two, and twice the
 // rows to a wave, dW of 1433 x 50257 x 1024 took 169 us (157 so); full rounds are about the same (dh of 4096 x 32768 x 4096 806 and 813).
