@@ -6,14 +6,14 @@
 //   logits    z = h W^T in tiles: of each tile's rows the largest logit and the sum of exponentials, and, where gradients are wanted,
 //             the exponentials; the logits of entries, and of a token's only one not its exponential in the sum
 //   rows      for each token: the sums of its tiles joined, the logits of its entries, its loss; the exponentials become dz
-//
-// The exponential of a target (or of a teacher's only entry) stays apart from the sum of all others, `rest`, until the end: loss = log(1 + rest / own),
-// and the gradient of its logit is -rest / (rest + own).  Of a word that a model has learned both are small, and as lse - z and p - 1 they would be what is left of
-// numbers thousands of times as large; and its logit is the one that the sum would have had, from the same product.  (Losses of 1e-6 to
-// 0.1, 8192 words of width 512 to 37543 of 64: from a second product and lse - z up to 4.6e-6 off, which can be more than all of one, and some below 0; at
-// most 3.9e-6 of itself off so, none below 0.  Scores of many tokens pay for the look at their words, 4096 x 32000 x 64 78 us, 84.6, x 256 106, 112.)
 //   products  dh = dz W, dW = dz^T h
 // How many tokens count is known on the GPU only.  Grids are made for all of them, and workgroups without work end at once.
+//
+// The exponential of a target (or of a teacher's only entry) stays apart from the sum of all others, `rest`, until the end: loss = log(1 + rest / own),
+// and the gradient of its logit is -rest / (rest + own).  Of a word that a model has learned both are small, and as lse - z and p - 1 they would be what is
+// left of numbers thousands of times as large; and its logit is the one that the sum would have had, from the same product.  (Losses of 1e-6 to
+// 0.1, 8192 words of width 512 to 37543 of 64: from a second product and lse - z up to 4.6e-6 off, which can be more than all of one, and some below 0; at
+// most 3.9e-6 of itself off so, none below 0.  Scores of many tokens pay for the look at their words, 4096 x 32000 x 64 78 us, 84.6, x 256 106, 112.)
 #pragma once
 #include "layer.hpp"
 #include "loss_plan.hpp"
