@@ -5,7 +5,7 @@
 //   gather    the piece's hidden states, one behind the other; outputs of those left out are cleared
 //   logits    z = h W^T in tiles: of each tile's rows the largest logit and the sum of exponentials, and, where gradients are wanted,
 //             the exponentials; the logits of entries, and of a token's only one not its exponential in the sum
-//   rows      for each token: the sums of its tiles joined, the logits of its entries, its loss; the exponentials become dz
+//   rows      for each token: the sums of its tiles joined, its loss; the exponentials become dz
 //   products  dh = dz W, dW = dz^T h
 // How many tokens count is known on the GPU only.  Grids are made for all of them, and workgroups without work end at once.
 //
